@@ -67,8 +67,9 @@ typedef enum {
     BS_ERR_SCRATCH_LIMIT = 8 /* bs_spmm_static: needs more than the static scratch   */
 } bs_status;
 
-/* storage type of W and vals; x, X, y, Y and all accumulation are fp32 */
-typedef enum { BS_F32 = 0, BS_F16 = 1 } bs_dtype;
+/* storage type of W and vals; x, X, y, Y and all accumulation are fp32.
+ * BS_BF16 is for the calls on 4-bit matrices and logits (last section) alone. */
+typedef enum { BS_F32 = 0, BS_F16 = 1, BS_BF16 = 2 } bs_dtype;
 
 /* ---- set-up ---------------------------------------------------------------- */
 
@@ -329,6 +330,94 @@ int bs_lstm_sequence_finish(const void* vals, const uint8_t* idx, int dtype, int
  * lanes per workgroup, workgroups, LDS bytes, LDS bytes of the finishing kernel. */
 int bs_lstm_sequence_plan(int dtype, int64_t H, int64_t I, int bank, int k, int threads, int workgroups,
                           int64_t* out, int n_out);
+
+/* ---- language models: 4-bit matrices, expert layers, log probabilities ------------
+ *
+ * What a model needs beside its pruned matrices: matrices that do not bear pruning (output
+ * products, experts) in 4 bits, and what is made of the last product.  dtype here is the type
+ * of the dense matrix, of activations and of logits: BS_F32, BS_F16 or BS_BF16; results have
+ * the type of what they are made from.  All sums are fp32, each result is rounded once.
+ *
+ * Format of a 4-bit matrix M x K: codes are E2M1 numbers, bit 3 the sign, bits 0..2 one of the
+ * magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6.  Element k of a row is in byte k / 2, in the low half
+ * for even k.  A row takes 16 * ceil(K / 32) bytes, codes behind K are 0.  A group of `group`
+ * (32, 64 or 128) consecutive elements of a row has one binary16 scale, [M][ceil(K / group)]:
+ * a code stands for its number times its group's scale.  M, K <= 2^24.  Codes must be 16-byte
+ * aligned, scales 4-byte; other pointers only as their type asks.
+ */
+size_t bs_q4_codes_bytes(int64_t M, int64_t K);                /* 0 if the shape is invalid */
+size_t bs_q4_scales_bytes(int64_t M, int64_t K, int group);
+
+/*
+ * W       DEVICE in   M x K row-major, contiguous
+ * scale = binary16(largest magnitude of the group * fp32(1/6), rounded to fp32), at most 65504; the code is the
+ * one whose number times the scale is nearest, the even code of two that are equally near.
+ * A group whose scale is 0 has magnitude 0 throughout.  NaN or Inf inside W: undefined.
+ */
+int bs_q4_pack(const void* W, int dtype, int64_t M, int64_t K, int group, uint8_t* codes, uint16_t* scales, void* stream);
+/* W  DEVICE out  M x K: the values the codes stand for, rounded to dtype */
+int bs_q4_unpack(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t K, int group, void* W, int dtype,
+                 void* stream);
+
+/*
+ * y[n][r] = sum_k W[r][k] * x[n][k] for N vectors, 1 <= N <= 65535
+ * x  DEVICE in   N rows of K, ldx >= K elements apart       y  DEVICE out  N rows of M, ldy >= M apart
+ * The weights' values and the products are exact, whatever dtype is.  The order of the additions
+ * depends on dtype, M, K, group and N alone.  workspace as for bs_spmm.
+ */
+size_t bs_q4_gemv_workspace_bytes(int dtype, int64_t M, int64_t K, int group, int64_t N);
+int bs_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t K, int group, const void* x, int dtype,
+               int64_t N, int64_t ldx, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A layer of E experts, of which every token uses top_k:
+ *     l = R x;   the top_k largest l, the lower expert first among equals
+ *     p = softmax of the chosen l (renormalise != 0), or softmax of all l at the chosen ones
+ *     y = sum over the chosen e of p_e * W2_e (silu(G_e x) * (U_e x)),   silu(a) = a / (1 + exp(-a))
+ * x        DEVICE in   T rows of D, ldx apart        y  DEVICE out  T rows of D, ldy apart
+ * router   DEVICE in   E x D, same type as x
+ * w1, s1   DEVICE in   E 4-bit matrices of 2F x D: the rows of G_e, then those of U_e
+ * w2, s2   DEVICE in   E 4-bit matrices of D x F
+ * ids      DEVICE out  T x top_k chosen experts, largest weight first     weights  DEVICE out  their p, fp32
+ * T <= BS_MOE_TOKENS_MAX, E <= BS_MOE_EXPERTS_MAX, top_k <= min(E, BS_MOE_TOP_K_MAX).
+ * workspace: bs_q4_moe_workspace_bytes(...) bytes, 16-byte aligned, as for bs_spmm.
+ */
+#define BS_MOE_TOKENS_MAX 64
+#define BS_MOE_EXPERTS_MAX 1024
+#define BS_MOE_TOP_K_MAX 32
+size_t bs_q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k, int group);
+int bs_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E,
+              const uint8_t* w1, const uint16_t* s1, const uint8_t* w2, const uint16_t* s2, int64_t F, int group,
+              int top_k, int renormalise, void* y, int64_t ldy, int32_t* ids, float* weights, void* workspace,
+              size_t workspace_bytes, void* stream);
+
+/*
+ * T rows of V logits, ld >= V elements apart (V < 2^31; only as aligned as the type), one target each (< 0: none)
+ *   lse[t]      log of the sum of exp(logits)        entropy[t]  of the row's distribution
+ *   logprob[t]  of the target; 0 without one, NaN for one that is not below V
+ *   top_values, top_ids  [T][top_n] the top_n largest log probabilities, the lower index first among equals;
+ *               0 <= top_n <= min(V, BS_LOGPROBS_TOP_MAX), may be NULL for 0
+ * A logit of -inf is a word that cannot be: log probability -inf, nothing in the entropy, last among the alternatives.  A row of
+ * nothing else has lse -inf, entropy 0.  A logit that is NaN or +inf makes the row's lse, entropy and log probabilities NaN.
+ * All outputs fp32, ids int32.  workspace as for bs_spmm.
+ */
+#define BS_LOGPROBS_TOP_MAX 64
+size_t bs_logprobs_workspace_bytes(int dtype, int64_t T, int64_t V, int top_n);
+int bs_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets, int top_n,
+                float* logprob, float* entropy, float* lse, float* top_values, int32_t* top_ids, void* workspace,
+                size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient with respect to the logits, from those with respect to logprob and entropy:
+ *   grad[t][v] = g_logprob[t] ([v == target] - p[t][v]) - g_entropy[t] p[t][v] (log p[t][v] + entropy[t])
+ * lse, entropy  DEVICE in   as bs_logprobs gave them          g_logprob, g_entropy  DEVICE in  T fp32 each
+ * grad          DEVICE out  T rows of V, same type as the logits, ldg >= V apart; may be the logits themselves
+ * entropy and g_entropy may both be NULL: the log probability's gradient alone.  A row without a target has that of its
+ * entropy alone; a row in which nothing is left (lse <= -1e30: all words -inf, or all the lowest fp32 / bfloat16 number) 0.
+ */
+int bs_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets,
+                         const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,
+                         void* grad, int64_t ldg, void* stream);
 
 /* ---- dense baseline the sparse path is compared with (Sec. 4: the paper's
  *      dense column; here a hand-written kernel on the same GPU) ----------- */

@@ -20,13 +20,15 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libbs.so")
 
-BS_F32, BS_F16 = 0, 1
+BS_F32, BS_F16, BS_BF16 = 0, 1, 2
 
 EXPORTS = (
     "bs_init", "bs_nnz", "bs_vals_bytes", "bs_idx_bytes", "bs_status_str", "bs_prune_pack", "bs_spmv",
     "bs_spmv_ex", "bs_spmv_plan", "bs_spmm_workspace_bytes", "bs_spmm_plan", "bs_spmm", "bs_spmm_static", "bs_spmm_static_limit", "bs_dense_gemv", "bs_dense_gemm",
     "bs_lstm_step", "bs_lstm_sequence", "bs_lstm_sequence_ex", "bs_lstm_sequence_finish", "bs_lstm_sequence_plan", "bs_reprune",
     "bs_idx_bytes_wide", "bs_prune_pack_wide", "bs_spmv_wide", "bs_spmm_workspace_bytes_wide", "bs_spmm_plan_wide", "bs_spmm_wide",
+    "bs_q4_codes_bytes", "bs_q4_scales_bytes", "bs_q4_pack", "bs_q4_unpack", "bs_q4_gemv_workspace_bytes", "bs_q4_gemv",
+    "bs_q4_moe_workspace_bytes", "bs_q4_moe", "bs_logprobs_workspace_bytes", "bs_logprobs", "bs_logprobs_backward",
 )
 
 
@@ -95,6 +97,22 @@ def load_library():
     lib.bs_spmm_wide.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, i64, i64, vp, i64, vp, sz, vp]
     for name in ("bs_prune_pack_wide", "bs_spmv_wide", "bs_spmm_wide"):
         getattr(lib, name).restype = i32
+    lib.bs_q4_codes_bytes.argtypes = [i64, i64]
+    lib.bs_q4_scales_bytes.argtypes = [i64, i64, i32]
+    lib.bs_q4_gemv_workspace_bytes.argtypes = [i32, i64, i64, i32, i64]
+    lib.bs_q4_moe_workspace_bytes.argtypes = [i32, i64, i64, i64, i32, i32, i32]
+    lib.bs_logprobs_workspace_bytes.argtypes = [i32, i64, i64, i32]
+    for name in ("bs_q4_codes_bytes", "bs_q4_scales_bytes", "bs_q4_gemv_workspace_bytes", "bs_q4_moe_workspace_bytes",
+                 "bs_logprobs_workspace_bytes"):
+        getattr(lib, name).restype = sz
+    lib.bs_q4_pack.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp]
+    lib.bs_q4_unpack.argtypes = [vp, vp, i64, i64, i32, vp, i32, vp]
+    lib.bs_q4_gemv.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, i64, vp, i64, vp, sz, vp]
+    lib.bs_q4_moe.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, i64, i32, i32, i32, vp, i64, vp, vp, vp, sz, vp]
+    lib.bs_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bs_logprobs_backward.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    for name in ("bs_q4_pack", "bs_q4_unpack", "bs_q4_gemv", "bs_q4_moe", "bs_logprobs", "bs_logprobs_backward"):
+        getattr(lib, name).restype = i32
     lib.bs_init.argtypes = []
     for name in ("bs_init", "bs_prune_pack", "bs_spmv", "bs_spmv_ex", "bs_spmm", "bs_spmm_static", "bs_dense_gemv",
                  "bs_dense_gemm", "bs_lstm_step", "bs_lstm_sequence", "bs_lstm_sequence_ex", "bs_lstm_sequence_finish", "bs_lstm_sequence_plan", "bs_reprune"):
@@ -140,13 +158,13 @@ def _out(t: torch.Tensor, what: str, n: int) -> torch.Tensor:
     return t
 
 
-def _rows(t: torch.Tensor, what: str) -> int:
-    """A 2-D fp32 GPU tensor whose rows are contiguous (a column slice of a wider
+def _rows(t: torch.Tensor, what: str, dtype=torch.float32) -> int:
+    """A 2-D GPU tensor of this type whose rows are contiguous (a column slice of a wider
     row-major tensor is fine): returns its leading dimension in elements."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a tensor on the GPU")
-    if t.dtype != torch.float32 or t.dim() != 2:
-        raise TypeError(f"{what} must be a 2-D float32 tensor")
+    if t.dtype != dtype or t.dim() != 2:
+        raise TypeError(f"{what} must be a 2-D {str(dtype)[6:]} tensor")
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{what}: elements of a row must be adjacent")
     ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
@@ -617,3 +635,209 @@ def bs_reprune(vals, idx, bank: int, k2: int, out=None):
     _check(load_library().bs_reprune(_ptr(vals), _ptr(idx), code, M, K, bank, k, k2, _ptr(vals2),
                                      _ptr(idx2), _stream()), "bs_reprune")
     return vals2, idx2
+
+
+# ---- language models: 4-bit matrices, expert layers, log probabilities
+
+_TYPES = {torch.float32: BS_F32, torch.float16: BS_F16, torch.bfloat16: BS_BF16}
+
+
+def _type_code(t, what: str) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a tensor on the GPU")
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{what} must be float32, float16 or bfloat16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _group(group: int) -> int:
+    if group not in (32, 64, 128):
+        raise ValueError(f"group must be 32, 64 or 128, got {group}")
+    return group
+
+
+def _codes(codes, scales, K: int, group: int, what: str = "codes"):
+    """Checks a 4-bit matrix [.., M, K]: returns the number of its rows."""
+    _dev(codes, what, torch.uint8)
+    _dev(scales, "scales", torch.float16)
+    _group(group)
+    if codes.dim() < 2 or K < 1 or codes.shape[-1] != 16 * -(-K // 32):
+        raise ValueError(f"{what} must be [.., M, {16 * -(-K // 32)}] for K = {K}")
+    if tuple(scales.shape) != (*codes.shape[:-1], -(-K // group)):
+        raise ValueError(f"scales must be {[*codes.shape[:-1], -(-K // group)]}")
+    return codes.numel() // codes.shape[-1]
+
+
+def _own_workspace(workspace, need: int, device):
+    workspace = _workspace(workspace, need, device)
+    if isinstance(workspace, torch.Tensor) and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def bs_q4_codes_bytes(M: int, K: int) -> int:
+    return load_library().bs_q4_codes_bytes(M, K)
+
+
+def bs_q4_scales_bytes(M: int, K: int, group: int) -> int:
+    return load_library().bs_q4_scales_bytes(M, K, group)
+
+
+def bs_q4_pack(W, group: int = 64):
+    """W [.., M, K] on the GPU (float32, float16 or bfloat16) -> (codes uint8 [.., M, 16 * ceil(K / 32)],
+    scales float16 [.., M, ceil(K / group)]): E2M1 numbers, two a byte, with a scale per group of a row."""
+    done = (_native or _calls()).q4_pack(W, group)
+    if done is not None:
+        return done
+    code = _type_code(_dev(W, "W"), "W")
+    _group(group)
+    if W.dim() < 2:
+        raise ValueError("W must be [.., M, K]")
+    K = W.shape[-1]
+    M = W.numel() // max(K, 1)
+    codes = torch.empty((*W.shape[:-1], 16 * -(-K // 32)), dtype=torch.uint8, device=W.device)
+    scales = torch.empty((*W.shape[:-1], -(-K // group)), dtype=torch.float16, device=W.device)
+    _check(load_library().bs_q4_pack(_ptr(W), code, M, K, group, _ptr(codes), _ptr(scales), _stream()), "bs_q4_pack")
+    return codes, scales
+
+
+def bs_q4_unpack(codes, scales, K: int, group: int = 64, dtype=torch.float32, out=None):
+    """The values [.., M, K] that a 4-bit matrix stands for, rounded to dtype (of `out`, if it is given)."""
+    if out is None and isinstance(codes, torch.Tensor):
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+        _codes(codes, scales, K, group)
+        out = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
+    done = (_native or _calls()).q4_unpack(codes, scales, K, group, out)
+    if done is not None:
+        return done
+    M = _codes(codes, scales, K, group)
+    code = _type_code(_dev(out, "out"), "out")
+    if out.numel() != M * K:
+        raise ValueError(f"out must be {[*codes.shape[:-1], K]}")
+    _check(load_library().bs_q4_unpack(_ptr(codes), _ptr(scales), M, K, group, _ptr(out), code, _stream()), "bs_q4_unpack")
+    return out
+
+
+def bs_q4_gemv_workspace_bytes(dtype: int, M: int, K: int, group: int, N: int) -> int:
+    return load_library().bs_q4_gemv_workspace_bytes(dtype, M, K, group, N)
+
+
+def bs_q4_gemv(codes, scales, group: int, x, out=None, workspace=None):
+    """W . x for a 4-bit matrix [M, K]: x [K] -> y [M], or one row per vector, x [N, K] -> y [N, M], of x's type
+    (float32, float16, bfloat16).  Rows of x and `out` may be slices of wider ones.  `workspace`: at least
+    bs_q4_gemv_workspace_bytes(...) bytes, or one from torch's allocator."""
+    y = (_native or _calls()).q4_gemv(codes, scales, group, x, out, workspace)
+    if y is not None:
+        return y
+    code = _type_code(x, "x")
+    if x.dim() not in (1, 2):
+        raise ValueError("x must be [K] or [N, K]")
+    X = x if x.dim() == 2 else _dev(x, "x").unsqueeze(0)
+    ldx, (N, K) = _rows(X, "x", x.dtype), X.shape
+    M = _codes(codes, scales, K, group)
+    if codes.dim() != 2:
+        raise ValueError("codes must be [M, ..]")
+    y = torch.empty((*x.shape[:-1], M), dtype=x.dtype, device=x.device) if out is None else out
+    if not isinstance(y, torch.Tensor) or tuple(y.shape) != (*x.shape[:-1], M):
+        raise ValueError(f"out must be {[*x.shape[:-1], M]}")
+    ldy = _rows(y if x.dim() == 2 else _dev(y, "out").unsqueeze(0), "out", x.dtype)
+    lib = load_library()
+    workspace, ws_bytes = _own_workspace(workspace, lib.bs_q4_gemv_workspace_bytes(code, M, K, group, N), x.device)
+    _check(lib.bs_q4_gemv(_ptr(codes), _ptr(scales), M, K, group, _ptr(x), code, N, ldx, _ptr(y), ldy, _ptr(workspace), ws_bytes,
+                          _stream()), "bs_q4_gemv")
+    return y
+
+
+def bs_q4_moe_workspace_bytes(dtype: int, T: int, D: int, F: int, E: int, top_k: int, group: int) -> int:
+    return load_library().bs_q4_moe_workspace_bytes(dtype, T, D, F, E, top_k, group)
+
+
+def bs_q4_moe(x, router, w1, s1, w2, s2, group: int, top_k: int, renormalise: bool = True, workspace=None):
+    """A mixture-of-experts layer for a few tokens: x [T, D] -> (y [T, D], ids int32 [T, top_k], weights float32
+    [T, top_k]).  router [E, D] has x's type; w1, s1 are the experts' 4-bit gate and up matrices [E, 2F, D] (gate rows
+    first), w2, s2 their down matrices [E, D, F]."""
+    done = (_native or _calls()).q4_moe(x, router, w1, s1, w2, s2, group, top_k, bool(renormalise), workspace)
+    if done is not None:
+        return done
+    code = _type_code(x, "x")
+    ldx, (T, D) = _rows(x, "x", x.dtype), x.shape
+    _dev(router, "router", x.dtype)
+    if router.dim() != 2 or router.shape[1] != D:
+        raise ValueError(f"router must be [E, {D}]")
+    E = router.shape[0]
+    _codes(w1, s1, D, group, "w1")
+    if w1.dim() != 3 or w1.shape[0] != E or w1.shape[1] % 2:
+        raise ValueError(f"w1 must be [{E}, 2F, ..]")
+    F = w1.shape[1] // 2
+    _codes(w2, s2, F, group, "w2")
+    if w2.dim() != 3 or tuple(w2.shape[:2]) != (E, D):
+        raise ValueError(f"w2 must be [{E}, {D}, ..]")
+    top_k = int(top_k)
+    y = torch.empty((T, D), dtype=x.dtype, device=x.device)
+    ids = torch.empty((T, max(top_k, 0)), dtype=torch.int32, device=x.device)
+    weights = torch.empty((T, max(top_k, 0)), dtype=torch.float32, device=x.device)
+    if top_k < 1:
+        raise BsError(2, "bs_q4_moe")
+    lib = load_library()
+    workspace, ws_bytes = _own_workspace(workspace, lib.bs_q4_moe_workspace_bytes(code, T, D, F, E, top_k, group), x.device)
+    _check(lib.bs_q4_moe(_ptr(x), code, T, ldx, D, _ptr(router), E, _ptr(w1), _ptr(s1), _ptr(w2), _ptr(s2), F, group, top_k,
+                         int(bool(renormalise)), _ptr(y), D, _ptr(ids), _ptr(weights), _ptr(workspace), ws_bytes, _stream()), "bs_q4_moe")
+    return y, ids, weights
+
+
+def _logits(logits, targets):
+    code = _type_code(logits, "logits")
+    ld = _rows(logits, "logits", logits.dtype)
+    _dev(targets, "targets", torch.int64)
+    if tuple(targets.shape) != (logits.shape[0],):
+        raise ValueError(f"targets must be [{logits.shape[0]}]")
+    return code, ld, *logits.shape
+
+
+def bs_logprobs_workspace_bytes(dtype: int, T: int, V: int, top_n: int) -> int:
+    return load_library().bs_logprobs_workspace_bytes(dtype, T, V, top_n)
+
+
+def bs_logprobs(logits, targets, top_n: int = 0, workspace=None):
+    """Rows of logits [T, V] and an int64 target each (negative: none) -> (logprob [T], entropy [T], lse [T],
+    top_values [T, top_n], top_ids int32 [T, top_n]), all float32 but the ids."""
+    done = (_native or _calls()).logprobs(logits, targets, top_n, workspace)
+    if done is not None:
+        return done
+    code, ld, T, V = _logits(logits, targets)
+    top_n = int(top_n)
+    if top_n < 0:
+        raise BsError(2, "bs_logprobs")
+    logprob, entropy, lse = (torch.empty(T, dtype=torch.float32, device=logits.device) for _ in range(3))
+    values = torch.empty((T, top_n), dtype=torch.float32, device=logits.device)
+    ids = torch.empty((T, top_n), dtype=torch.int32, device=logits.device)
+    lib = load_library()
+    workspace, ws_bytes = _own_workspace(workspace, lib.bs_logprobs_workspace_bytes(code, T, V, top_n), logits.device)
+    _check(lib.bs_logprobs(_ptr(logits), code, T, V, ld, _ptr(targets), top_n, _ptr(logprob), _ptr(entropy), _ptr(lse),
+                           _ptr(values), _ptr(ids), _ptr(workspace), ws_bytes, _stream()), "bs_logprobs")
+    return logprob, entropy, lse, values, ids
+
+
+def bs_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entropy, out=None):
+    """The gradient [T, V], of the logits' type, from those of logprob and entropy [T]; lse and entropy as bs_logprobs gave
+    them.  entropy and g_entropy may both be None.  `out` may be the logits."""
+    done = (_native or _calls()).logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entropy, out)
+    if done is not None:
+        return done
+    code, ld, T, V = _logits(logits, targets)
+    if (entropy is None) != (g_entropy is None):
+        raise ValueError("entropy and g_entropy go together")
+    for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy")):
+        if t is None and name in ("entropy", "g_entropy"):
+            continue
+        _dev(t, name, torch.float32)
+        if t.numel() != T:
+            raise ValueError(f"{name} must have {T} elements")
+    grad = torch.empty((T, V), dtype=logits.dtype, device=logits.device) if out is None else out
+    ldg = _rows(grad, "out", logits.dtype)
+    if tuple(grad.shape) != (T, V):
+        raise ValueError(f"out must be [{T}, {V}]")
+    _check(load_library().bs_logprobs_backward(_ptr(logits), code, T, V, ld, _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(g_logprob),
+                                               _ptr(g_entropy), _ptr(grad), ldg, _stream()), "bs_logprobs_backward")
+    return grad

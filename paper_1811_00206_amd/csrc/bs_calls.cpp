@@ -68,9 +68,9 @@ struct Packed {
     at::Tensor floats(at::IntArrayRef size) const { return at::empty(size, vals->options().dtype(at::kFloat)); }
 };
 
-// leading dimension of a 2-D fp32 tensor whose rows are contiguous; -1 if it is not one
-int64_t row_pitch(const at::Tensor& t) {
-    if (t.scalar_type() != at::kFloat || t.dim() != 2) return -1;
+// leading dimension of a 2-D tensor of this type whose rows are contiguous; -1 if it is not one
+int64_t row_pitch(const at::Tensor& t, at::ScalarType type = at::kFloat) {
+    if (t.scalar_type() != type || t.dim() != 2) return -1;
     const int64_t rows = t.size(0), n = t.size(1);
     if (n > 1 && t.stride(1) != 1) return -1;
     const int64_t ld = rows > 1 ? t.stride(0) : std::max<int64_t>(n, 1);
@@ -331,6 +331,249 @@ PyObject* lstm_sequence(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- 4-bit matrices and logits
+
+// activations, dense matrices and logits of those calls
+int any_dtype(const at::Tensor& t) {
+    return t.scalar_type() == at::kFloat ? BS_F32 : t.scalar_type() == at::kHalf ? BS_F16 : t.scalar_type() == at::kBFloat16 ? BS_BF16 : -1;
+}
+bool group_arg(PyObject* obj, int& group) { return int_arg(obj, group) && (group == 32 || group == 64 || group == 128); }
+
+// codes [.., M, 16 * ceil(K / 32)] and scales [.., M, ceil(K / group)], M counting all rows
+struct Q4 {
+    const at::Tensor *codes, *scales;
+    int64_t M;
+    bool read(PyObject* c, PyObject* s, int64_t K, int group) {
+        codes = gpu_tensor(c, at::kByte);
+        scales = gpu_tensor(s, at::kHalf);
+        if (!codes || !scales || K < 1) return false;
+        const int64_t d = codes->dim();
+        if (d < 2 || scales->dim() != d || codes->size(d - 1) != 16 * ((K + 31) / 32) || scales->size(d - 1) != (K + group - 1) / group)
+            return false;
+        for (int64_t i = 0; i < d - 1; ++i)
+            if (codes->size(i) != scales->size(i)) return false;
+        M = codes->numel() / codes->size(d - 1);
+        return M >= 1;
+    }
+    const uint8_t* c() const { return static_cast<const uint8_t*>(codes->const_data_ptr()); }
+    const uint16_t* s() const { return static_cast<const uint16_t*>(scales->const_data_ptr()); }
+};
+
+// a workspace of a call: the caller's, or one from torch's allocator
+struct Workspace {
+    PyObject* given;
+    at::Tensor own;
+    void* p = nullptr;
+    size_t bytes = 0;
+    bool read() {
+        if (given == Py_None) return true;
+        const at::Tensor* w = gpu_tensor(given);
+        if (!w || !w->is_contiguous()) return false;
+        p = w->mutable_data_ptr();
+        bytes = (size_t)w->numel() * w->element_size();
+        return true;
+    }
+    void allocate(size_t need, const at::Tensor& like) {
+        if (given != Py_None || !need) return;
+        own = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+        p = own.mutable_data_ptr();
+        bytes = need;
+    }
+};
+
+template <size_t N>
+PyObject* tuple_of(at::Tensor (&t)[N]) {
+    PyObject* all = PyTuple_New(N);
+    for (size_t i = 0; all && i < N; ++i) {
+        PyObject* one = THPVariable_Wrap(std::move(t[i]));
+        if (!one) Py_CLEAR(all);
+        else PyTuple_SET_ITEM(all, i, one);
+    }
+    return all;
+}
+
+// (W, group) -> (codes, scales)
+PyObject* q4_pack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int group;
+    if (n != 2 || !group_arg(args[1], group)) Py_RETURN_NONE;
+    const at::Tensor* W = gpu_tensor(args[0]);
+    if (!W || W->dim() < 2 || !W->is_contiguous() || !W->numel()) Py_RETURN_NONE;
+    const int dtype = any_dtype(*W);
+    if (dtype < 0) Py_RETURN_NONE;
+    const int64_t K = W->size(-1), M = W->numel() / K;
+    at::Tensor out[2];
+    const int status = enqueue([&](void* st) {
+        at::DimVector size(W->sizes());
+        size.back() = 16 * ((K + 31) / 32);
+        out[0] = at::empty(size, W->options().dtype(at::kByte));
+        size.back() = (K + group - 1) / group;
+        out[1] = at::empty(size, W->options().dtype(at::kHalf));
+        return bs_q4_pack(W->const_data_ptr(), dtype, M, K, group, static_cast<uint8_t*>(out[0].mutable_data_ptr()),
+                          static_cast<uint16_t*>(out[1].mutable_data_ptr()), st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_q4_pack");
+    return tuple_of(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, K, group, out) -> out
+PyObject* q4_unpack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int group, K;
+    Q4 w;
+    if (n != 5 || !int_arg(args[2], K) || !group_arg(args[3], group) || !w.read(args[0], args[1], K, group)) Py_RETURN_NONE;
+    const at::Tensor* out = gpu_tensor(args[4]);
+    if (!out || !out->is_contiguous() || out->numel() != w.M * K) Py_RETURN_NONE;
+    const int dtype = any_dtype(*out);
+    if (dtype < 0) Py_RETURN_NONE;
+    const int status = enqueue([&](void* st) { return bs_q4_unpack(w.c(), w.s(), w.M, K, group, out->mutable_data_ptr(), dtype, st); });
+    if (status != BS_OK) return failed(self, status, "bs_q4_unpack");
+    Py_INCREF(args[4]);
+    return args[4];
+    END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, group, x, out, workspace) -> y
+PyObject* q4_gemv(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int group;
+    if (n != 6 || !group_arg(args[2], group)) Py_RETURN_NONE;
+    const at::Tensor* x = gpu_tensor(args[3]);
+    if (!x) Py_RETURN_NONE;
+    const int dtype = any_dtype(*x);
+    const bool one = x->dim() == 1;
+    if (dtype < 0 || x->dim() < 1 || x->dim() > 2) Py_RETURN_NONE;
+    const int64_t N = one ? 1 : x->size(0), K = x->size(-1);
+    const int64_t ldx = one ? (K > 1 && x->stride(0) != 1 ? -1 : K) : row_pitch(*x, x->scalar_type());
+    Q4 w;
+    if (ldx < 0 || !w.read(args[0], args[1], K, group) || w.codes->dim() != 2) Py_RETURN_NONE;
+    Workspace ws{args[5]};
+    if (!ws.read()) Py_RETURN_NONE;
+    at::Tensor y;
+    const at::Tensor* out = &y;
+    int64_t ldy = w.M;
+    if (args[4] != Py_None) {
+        if (!(out = gpu_tensor(args[4])) || out->scalar_type() != x->scalar_type() || out->dim() != x->dim()) Py_RETURN_NONE;
+        ldy = one ? (out->is_contiguous() ? w.M : -1) : row_pitch(*out, x->scalar_type());
+        if (ldy < 0 || out->size(-1) != w.M || (!one && out->size(0) != N)) Py_RETURN_NONE;
+    }
+    const size_t need = bs_q4_gemv_workspace_bytes(dtype, w.M, K, group, N);
+    const int status = enqueue([&](void* st) {
+        if (out == &y) y = one ? at::empty({w.M}, x->options()) : at::empty({N, w.M}, x->options());
+        ws.allocate(need, *x);
+        return bs_q4_gemv(w.c(), w.s(), w.M, K, group, x->const_data_ptr(), dtype, N, ldx, out->mutable_data_ptr(), ldy, ws.p, ws.bytes,
+                          st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_q4_gemv");
+    return result(args[4], y);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, router, w1, s1, w2, s2, group, top_k, renormalise, workspace) -> (y, ids, weights)
+PyObject* q4_moe(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int group, top_k;
+    if (n != 10 || !group_arg(args[6], group) || !int_arg(args[7], top_k)) Py_RETURN_NONE;
+    const at::Tensor *x = gpu_tensor(args[0]), *router = gpu_tensor(args[1]);
+    if (!x || !router || router->scalar_type() != x->scalar_type() || !router->is_contiguous() || router->dim() != 2) Py_RETURN_NONE;
+    const int dtype = any_dtype(*x);
+    const int64_t ldx = row_pitch(*x, x->scalar_type());
+    if (dtype < 0 || ldx < 0) Py_RETURN_NONE;
+    const int64_t T = x->size(0), D = x->size(1), E = router->size(0);
+    Q4 w1, w2;
+    if (!w1.read(args[2], args[3], D, group) || w1.codes->dim() != 3 || router->size(1) != D) Py_RETURN_NONE;
+    const int64_t F = w1.codes->size(1) / 2;
+    if (w1.codes->size(0) != E || w1.codes->size(1) % 2 || E > INT32_MAX || top_k < 1) Py_RETURN_NONE;
+    if (!w2.read(args[4], args[5], F, group) || w2.codes->dim() != 3 || w2.codes->size(0) != E || w2.codes->size(1) != D) Py_RETURN_NONE;
+    Workspace ws{args[9]};
+    if (!ws.read()) Py_RETURN_NONE;
+    at::Tensor out[3];
+    const size_t need = bs_q4_moe_workspace_bytes(dtype, T, D, F, (int)E, top_k, group);
+    const int status = enqueue([&](void* st) {
+        out[0] = at::empty({T, D}, x->options());
+        out[1] = at::empty({T, top_k}, x->options().dtype(at::kInt));
+        out[2] = at::empty({T, top_k}, x->options().dtype(at::kFloat));
+        ws.allocate(need, *x);
+        return bs_q4_moe(x->const_data_ptr(), dtype, T, ldx, D, router->const_data_ptr(), (int)E, w1.c(), w1.s(), w2.c(), w2.s(), F, group,
+                         top_k, args[8] == Py_True, out[0].mutable_data_ptr(), D, static_cast<int32_t*>(out[1].mutable_data_ptr()),
+                         static_cast<float*>(out[2].mutable_data_ptr()), ws.p, ws.bytes, st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_q4_moe");
+    return tuple_of(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// rows of logits and their targets
+struct Logits {
+    const at::Tensor *x, *targets;
+    int dtype;
+    int64_t T, V, ld;
+    bool read(PyObject* l, PyObject* t) {
+        x = gpu_tensor(l);
+        targets = gpu_tensor(t, at::kLong);
+        if (!x || !targets || (dtype = any_dtype(*x)) < 0 || (ld = row_pitch(*x, x->scalar_type())) < 0) return false;
+        T = x->size(0);
+        V = x->size(1);
+        return targets->dim() == 1 && targets->size(0) == T;
+    }
+    const int64_t* t() const { return static_cast<const int64_t*>(targets->const_data_ptr()); }
+};
+
+// (logits, targets, top_n, workspace) -> (logprob, entropy, lse, top_values, top_ids)
+PyObject* logprobs(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Logits g;
+    int top;
+    if (n != 4 || !g.read(args[0], args[1]) || !int_arg(args[2], top) || top < 0) Py_RETURN_NONE;
+    Workspace ws{args[3]};
+    if (!ws.read()) Py_RETURN_NONE;
+    at::Tensor out[5];
+    const size_t need = bs_logprobs_workspace_bytes(g.dtype, g.T, g.V, top);
+    const int status = enqueue([&](void* st) {
+        const at::TensorOptions f = g.x->options().dtype(at::kFloat);
+        for (int i = 0; i < 3; ++i) out[i] = at::empty({g.T}, f);
+        out[3] = at::empty({g.T, top}, f);
+        out[4] = at::empty({g.T, top}, f.dtype(at::kInt));
+        ws.allocate(need, *g.x);
+        float* p[4];
+        for (int i = 0; i < 4; ++i) p[i] = static_cast<float*>(out[i].mutable_data_ptr());
+        return bs_logprobs(g.x->const_data_ptr(), g.dtype, g.T, g.V, g.ld, g.t(), top, p[0], p[1], p[2], p[3],
+                           static_cast<int32_t*>(out[4].mutable_data_ptr()), ws.p, ws.bytes, st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_logprobs");
+    return tuple_of(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (logits, targets, lse, entropy, g_logprob, g_entropy, out) -> grad
+PyObject* logprobs_backward(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Logits g;
+    if (n != 7 || !g.read(args[0], args[1]) || (args[3] == Py_None) != (args[5] == Py_None)) Py_RETURN_NONE;
+    const at::Tensor* in[4] = {};
+    for (int i = 0; i < 4; ++i) {
+        if (args[2 + i] == Py_None && i % 2) continue;
+        if (!(in[i] = gpu_floats(args[2 + i], g.T))) Py_RETURN_NONE;
+    }
+    at::Tensor grad;
+    const at::Tensor* out = &grad;
+    int64_t ldg = g.V;
+    if (args[6] != Py_None) {
+        if (!(out = gpu_tensor(args[6])) || (ldg = row_pitch(*out, g.x->scalar_type())) < 0 || out->sizes() != g.x->sizes()) Py_RETURN_NONE;
+    }
+    const int status = enqueue([&](void* st) {
+        if (out == &grad) grad = at::empty({g.T, g.V}, g.x->options());
+        const float* p[4];
+        for (int i = 0; i < 4; ++i) p[i] = in[i] ? static_cast<const float*>(in[i]->const_data_ptr()) : nullptr;
+        return bs_logprobs_backward(g.x->const_data_ptr(), g.dtype, g.T, g.V, g.ld, g.t(), p[0], p[1], p[2], p[3], out->mutable_data_ptr(),
+                                    ldg, st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_logprobs_backward");
+    return result(args[6], grad);
+    END_HANDLE_TH_ERRORS
+}
+
 // () -> torch's current stream as an integer
 PyObject* stream(PyObject*, PyObject*) {
     HANDLE_TH_ERRORS
@@ -341,6 +584,7 @@ PyObject* stream(PyObject*, PyObject*) {
 #define BS_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     BS_FAST(spmv), BS_FAST(spmm), BS_FAST(prune_pack), BS_FAST(reprune), BS_FAST(lstm_step), BS_FAST(lstm_sequence),
+    BS_FAST(q4_pack), BS_FAST(q4_unpack), BS_FAST(q4_gemv), BS_FAST(q4_moe), BS_FAST(logprobs), BS_FAST(logprobs_backward),
     {"stream", stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -72,6 +72,23 @@ int launch_dense_gemv(const void* W, int dtype, int64_t M, int64_t K, const floa
                       hipStream_t st);
 int launch_dense_gemm(const void* W, int dtype, int64_t M, int64_t K, const float* X, int64_t N,
                       int64_t ldx, float* Y, int64_t ldy, hipStream_t st);
+// 4-bit matrices (bs_q4_pack.hip, bs_q4_gemv.hip, bs_q4_moe.hip) and logits (bs_logprobs.hip)
+// out: nullptr to pack W, else where the codes' values go
+int launch_q4_pack(const void* W, int dtype, int64_t M, int64_t K, int group, uint8_t* codes, uint16_t* scales, void* out, hipStream_t st);
+size_t q4_gemv_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N);
+int launch_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t K, int group, const void* x, int dtype,
+                   int64_t N, int64_t ldx, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, hipStream_t st);
+size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int top_k);
+int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,
+                  const uint16_t* s1, const uint8_t* w2, const uint16_t* s2, int64_t F, int group, int top_k, int renormalise, void* y,
+                  int64_t ldy, int32_t* ids, float* weights, void* workspace, size_t workspace_bytes, hipStream_t st);
+size_t logprobs_workspace_bytes(int dtype, int64_t T, int64_t V, int top_n);
+int launch_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets, int top_n, float* logprob,
+                    float* entropy, float* lse, float* top_values, int32_t* top_ids, void* workspace, size_t workspace_bytes,
+                    hipStream_t st);
+int launch_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets, const float* lse,
+                             const float* entropy, const float* g_logprob, const float* g_entropy, void* grad, int64_t ldg,
+                             hipStream_t st);
 inline int hip_status(hipError_t e) { return e == hipSuccess ? BS_OK : BS_ERR_HIP; }
 
 // ---- kernels that may use more than 48 KB of LDS --------------------------------

@@ -1,0 +1,522 @@
+// Log probabilities of given tokens, entropy and most likely alternatives of rows of logits, and their gradient
+// (bs.h: bs_logprobs, bs_logprobs_backward).  Bound: HBM, the logits once (the gradient: once in, once out).
+//
+// Softmax statistics in one pass: a thread keeps the largest logit m it has seen and, with u = (x - m) log2(e),
+//     s = sum 2^u,   t = sum u 2^u,   so that  lse = m + log s  and  entropy = ln2 (log2 s - t / s).
+// A batch of 32 elements moves m once.  u is cut off at -200, where 2^u is 0: a banned word, x = -inf, adds nothing to
+// either sum (and no 0 * inf), and what is no number stays so.  x - m comes first because it is exact where it matters: rows
+// whose logits are all a type's lowest value are uniform, and come out so.
+//
+// The n largest: a lower bound of the n-th largest comes out of the first batch of a slice (32 elements a thread): each of
+// the four wavefronts finds the ceil(n / 4)-th largest of its lanes' maxima, and at least n elements reach the least of
+// those.  Whatever reaches it is put into a list in LDS, a few times n elements of a row; a thread whose batch has no such
+// element, nearly every one, does one comparison for it.  In the end the list is ordered by counting, for every entry,
+// the entries before it.  Entries are 64-bit keys (value, then index), all different, so the order in which threads reach
+// the list does not matter.  Rows that flood the list (masks that leave fewer than n words, equal logits, rising ones) are
+// gone over once more with the strict bound, or n times, which is slow and right.
+#include "bs_q4.h"
+
+namespace bs {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kBatch = 32;                     // elements of a thread
+constexpr int kList = 1024;                    // keys in LDS
+constexpr int kTidy = 256;                     // a longer list is cut to its n largest before the next batch
+constexpr int kTopMax = BS_LOGPROBS_TOP_MAX;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Stats {
+    float m, s, t;      // m: -inf before anything was seen
+};
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// u, at least `least`; NaN where u is
+__device__ __forceinline__ float at_least(float u, float least) { return __builtin_elementwise_maximum(u, least); }
+
+__device__ __forceinline__ void raise(Stats& a, float m) {       // to a larger m
+    const float d = at_least((a.m - m) * kLog2e, -200.f), f = exp2_hw(d);
+    a.t = fmaf(a.s, d, a.t) * f;
+    a.s *= f;
+    a.m = m;
+}
+__device__ __forceinline__ Stats join(Stats a, Stats b) {
+    const float m = fmaxf(a.m, b.m);
+    if (a.m != m) raise(a, m);
+    if (b.m != m) raise(b, m);
+    return {m, a.s + b.s, a.t + b.t};
+}
+__device__ __forceinline__ Stats wave_join(Stats a) {
+    for (int o = 1; o < 64; o *= 2) a = join(a, Stats{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)});
+    return a;
+}
+
+struct Args {
+    const void* logits;
+    int64_t T, V, ld, first_row;
+    const int64_t* targets;
+    int n, slices;
+    int64_t slice_vectors;      // 16-byte pieces of a row in a slice
+    float *logprob, *entropy, *lse, *top_values;
+    int32_t* top_ids;
+    Stats* part_stats;          // [rows][slices]
+    uint64_t* part_keys;        // [rows][slices][n]
+};
+
+// A row as 16-byte pieces on 16-byte boundaries: piece v has the elements v * E - head .. + E - 1 of the row; those
+// before or behind the row are -inf here and nowhere looked at.
+template <typename XT>
+struct Row {
+    using T = typename XT::type;
+    static constexpr int E = 16 / sizeof(T);
+    const T* p;
+    int64_t V;
+    int head;
+    __device__ Row(const void* base, int64_t row, int64_t ld, int64_t V_) : p(static_cast<const T*>(base) + row * ld), V(V_) {
+        head = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    }
+    __device__ __forceinline__ int64_t vectors() const { return (V + head + E - 1) / E; }
+    __device__ __forceinline__ void load(int64_t v, float* out) const {
+        const int64_t e = v * E - head;
+        if (e >= 0 && e + E <= V) {
+            const uint4 a = *reinterpret_cast<const uint4*>(p + e);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if constexpr (sizeof(T) == 4) out[i] = __builtin_bit_cast(float, word_of(a, i));
+                else out[i] = XT::load((uint16_t)(word_of(a, i >> 1) >> (16 * (i & 1))));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) out[i] = e + i >= 0 && e + i < V ? XT::load(p[e + i]) : -__builtin_inff();
+        }
+    }
+};
+
+struct TopList {
+    uint64_t keys[kList];
+    uint64_t sorted[kTopMax];
+    float bound[kWaves];
+    int count, wave_count[kWaves];
+    uint64_t wave_best[kWaves];
+};
+
+// the n largest keys of the list, in order; entries behind the list's end become 0.  All threads, barriers inside.
+__device__ __forceinline__ void order_list(TopList& l, int count, int n) {
+    for (int i = threadIdx.x; i < n; i += kThreads)
+        if (i >= count) l.sorted[i] = 0;
+    for (int i = threadIdx.x; i < count; i += kThreads) {
+        const uint64_t key = l.keys[i];
+        int before = 0;
+        for (int j = 0; j < count; ++j) before += l.keys[j] > key;
+        if (before < n) l.sorted[before] = key;
+    }
+    __syncthreads();
+}
+
+// the k-th largest of the lanes' values
+__device__ __forceinline__ float kth_largest(float v, int k) {
+    float most = v;
+    for (int j = 0; j < k; ++j) {
+        most = v;
+        for (int o = 1; o < 64; o *= 2) most = fmaxf(most, __shfl_xor(most, o));
+        const uint64_t m = __ballot(v == most);
+        if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)m) - 1) v = -__builtin_inff();
+    }
+    return most;
+}
+
+// The list flooded.  First what is larger than the bound; if that is too many too, the n largest one after the other.
+// Then, where the list is short, the first elements of the row that are not larger than `fill`.
+template <typename XT>
+__device__ void flooded(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, float bound, int n) {
+    constexpr int E = Row<XT>::E;
+    __syncthreads();
+    if (threadIdx.x == 0) l.count = 0;
+    __syncthreads();
+    for (int64_t v = v0 + threadIdx.x; v < v1; v += kThreads) {
+        float x[E];
+        row.load(v, x);
+        for (int i = 0; i < E; ++i)
+            if (x[i] > bound) {
+                const int at = atomicAdd(&l.count, 1);
+                if (at < kList) l.keys[at] = order_key(x[i], (uint32_t)(v * E - row.head + i));
+            }
+    }
+    __syncthreads();
+    const int count = l.count;
+    if (count <= kList) {
+        order_list(l, count, n);
+        return;
+    }
+    uint64_t last = ~(uint64_t)0;
+    for (int j = 0; j < n; ++j) {
+        uint64_t best = 0;
+        for (int64_t v = v0 + threadIdx.x; v < v1; v += kThreads) {
+            float x[E];
+            row.load(v, x);
+            for (int i = 0; i < E; ++i) {
+                const int64_t e = v * E - row.head + i;
+                const uint64_t key = order_key(x[i], (uint32_t)e);
+                if (e >= 0 && e < row.V && key < last && key > best) best = key;
+            }
+        }
+        best = wave_max(best);
+        if ((threadIdx.x & 63) == 0) l.wave_best[threadIdx.x >> 6] = best;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) best = l.wave_best[w] > best ? l.wave_best[w] : best;
+        last = best;
+        if (threadIdx.x == 0) l.sorted[j] = best;
+        __syncthreads();
+    }
+}
+
+// Entries of sorted[] that are still 0: the first elements of the slice that are not larger than `bound` (all that are
+// larger are there already)
+template <typename XT>
+__device__ void fill(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, float bound, int n) {
+    constexpr int E = Row<XT>::E;
+    int have = 0;
+    while (have < n && l.sorted[have]) ++have;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the equals of the bound, in order of their index; then, lower than any number, what is none
+    for (int pass = 0; pass < 2 && have < n; ++pass) {
+        for (int64_t b = v0; b < v1 && have < n; b += kThreads) {
+            const int64_t v = b + threadIdx.x;
+            float x[E];
+            uint32_t mine = 0;
+            if (v < v1) {
+                row.load(v, x);
+                for (int i = 0; i < E; ++i) {
+                    const int64_t e = v * E - row.head + i;
+                    if (e >= 0 && e < row.V && (pass ? x[i] != x[i] : x[i] == bound)) mine |= 1u << i;
+                }
+            }
+            const int c = __popc(mine);
+            const int before = group_prefix_i<64>(c, lane);
+            if (lane == 63) l.wave_count[wave] = before + c;
+            __syncthreads();
+            int at = have + before, all = 0;
+            for (int w = 0; w < kWaves; ++w) {
+                if (w < wave) at += l.wave_count[w];
+                all += l.wave_count[w];
+            }
+            for (int i = 0; i < E; ++i)
+                if (mine >> i & 1) {
+                    if (at < n) l.sorted[at] = order_key(x[i], (uint32_t)(v * E - row.head + i));
+                    ++at;
+                }
+            have += all;
+            __syncthreads();
+        }
+    }
+    __syncthreads();
+}
+
+// what a log probability is made of: (x - m) - log s
+struct Norm {
+    float m, log_s;
+};
+
+__device__ __forceinline__ float logprob_of(float x, Norm z) {
+    if (z.log_s != z.log_s) return z.log_s;
+    return x == -__builtin_inff() ? x : (x - z.m) - z.log_s;      // a row without words: all are impossible
+}
+
+// a row's results, by one lane
+template <typename XT>
+__device__ __forceinline__ Norm finish(const Args& g, int64_t row, Stats st) {
+    const double log_s = log((double)st.s);
+    const Norm z{st.m, (float)log_s};
+    const bool words = st.s != 0.f;
+    g.lse[row] = words ? (float)((double)st.m + log_s) : -__builtin_inff();
+    g.entropy[row] = words ? (float)(log_s - (double)st.t / (double)st.s * 0.69314718055994530942) : 0.f;
+    const int64_t target = g.targets[row];
+    float p = 0.f;
+    if (target >= g.V) p = __builtin_nanf("");
+    else if (target >= 0) p = logprob_of(XT::load(static_cast<const typename XT::type*>(g.logits)[row * g.ld + target]), z);
+    g.logprob[row] = p;
+    return z;
+}
+
+__device__ __forceinline__ void write_top(const Args& g, int64_t row, const uint64_t* sorted, Norm z) {
+    for (int i = threadIdx.x; i < g.n; i += kThreads) {
+        g.top_values[row * g.n + i] = logprob_of(value_of_key(sorted[i]), z);
+        g.top_ids[row * g.n + i] = (int32_t)index_of_key(sorted[i]);
+    }
+}
+
+template <typename XT, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprobs_kernel(Args g) {
+    constexpr int E = Row<XT>::E, U = kBatch / E;
+    __shared__ TopList l;
+    __shared__ Stats stats[kWaves];
+    __shared__ Norm norm;
+    const int64_t r = blockIdx.x / g.slices, slice = blockIdx.x % g.slices, row_no = g.first_row + r;
+    const Row<XT> row(g.logits, row_no, g.ld, g.V);
+    const int64_t v0 = slice * g.slice_vectors, v1 = min(row.vectors(), v0 + g.slice_vectors);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (TOP && threadIdx.x == 0) l.count = 0;
+    Stats st{-__builtin_inff(), 0.f, 0.f};
+    float bound = 0.f;
+    bool flood = false;
+    for (int64_t b = v0; b < v1; b += kThreads * U) {
+        float x[kBatch];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t v = b + u * kThreads + threadIdx.x;
+            if (v < v1) row.load(v, x + u * E);
+            else
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[u * E + i] = -__builtin_inff();
+        }
+        float most = x[0];
+#pragma unroll
+        for (int i = 1; i < kBatch; ++i) most = fmaxf(most, x[i]);
+        if (most > st.m) raise(st, most);
+        const float m = st.m == -__builtin_inff() ? 0.f : st.m;
+        float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < kBatch; i += 2) {
+            const float u0 = at_least((x[i] - m) * kLog2e, -200.f), u1 = at_least((x[i + 1] - m) * kLog2e, -200.f);
+            const float p0 = exp2_hw(u0), p1 = exp2_hw(u1);
+            s0 += p0; s1 += p1;
+            t0 = fmaf(p0, u0, t0); t1 = fmaf(p1, u1, t1);
+        }
+        st.s += s0 + s1;
+        st.t += t0 + t1;
+        if constexpr (TOP) {
+            if (b == v0) {
+                const float k = kth_largest(fmaxf(most, -__builtin_inff()), (g.n + kWaves - 1) / kWaves);
+                if (lane == 0) l.bound[wave] = k;
+                __syncthreads();
+                bound = l.bound[0];
+                for (int w = 1; w < kWaves; ++w) bound = fminf(bound, l.bound[w]);
+            } else {
+                __syncthreads();
+                const int count = l.count;
+                __syncthreads();
+                if (count > kList) flood = true;      // and nothing is put into the list any more
+                else if (count > kTidy) {
+                    order_list(l, count, g.n);
+                    if (threadIdx.x < g.n) l.keys[threadIdx.x] = l.sorted[threadIdx.x];
+                    if (threadIdx.x == 0) l.count = g.n;
+                    bound = fmaxf(bound, value_of_key(l.sorted[g.n - 1]));
+                    __syncthreads();
+                }
+            }
+            if (!flood && most >= bound && most > -__builtin_inff()) {
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    if (x[i] >= bound && x[i] > -__builtin_inff()) {
+                        const int at = atomicAdd(&l.count, 1);
+                        const int64_t v = b + i / E * kThreads + threadIdx.x;
+                        if (at < kList) l.keys[at] = order_key(x[i], (uint32_t)(v * E - row.head + i % E));
+                    }
+            }
+        }
+    }
+    st = wave_join(st);
+    if (lane == 0) stats[wave] = st;
+    __syncthreads();
+    if constexpr (TOP) {
+        const int count = l.count;
+        if (flood || count > kList) flooded(l, row, v0, v1, bound, g.n);
+        else order_list(l, count, g.n);
+        // a slice can have fewer words than n that are larger than its bound
+        if (!l.sorted[g.n - 1]) fill(l, row, v0, v1, bound, g.n);
+    }
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kWaves; ++w) st = join(st, stats[w]);
+        if (g.slices == 1) norm = finish<XT>(g, row_no, st);
+        else g.part_stats[blockIdx.x] = st;
+    }
+    if constexpr (TOP) {
+        if (g.slices == 1) {
+            __syncthreads();
+            write_top(g, row_no, l.sorted, norm);
+        } else {
+            for (int i = threadIdx.x; i < g.n; i += kThreads) g.part_keys[(int64_t)blockIdx.x * g.n + i] = l.sorted[i];
+        }
+    }
+}
+
+// joins the slices of a row
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void logprobs_join_kernel(Args g) {
+    __shared__ uint64_t sorted[kTopMax];
+    __shared__ Norm norm;
+    extern __shared__ uint64_t keys[];
+    const int64_t row = g.first_row + blockIdx.x;
+    const int all = g.slices * g.n;
+    for (int i = threadIdx.x; i < all; i += kThreads) keys[i] = g.part_keys[(int64_t)blockIdx.x * all + i];
+    if (threadIdx.x < 64) {
+        Stats st{-__builtin_inff(), 0.f, 0.f};
+        for (int i = threadIdx.x; i < g.slices; i += 64) st = join(st, g.part_stats[(int64_t)blockIdx.x * g.slices + i]);
+        st = wave_join(st);
+        if (threadIdx.x == 0) norm = finish<XT>(g, row, st);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < all; i += kThreads) {
+        const uint64_t key = keys[i];
+        if (!key) continue;                 // a slice with fewer elements than n
+        int before = 0;
+        for (int j = 0; j < all; ++j) before += keys[j] > key;
+        if (before < g.n) sorted[before] = key;
+    }
+    __syncthreads();
+    write_top(g, row, sorted, norm);
+}
+
+struct BackArgs {
+    const void* logits;
+    void* grad;
+    int64_t V, ld, ldg, first_row;
+    const int64_t* targets;
+    const float *lse, *entropy, *g_logprob, *g_entropy;
+    int slices;
+};
+
+// d = p * -(g_lp + g_H (log p + H)), and g_lp at the target
+template <typename XT>
+__global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(BackArgs g) {
+    using T = typename XT::type;
+    constexpr int E = Row<XT>::E, U = 16 / E;
+    const int64_t r = blockIdx.x / g.slices, slice = blockIdx.x % g.slices, row_no = g.first_row + r;
+    const Row<XT> row(g.logits, row_no, g.ld, g.V);
+    T* const out = static_cast<T*>(g.grad) + row_no * g.ldg;
+    const bool together = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15) == 0;
+    const float lse = g.lse[row_no];
+    // A row in which a mask has left nothing has no gradient: its lse is -inf, or so near the lowest fp32 number that the
+    // differences from it are lost.
+    const bool empty = lse <= -1e30f;
+    int64_t target = g.targets[row_no];
+    const float gl = target < 0 ? 0.f : g.g_logprob[row_no], gh = g.g_entropy ? g.g_entropy[row_no] : 0.f;
+    const float at0 = -fmaf(gh, gh != 0.f ? g.entropy[row_no] : 0.f, gl);
+    if (empty) target = -1;
+    const int64_t v0 = slice * (kThreads * U), v1 = min(row.vectors(), v0 + kThreads * U);
+    float x[U][E];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t v = v0 + u * kThreads + threadIdx.x;
+        if (v < v1) row.load(v, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t v = v0 + u * kThreads + threadIdx.x, e = v * E - row.head;
+        if (v >= v1) break;
+        T d[E];
+        const int64_t mine = target - e;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float logp = empty ? -1e4f : at_least(x[u][i] - lse, -1e4f);      // exp of which is 0
+            float v = exp2_hw(logp * kLog2e) * fmaf(-gh, logp, at0);
+            if (mine == i) v += gl;
+            d[i] = XT::store(v);
+        }
+        if (together && e >= 0 && e + E <= g.V) {
+            uint4 w;
+            __builtin_memcpy(&w, d, 16);
+            *reinterpret_cast<uint4*>(out + e) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (e + i >= 0 && e + i < g.V) out[e + i] = d[i];
+        }
+    }
+}
+
+struct Plan {
+    int slices;
+    int64_t slice_vectors;
+};
+
+Plan plan_for(int dtype, int64_t T, int64_t V) {
+    const int e = 16 / dtype_bytes(dtype);
+    const int64_t vectors = (V + e - 1) / e + 1;      // one more for a row that starts between boundaries
+    // workgroups for every compute unit, but not slices of less than two pieces a thread
+    int64_t slices = 1;
+    while (slices < 32 && T * slices < 512 && vectors / (slices * 2) >= 2 * kThreads) slices *= 2;
+    Plan p;
+    p.slice_vectors = (vectors + slices - 1) / slices;
+    p.slices = (int)((vectors + p.slice_vectors - 1) / p.slice_vectors);
+    return p;
+}
+
+size_t stats_bytes(int64_t T, const Plan& p) { return ((size_t)T * p.slices * sizeof(Stats) + 15) / 16 * 16; }
+
+template <typename XT>
+int launch(Args g, hipStream_t st) {
+    const int64_t most = ((int64_t)1 << 23) / g.slices;      // rows of a launch: a grid has fewer than 2^32 lanes
+    Stats* const stats = g.part_stats;
+    for (int64_t r = 0; r < g.T; r += most) {
+        const int64_t rows = g.T - r < most ? g.T - r : most;
+        g.first_row = r;
+        g.part_stats = stats;
+        const dim3 grid((unsigned)(rows * g.slices));
+        if (g.n) hipLaunchKernelGGL((logprobs_kernel<XT, true>), grid, dim3(kThreads), 0, st, g);
+        else hipLaunchKernelGGL((logprobs_kernel<XT, false>), grid, dim3(kThreads), 0, st, g);
+        int rc = hip_status(hipGetLastError());
+        if (rc != BS_OK) return rc;
+        if (g.slices == 1) continue;
+        hipLaunchKernelGGL(logprobs_join_kernel<XT>, dim3((unsigned)rows), dim3(kThreads), (size_t)g.slices * g.n * 8, st, g);
+        rc = hip_status(hipGetLastError());
+        if (rc != BS_OK) return rc;
+    }
+    return BS_OK;
+}
+
+template <typename XT>
+int launch_backward(BackArgs g, int64_t T, hipStream_t st) {
+    constexpr int E = Row<XT>::E, U = 16 / E;
+    g.slices = (int)(((g.V + E - 1) / E + 1 + kThreads * U - 1) / (kThreads * U));
+    const int64_t most = ((int64_t)1 << 23) / g.slices > 1 ? ((int64_t)1 << 23) / g.slices : 1;
+    for (int64_t r = 0; r < T; r += most) {
+        g.first_row = r;
+        const int64_t rows = T - r < most ? T - r : most;
+        hipLaunchKernelGGL(logprobs_backward_kernel<XT>, dim3((unsigned)(rows * g.slices)), dim3(kThreads), 0, st, g);
+        const int rc = hip_status(hipGetLastError());
+        if (rc != BS_OK) return rc;
+    }
+    return BS_OK;
+}
+
+}  // namespace
+
+size_t logprobs_workspace_bytes(int dtype, int64_t T, int64_t V, int top_n) {
+    const Plan p = plan_for(dtype, T, V);
+    return p.slices == 1 ? 0 : stats_bytes(T, p) + (size_t)T * p.slices * top_n * 8;
+}
+
+int launch_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets, int top_n, float* logprob,
+                    float* entropy, float* lse, float* top_values, int32_t* top_ids, void* workspace, size_t workspace_bytes,
+                    hipStream_t st) {
+    const Plan p = plan_for(dtype, T, V);
+    const size_t need = logprobs_workspace_bytes(dtype, T, V, top_n);
+    if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))) return BS_ERR_WORKSPACE;
+    Args g{};
+    g.logits = logits; g.T = T; g.V = V; g.ld = ld; g.targets = targets; g.n = top_n;
+    g.slices = p.slices; g.slice_vectors = p.slice_vectors;
+    g.logprob = logprob; g.entropy = entropy; g.lse = lse; g.top_values = top_values; g.top_ids = top_ids;
+    g.part_stats = static_cast<Stats*>(workspace);
+    g.part_keys = need ? reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + stats_bytes(T, p)) : nullptr;
+    switch (dtype) {
+        case BS_F32: return launch<F32>(g, st);
+        case BS_F16: return launch<F16>(g, st);
+        default: return launch<BF16>(g, st);
+    }
+}
+
+int launch_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets, const float* lse,
+                             const float* entropy, const float* g_logprob, const float* g_entropy, void* grad, int64_t ldg,
+                             hipStream_t st) {
+    BackArgs g{};
+    g.logits = logits; g.grad = grad; g.V = V; g.ld = ld; g.ldg = ldg; g.targets = targets;
+    g.lse = lse; g.entropy = entropy; g.g_logprob = g_logprob; g.g_entropy = g_entropy;
+    switch (dtype) {
+        case BS_F32: return launch_backward<F32>(g, T, st);
+        case BS_F16: return launch_backward<F16>(g, T, st);
+        default: return launch_backward<BF16>(g, T, st);
+    }
+}
+
+}  // namespace bs
