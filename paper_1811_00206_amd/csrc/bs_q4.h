@@ -99,41 +99,85 @@ __device__ __forceinline__ void swap_rows(uint32_t& a, uint32_t& b) {
     asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
 }
 
-// The walk of one wavefront over chunks c, c + step, ... of 16 * R matrix rows against NT tiles of 16 virtual rows.
-// U chunks' loads are issued together.  `a(t, k)`: the lane's 16 bytes of tile t at column k (a multiple of 32) + 8 * kb;
-// columns behind K are zero there.  GL = log2(group / 32).
+// The walk of one wavefront over K, in steps of U adjacent chunks, of 16 * R matrix rows against NT tiles of 16 virtual rows.
+// A row gives 64 bytes to a chunk, half a cache line: adjacent chunks are the same wavefront's, or the other half is fetched
+// again where rows are a power of two apart (16384 x 8192: 20 us instead of 15).  Loads have no branch around them: chunks and
+// blocks behind the end are read as the last ones and count for nothing, because activations behind K are zero and a code is
+// always a number.  Of the scales a lane loads those of one chunk of the step, chunk kb % U, and lane exchanges spread them.
+// GL = log2(group / 32).
 template <bool HALF, int NT, int R, int GL, int U>
 struct Q4Walk {
-    const uint8_t* codes[R];      // the lane's row, at its 16 bytes of chunk 0
-    const uint16_t* scales[R];    // the lane's row
-    int kb, blocks;               // blocks: 32-column blocks of a row; a chunk is four, one for each kb
-    uint4 q[R][U];
-    uint32_t s[R][U];
+    static_assert(U == 2 || U == 4);
+    static constexpr int kHalves = 4 >> GL, kWords = kHalves > 1 ? kHalves / 2 : 1;      // scales of a chunk
+    const uint8_t* codes[R];               // the first of 16 rows (the same for all lanes)
+    const uint16_t* scales[R];
+    uint32_t code_at[R], scale_at[R];      // the lane's row in them
+    int kb, blocks, groups;                // blocks: 32-column blocks of a row; a chunk is four, one for each kb
+    uint4 next_q[R][U], q[R][U];
+    uint32_t next_s[R][kWords], s[R][kWords];
 
-    __device__ __forceinline__ void rows(int r, const uint8_t* c, const uint16_t* sc) { codes[r] = c + 16 * kb; scales[r] = sc; }
+    // tile i: matrix rows row .. row + 15 of a matrix of `rows` (those behind it repeat its last row)
+    __device__ __forceinline__ void tile(int i, const uint8_t* c, const uint16_t* sc, int64_t row, int64_t rows, int64_t K, int lane) {
+        const int64_t pitch = q4_row_bytes(K);
+        row = min(row, rows - 1);
+        const uint32_t r = (uint32_t)min((int64_t)(lane & 15), rows - 1 - row);
+        kb = lane >> 4;
+        blocks = (int)((K + 31) >> 5);
+        groups = (int)((K + (32 << GL) - 1) >> (5 + GL));
+        codes[i] = c + row * pitch;
+        scales[i] = sc + row * groups;
+        code_at[i] = r * (uint32_t)pitch;
+        scale_at[i] = r * (uint32_t)groups;
+    }
 
-    __device__ __forceinline__ void load(int c, int step, int end) {
+    __device__ __forceinline__ void load(int c) {      // chunks c .. c + U - 1
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int cc = c + u * step, block = 4 * cc + kb;
-            const bool in = cc < end && block < blocks;
+            const uint32_t block = (uint32_t)min(4 * (c + u) + kb, blocks - 1);
+#pragma unroll
+            for (int r = 0; r < R; ++r) next_q[r][u] = *reinterpret_cast<const uint4*>(codes[r] + (code_at[r] + 16 * block));
+        }
+        const int first = (c + (kb & (U - 1))) * kHalves;
+        if ((c + U) * kHalves <= groups) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) __builtin_memcpy(next_s[r], scales[r] + (scale_at[r] + (uint32_t)first), 2 * kHalves);
+        } else {
+            uint16_t h[4];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                q[r][u] = in ? *reinterpret_cast<const uint4*>(codes[r] + (int64_t)cc * 64) : uint4{0, 0, 0, 0};
-                // every lane has use for the scale of a chunk that only others' columns reach
-                s[r][u] = cc < end ? scales[r][min(block, blocks - 1) >> GL] : 0;
+#pragma unroll
+                for (int i = 0; i < kHalves; ++i) h[i] = scales[r][scale_at[r] + (uint32_t)min(first + i, groups - 1)];
+                __builtin_memcpy(next_s[r], h, 2 * kHalves);
             }
         }
     }
 
-    template <typename A>
-    __device__ __forceinline__ void eat(int c, int step, int end, A&& a, f32x4 (&acc)[R][NT]) {
+    // Takes what load() has brought.  The copies are real ones (the empty statements), so that the registers a load writes are
+    // free again and the next step can fly while this one is multiplied.
+    __device__ __forceinline__ void take() {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int cc = c + u * step;
-            if (cc >= end) break;
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                q[r][u] = next_q[r][u];
+                asm volatile("" : "+v"(q[r][u].x), "+v"(q[r][u].y), "+v"(q[r][u].z), "+v"(q[r][u].w));
+            }
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                s[r][i] = next_s[r][i];
+                asm volatile("" : "+v"(s[r][i]));
+            }
+        }
+    }
+
+    // chunks c + U0 .. c + U1 - 1 of the step; x(t, c, u, i): the lane's 16 bytes of tile t at column 32 * i + 8 * kb of chunk
+    // c + u.  Chunks from `end` on are left out.
+    template <int U0, int U1, typename X>
+    __device__ __forceinline__ void eat(int c, int end, X&& x, const uint32_t (&sc)[R][kWords][4], f32x4 (&acc)[R][NT]) {
+#pragma unroll
+        for (int u = U0; u < U1; ++u) {
+            if (c + u >= end) break;
             uint32_t w[R][4];
-            float sc[R][4];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 // lane kb holds block kb, words 0..3; step i wants word kb of block i
@@ -142,36 +186,125 @@ struct Q4Walk {
                 swap_halves(w[r][1], w[r][3]);
                 swap_rows(w[r][0], w[r][1]);
                 swap_rows(w[r][2], w[r][3]);
-                // lane kb holds the scale of block kb; step i wants that of block i in every lane
-                uint32_t s0 = __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)s[r][u])), s2 = s0;
-                if constexpr (GL < 2) swap_halves(s0, s2);
-                uint32_t s1 = s0, s3 = s2;
-                if constexpr (GL < 1) { swap_rows(s0, s1); swap_rows(s2, s3); }
-                sc[r][0] = __builtin_bit_cast(float, s0); sc[r][1] = __builtin_bit_cast(float, s1);
-                sc[r][2] = __builtin_bit_cast(float, s2); sc[r][3] = __builtin_bit_cast(float, s3);
             }
             f32x4 d[R][NT];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                uint4 x[NT];
+                uint4 v[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) x[t] = a(t, cc * kQ4Chunk + 32 * i);
+                for (int t = 0; t < NT; ++t) v[t] = x(t, c, u, i);
+                const int g = i >> GL;      // the group in the chunk
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const uint4 v = q4_values<HALF>(w[r][i]);
+                    const uint4 b = q4_values<HALF>(w[r][i]);
+                    const uint32_t word = sc[r][g >> 1][u];
+                    const float scale = (float)__builtin_bit_cast(_Float16, (uint16_t)(g & 1 ? word >> 16 : word));
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         if (i % (1 << GL) == 0) d[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-                        d[r][t] = mfma_16x16x32<HALF>(x[t], v, d[r][t]);
+                        d[r][t] = mfma_16x16x32<HALF>(v[t], b, d[r][t]);
                         if ((i + 1) % (1 << GL) == 0) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[r][t][j] = fmaf(sc[r][i], d[r][t][j], acc[r][t][j]);
+                            for (int j = 0; j < 4; ++j) acc[r][t][j] = fmaf(scale, d[r][t][j], acc[r][t][j]);
                         }
                     }
                 }
             }
         }
     }
+
+    __device__ __forceinline__ void spread(uint32_t (&sc)[R][kWords][4]) {      // the scales of chunk c + u in every lane
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                uint32_t s0 = s[r][i], s2 = s0;
+                if constexpr (U == 4) swap_halves(s0, s2);
+                uint32_t s1 = s0, s3 = s2;
+                swap_rows(s0, s1);
+                if constexpr (U == 4) swap_rows(s2, s3);
+                sc[r][i][0] = s0; sc[r][i][1] = s1; sc[r][i][2] = s2; sc[r][i][3] = s3;
+            }
+    }
+
+    // Steps c, c + stride, ... before `end`, the first of which is loaded already.  x.fetch(c, u) issues the loads of chunk
+    // c + u of x, where it has any; they come before those of the next step, because loads arrive in order: whoever waits for
+    // x does not wait for them.  FETCH: chunks of x that are held at once.
+    template <int FETCH, typename X>
+    __device__ __forceinline__ void rest(int c, int stride, int end, X& x, f32x4 (&acc)[R][NT]) {
+        static_assert(FETCH == U || (FETCH == 1 && U == 2));
+        while (c < end) {
+            const int now = c;
+            take();
+            c += stride * U;
+            uint32_t sc[R][kWords][4];
+#pragma unroll
+            for (int u = 0; u < FETCH; ++u) x.fetch(now, u);
+            if constexpr (FETCH == 1) {
+                spread(sc);
+                eat<0, 1>(now, end, x, sc, acc);
+                x.fetch(now, 1);
+            }
+            if (c < end) load(c);
+            if constexpr (FETCH == 1) {
+                eat<1, 2>(now, end, x, sc, acc);
+            } else {
+                spread(sc);
+                eat<0, U>(now, end, x, sc, acc);
+            }
+        }
+    }
+    template <int FETCH, typename X>
+    __device__ __forceinline__ void walk(int first, int stride, int end, X& x, f32x4 (&acc)[R][NT]) {
+        load(first * U);
+        rest<FETCH>(first * U, stride, end, x, acc);
+    }
+};
+
+// x of a walk, read from memory: virtual rows at[t], 16-byte pieces from column 8 * kb on, zero behind `columns` (a multiple
+// of 8).  Chunks are read as far as there are any, and no further than `chunks`.
+template <int NT, int FETCH>
+struct RowsOfX {
+    const uint16_t* at[NT];
+    int kb, columns, last;      // last: the last chunk
+    uint4 v[NT][FETCH][4];
+    __device__ __forceinline__ void fetch(int c, int u) {
+        const int k = min(c + u, last) * kQ4Chunk;
+        if (k + kQ4Chunk <= columns) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[t][u % FETCH][i] = *reinterpret_cast<const uint4*>(at[t] + k + 32 * i + 8 * kb);
+        } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int p = k + 32 * i + 8 * kb;
+                    const uint4 w = *reinterpret_cast<const uint4*>(at[t] + (p < columns ? p : 0));
+                    v[t][u % FETCH][i] = p < columns ? w : uint4{0, 0, 0, 0};
+                }
+        }
+    }
+    __device__ __forceinline__ uint4 operator()(int t, int, int u, int i) const { return v[t][u % FETCH][i]; }
+};
+
+// x of a walk as the matrix unit takes it: 1 KB, the wavefront's 16-byte pieces side by side, for every tile, chunk and 32
+// columns of it (tile by tile, `chunks` chunks each)
+template <int NT, int FETCH>
+struct TilesOfX {
+    const uint16_t* at;      // the lane's piece of tile 0, chunk 0
+    int64_t tile;            // elements between tiles
+    int last;
+    uint4 v[NT][FETCH][4];
+    __device__ __forceinline__ void fetch(int c, int u) {
+        const int cc = min(c + u, last);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[t][u % FETCH][i] = *reinterpret_cast<const uint4*>(at + t * tile + (cc * 4 + i) * 512);
+    }
+    __device__ __forceinline__ uint4 operator()(int t, int, int u, int i) const { return v[t][u % FETCH][i]; }
 };
 
 // 8 activations from column k on; zero behind K.  `whole`: rows start on 16-byte boundaries.

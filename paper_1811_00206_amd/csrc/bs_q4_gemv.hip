@@ -1,19 +1,21 @@
 // y[n] = W . x[n] for a 4-bit matrix and one or a few vectors (bs.h: bs_q4_gemv).
 //
-// Bound: the codes are read once, M * K / 2 bytes.  A workgroup owns 16 * R rows; its wavefronts share K between them
-// (chunk c of 128 columns goes to wavefront c % ways), so that a few thousand rows already fill the chip, and add their
-// sums in LDS in the order of the wavefronts: the same bits from every call.
+// Bound: the codes are read once, M * K / 2 bytes.  A wavefront owns 16 * R rows; the wavefronts of a workgroup share K
+// (step i of U chunks goes to wavefront i % ways), so that a few thousand rows already fill the chip, and add their sums in
+// LDS in the order of the wavefronts: the same bits from every call.
 //
-// Up to 16 virtual rows (16 vectors in 16 bits, 4 in fp32) the workgroup brings x to LDS itself, in slabs of K, split into
-// its parts there.  With more, a first kernel writes the parts of every vector to the workspace, padded with zeros, and
-// the product reads them from there: what a workgroup needs of x no longer fits LDS, and one split serves all workgroups.
+// x comes to the matrix unit in two ways.  A few virtual rows (4: one fp32 vector, four in 16 bits) a workgroup brings to LDS
+// itself, in slabs of K, split into parts there; `tiles` groups of 16 rows share them.  More are read from memory by every
+// wavefront, 64 bytes of 16 rows at a time, which the caches hold: rows of 16-bit vectors as they are, where they start on
+// 16-byte boundaries and are whole pieces; else from the workspace, where a first kernel puts the parts of every vector,
+// padded with zeros.
 #include "bs_q4.h"
 
 namespace bs {
 namespace {
 
-constexpr int kU = 4;                       // chunks in flight per wavefront
-constexpr size_t kSlabBytes = 48 * 1024;    // of x in LDS
+constexpr size_t kSlabBytes = 64 * 1024;    // of x in LDS
+constexpr int kStagedRows = 4;              // virtual rows that are brought to LDS
 
 struct GemvArgs {
     const uint8_t* codes;
@@ -21,91 +23,121 @@ struct GemvArgs {
     int64_t M, K, N, ldx, ldy;
     const void* x;      // as given, or the parts of every vector in the workspace
     void* y;
-    int ways, slab;     // wavefronts that share K; columns of x in LDS at once
+    int ways, tiles;    // wavefronts that share K; groups of wavefronts that share x in LDS
+    int slab;           // columns of x in LDS at once
     bool whole;         // rows of x start on 16-byte boundaries
 };
 
-template <typename XT, int NT, int R, int GL, bool STAGED>
-__global__ __launch_bounds__(STAGED ? 1024 : 512) void q4_gemv_kernel(GemvArgs g) {
-    using T = typename XT::type;
-    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S;     // tokens per tile of virtual rows
-    extern __shared__ __align__(16) uint8_t lds[];
-    const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t row0 = (int64_t)blockIdx.x * (16 * R);
-    const int64_t n0 = (int64_t)blockIdx.y * (NT * TPT);
-    const int tokens = (int)min(g.N - n0, (int64_t)(NT * TPT));
-    const int chunks = (int)((g.K + kQ4Chunk - 1) / kQ4Chunk);
-
-    Q4Walk<XT::kHalf, NT, R, GL, kU> walk;
-    walk.kb = kb;
-    walk.blocks = (int)((g.K + 31) / 32);
-    const int64_t pitch = q4_row_bytes(g.K), groups = (g.K + (32 << GL) - 1) >> (5 + GL);
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int64_t row = min(row0 + 16 * i + r, g.M - 1);
-        walk.rows(i, g.codes + row * pitch, g.scales + row * groups);
-    }
-    f32x4 acc[R][NT] = {};
-    // the lane's virtual row of tile t, in tokens of this workgroup; rows without a token repeat the last one
-    const int part = min(r % S, P - 1);
-
-    if constexpr (STAGED) {
-        static_assert(NT == 1);
-        uint16_t* xs = reinterpret_cast<uint16_t*>(lds);
-        const int xp = g.slab + 8;                              // row pitch: 16 bytes more, so that rows start on other banks
-        const uint16_t* mine = xs + (min(r / S, tokens - 1) * P + part) * xp + 8 * kb;
-        const int per_slab = g.slab / kQ4Chunk;
-        for (int c0 = 0; c0 < chunks; c0 += per_slab) {
-            const int end = min(chunks, c0 + per_slab);
-            int c = c0 + wave;
-            walk.load(c, g.ways, end);
-            if (c0) __syncthreads();
-            const int64_t k0 = (int64_t)c0 * kQ4Chunk;
-            const int pieces = (end - c0) * (kQ4Chunk / 8);
-            for (int n = 0; n < tokens; ++n) {
-                const T* row = static_cast<const T*>(g.x) + (n0 + n) * g.ldx;
-                for (int j = threadIdx.x; j < pieces; j += blockDim.x) {
-                    uint4 p[P];
-                    pieces8<XT>(row, k0 + 8 * j, g.K, g.whole, p);
-#pragma unroll
-                    for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(xs + (n * P + i) * xp + 8 * j) = p[i];
-                }
-            }
-            __syncthreads();
-            const uint16_t* at = mine - k0;
-            while (c < end) {
-                walk.eat(c, g.ways, end, [&](int, int k) { return *reinterpret_cast<const uint4*>(at + k); }, acc);
-                c += kU * g.ways;
-                if (c < end) walk.load(c, g.ways, end);
-            }
-        }
-        __syncthreads();
-    } else {
-        const int64_t xp = q4_padded(g.K);
-        const uint16_t* at[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-            at[t] = static_cast<const uint16_t*>(g.x) + ((n0 + min(t * TPT + r / S, tokens - 1)) * P + part) * xp + 8 * kb;
-        for (int c = wave; c < chunks; c += kU * g.ways) {
-            walk.load(c, g.ways, chunks);
-            walk.eat(c, g.ways, chunks, [&](int t, int k) { return *reinterpret_cast<const uint4*>(at[t] + k); }, acc);
-        }
-    }
-
-    // a lane's four rows are four tokens, or the parts of one (the small parts are added first)
-    constexpr int V = 4 / S;
-    float* sums = reinterpret_cast<float*>(lds);            // [wave][R][NT][TPT][16]
+// a wavefront's sums to LDS: [wave][R][NT][TPT][16]
+template <int S, int R, int NT>
+__device__ __forceinline__ void put_sums(float* sums, int wave, int lane, const f32x4 (&acc)[R][NT]) {
+    constexpr int TPT = 16 / S, V = 4 / S;
+    const int kb = lane >> 4, r = lane & 15;
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
+                // a lane's four rows are four tokens, or the parts of one (the small parts are added first)
                 float sum = acc[i][t][v];
                 if constexpr (S == 4) sum = acc[i][t][0] + (acc[i][t][1] + acc[i][t][2]);
                 sums[(((wave * R + i) * NT + t) * TPT + kb * V + v) * 16 + r] = sum;
             }
+}
+
+template <typename XT, int GL, int U>
+__global__ __launch_bounds__(1024) void q4_gemv_kernel(GemvArgs g) {
+    using T = typename XT::type;
+    constexpr int P = XT::kParts, S = XT::kSlots;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), way = wave % g.ways, tile = wave / g.ways;
+    const int64_t row0 = (int64_t)blockIdx.x * (16 * g.tiles);
+    const int chunks = (int)((g.K + kQ4Chunk - 1) / kQ4Chunk), tokens = (int)g.N;
+    Q4Walk<XT::kHalf, 1, 1, GL, U> walk;
+    walk.tile(0, g.codes, g.scales, row0 + 16 * tile, g.M, g.K, lane);
+    f32x4 acc[1][1] = {};
+    uint16_t* xs = reinterpret_cast<uint16_t*>(lds);
+    const int xp = g.slab + 8;                              // row pitch: 16 bytes more, so that rows start on other banks
+    // the lane's virtual row; rows without a token repeat the last one
+    const uint16_t* mine = xs + (min(r / S, tokens - 1) * P + min(r % S, P - 1)) * xp + 8 * kb;
+    const int per_slab = g.slab / kQ4Chunk;
+    for (int c0 = 0; c0 < chunks; c0 += per_slab) {
+        const int end = min(chunks, c0 + per_slab), c = c0 + U * way;
+        walk.load(c);
+        if (c0) __syncthreads();
+        const int64_t k0 = (int64_t)c0 * kQ4Chunk;
+        const int pieces = (end - c0) * (kQ4Chunk / 8);
+        for (int n = 0; n < tokens; ++n) {
+            const T* row = static_cast<const T*>(g.x) + n * g.ldx;
+            for (int j = threadIdx.x; j < pieces; j += blockDim.x) {
+                uint4 p[P];
+                pieces8<XT>(row, k0 + 8 * j, g.K, g.whole, p);
+#pragma unroll
+                for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(xs + (n * P + i) * xp + 8 * j) = p[i];
+            }
+        }
+        __syncthreads();
+        struct {
+            const uint16_t* at;
+            __device__ __forceinline__ void fetch(int, int) {}
+            __device__ __forceinline__ uint4 operator()(int, int c, int u, int i) const {
+                return *reinterpret_cast<const uint4*>(at + (c + u) * kQ4Chunk + 32 * i);
+            }
+        } staged{mine - k0};
+        walk.template rest<U>(c, g.ways, end, staged, acc);
+    }
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(lds);
+    put_sums<S>(sums, wave, lane, acc);
+    __syncthreads();
+    constexpr int kOut = 256 / S;      // of a tile
+    for (int o = threadIdx.x; o < kOut * g.tiles; o += blockDim.x) {
+        const int i = o / kOut, n = o % kOut / 16;
+        const int64_t row = row0 + 16 * i + o % 16;
+        if (n >= tokens || row >= g.M) continue;
+        const float* from = sums + i * g.ways * kOut + o % kOut;
+        float sum = from[0];
+        for (int w = 1; w < g.ways; ++w) sum += from[w * kOut];
+        static_cast<T*>(g.y)[n * g.ldy + row] = XT::store(sum);
+    }
+}
+
+template <typename XT, int NT, int R, int GL, bool TILED>
+__global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(GemvArgs g) {
+    using T = typename XT::type;
+    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S, U = 2;     // TPT: tokens per tile of virtual rows
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row0 = (int64_t)blockIdx.x * (16 * R), n0 = (int64_t)blockIdx.y * (NT * TPT);
+    const int tokens = (int)min(g.N - n0, (int64_t)(NT * TPT));
+    const int chunks = (int)((g.K + kQ4Chunk - 1) / kQ4Chunk);
+    Q4Walk<XT::kHalf, NT, R, GL, U> walk;
+#pragma unroll
+    for (int i = 0; i < R; ++i) walk.tile(i, g.codes, g.scales, row0 + 16 * i, g.M, g.K, lane);
+    f32x4 acc[R][NT] = {};
+    constexpr int kFetch = NT <= 2 ? U : 1;
+    if constexpr (TILED) {
+        TilesOfX<NT, kFetch> x;
+        x.tile = (int64_t)chunks * 2048;
+        x.at = static_cast<const uint16_t*>(g.x) + blockIdx.y * NT * x.tile + 8 * lane;
+        x.last = chunks - 1;
+        walk.template walk<kFetch>(wave, g.ways, chunks, x, acc);
+    } else {
+        static_assert(S == 1);
+        RowsOfX<NT, kFetch> x;
+        x.kb = kb;
+        x.columns = (int)g.K;
+        x.last = chunks - 1;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)      // rows without a token repeat the last one
+            x.at[t] = static_cast<const uint16_t*>(g.x) + (n0 + min(t * TPT + r, tokens - 1)) * g.ldx;
+        walk.template walk<kFetch>(wave, g.ways, chunks, x, acc);
+    }
+    float* sums = reinterpret_cast<float*>(lds);
+    put_sums<S>(sums, wave, lane, acc);
     __syncthreads();
     constexpr int kOut = R * NT * TPT * 16;
     for (int o = threadIdx.x; o < kOut; o += blockDim.x) {
@@ -118,79 +150,132 @@ __global__ __launch_bounds__(STAGED ? 1024 : 512) void q4_gemv_kernel(GemvArgs g
     }
 }
 
-// the parts of every vector, padded with zeros to whole chunks
+// x as the matrix unit takes it (TilesOfX): a workgroup writes a chunk of a tile, 4 KB.  Columns behind K are zero, rows
+// without a token stay as they are.
 template <typename XT>
-__global__ __launch_bounds__(256) void q4_split_kernel(const void* x, int64_t K, int64_t ldx, bool whole, uint16_t* parts) {
+__global__ __launch_bounds__(256) void q4_tiles_kernel(const void* x, int64_t K, int64_t N, int64_t ldx, bool whole, uint16_t* tiles) {
     using T = typename XT::type;
-    constexpr int P = XT::kParts;
-    const int64_t n = blockIdx.y, xp = q4_padded(K), k = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (k >= xp) return;
+    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S;
+    const int token = threadIdx.x % TPT, piece = threadIdx.x / TPT;
+    const int64_t n = (int64_t)blockIdx.y * TPT + token, k = (int64_t)blockIdx.x * kQ4Chunk + 8 * piece;
+    if (n >= N) return;
     uint4 p[P];
     pieces8<XT>(static_cast<const T*>(x) + n * ldx, k, K, whole, p);
+    uint16_t* to = tiles + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2048 + 128 * piece + 8 * S * token;
 #pragma unroll
-    for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(parts + (n * P + i) * xp + k) = p[i];
+    for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(to + 8 * i) = p[i];
 }
 
 struct Plan {
-    int nt, r, ways, slab;
     bool staged;
+    bool tiled;
+    int nt, r, u, ways, tiles, slab;
     size_t lds, workspace;
 };
 
 Plan plan_for(int dtype, int64_t M, int64_t K, int64_t N) {
     const int parts = dtype == BS_F32 ? 3 : 1, tpt = dtype == BS_F32 ? 4 : 16;
-    Plan p;
-    p.staged = N <= tpt;
     const int64_t tiles = (M + 15) / 16, chunks = (K + kQ4Chunk - 1) / kQ4Chunk;
-    p.nt = p.staged ? 1 : N <= 2 * tpt ? 2 : 4;
-    p.r = p.staged ? 1 : 2;
-    p.ways = 1;
-    while (p.ways < 16 && p.ways * 2 <= chunks && (p.ways * kU < chunks || tiles * p.ways < 2048)) p.ways *= 2;
-    if (!p.staged && p.ways > 8) p.ways = 8;      // registers of 512 lanes
-    const int rows = p.staged ? (int)N * parts : 0;
-    p.slab = 0;
-    if (rows) {
-        const int64_t most = (int64_t)kSlabBytes / (rows * 2) / kQ4Chunk * kQ4Chunk;
-        p.slab = (int)(chunks * kQ4Chunk <= most ? chunks * kQ4Chunk : most);
+    Plan p{};
+    p.staged = N * parts <= kStagedRows;
+    if (p.staged) {
+        // Wavefronts that share K: as many as give the chip 2048 (eight for a compute unit), or what K has steps for.  Where
+        // two are enough, four groups share x.  16384 x 8192: 14.9 us with 2 x 4, 16.6 with 2 x 1, 15.4 with 4 x 1, 17.2 with
+        // 8 x 1; 10000 x 1500: 6.1 / 6.1 / 5.6 / 6.0; 4096 x 25088: 37 / 40 / 22 / 15.
+        const int64_t steps = (chunks + 1) / 2;
+        p.ways = 1;
+        while (p.ways < 16 && tiles * p.ways < 2048 && p.ways < steps) p.ways *= 2;
+        p.tiles = p.ways <= 2 ? 4 : 1;
+        // four chunks a step where every wavefront has many: 16384 x 8192 14.1 us against 14.9
+        p.u = chunks >= 16 * p.ways ? 4 : 2;
+        const int rows = (int)N * parts;
+        const int64_t whole = p.u * kQ4Chunk, most = (int64_t)kSlabBytes / (rows * 2) / whole * whole, all = (K + whole - 1) / whole * whole;
+        p.slab = (int)(all < most ? all : most);
+        const size_t xs = (size_t)rows * (p.slab + 8) * 2, sums = (size_t)p.ways * p.tiles * tpt * 16 * 4;
+        p.lds = xs > sums ? xs : sums;
+        return p;
     }
-    const size_t xs = (size_t)rows * (p.slab + 8) * 2, sums = (size_t)p.ways * p.r * p.nt * tpt * 16 * 4;
-    p.lds = xs > sums ? xs : sums;
-    p.workspace = p.staged ? 0 : (size_t)N * parts * q4_padded(K) * 2;
+    // A wavefront loads as much of x as R rows' worth of codes, so R is as large as leaves a workgroup for every compute unit:
+    // 16384 x 8192 for 16 vectors 24.1 / 19.9 / 19.0 us with R = 1 / 2 / 4, 4096 x 25088 17.3 / 23.0 / 38.
+    p.nt = N <= tpt ? 1 : N <= 2 * tpt ? 2 : 4;
+    p.r = p.nt == 4 || tiles < 320 ? 1 : tiles < 1024 ? 2 : 4;
+    const int most = p.r == 4 ? 4 : 8;
+    const int64_t steps = (chunks + 1) / 2;
+    p.ways = (int)(steps < most ? steps : most);
+    // 16-bit vectors as they are, unless rows a power of two apart and half lines cost more than a kernel that lays them out
+    // (about 3 us): 16384 x 8192 for 32 vectors 32 us as they are, 23 + 3 as tiles; 6000 x 3000 for 16 vectors 5.5 and 5.6 + 2.
+    p.tiled = dtype == BS_F32 || p.nt == 4 || M * K >= ((int64_t)1 << 26);
+    p.lds = (size_t)p.ways * p.r * p.nt * tpt * 16 * 4;
+    p.workspace = (size_t)((N + tpt - 1) / tpt) * 32 * q4_padded(K);
     return p;
 }
 
-template <typename XT, int NT, int R, int GL, bool STAGED>
-int launch(const GemvArgs& g, const Plan& p, hipStream_t st) {
-    using Reg = LdsKernelOf<q4_gemv_kernel<XT, NT, R, GL, STAGED>>;
+template <typename XT, int GL, int U>
+int launch_staged(const GemvArgs& g, const Plan& p, hipStream_t st) {
+    using Reg = LdsKernelOf<q4_gemv_kernel<XT, GL, U>>;
+    if (p.lds > kLdsWithoutLimit) {
+        const int rc = ensure_lds_limit(Reg::reg, st);
+        if (rc != BS_OK) return rc;
+    }
+    const dim3 grid((unsigned)((g.M + 16 * p.tiles - 1) / (16 * p.tiles)));
+    hipLaunchKernelGGL((q4_gemv_kernel<XT, GL, U>), grid, dim3(64 * p.ways * p.tiles), p.lds, st, g);
+    return hip_status(hipGetLastError());
+}
+
+template <typename XT, int NT, int R, int GL, bool TILED>
+int launch_many(const GemvArgs& g, const Plan& p, hipStream_t st) {
+    using Reg = LdsKernelOf<q4_gemv_many_kernel<XT, NT, R, GL, TILED>>;
     if (p.lds > kLdsWithoutLimit) {
         const int rc = ensure_lds_limit(Reg::reg, st);
         if (rc != BS_OK) return rc;
     }
     const int per = NT * (16 / XT::kSlots);
     const dim3 grid((unsigned)((g.M + 16 * R - 1) / (16 * R)), (unsigned)((g.N + per - 1) / per));
-    hipLaunchKernelGGL((q4_gemv_kernel<XT, NT, R, GL, STAGED>), grid, dim3(64 * p.ways), p.lds, st, g);
+    hipLaunchKernelGGL((q4_gemv_many_kernel<XT, NT, R, GL, TILED>), grid, dim3(64 * p.ways), p.lds, st, g);
     return hip_status(hipGetLastError());
 }
 
+template <typename XT, int NT, int GL>
+int launch_rows(const GemvArgs& g, const Plan& p, bool tiled, hipStream_t st) {
+    if constexpr (XT::kParts == 1 && NT <= 2) {
+        if (!tiled)
+            return p.r == 1 ? launch_many<XT, NT, 1, GL, false>(g, p, st) : p.r == 2 ? launch_many<XT, NT, 2, GL, false>(g, p, st)
+                                                                                     : launch_many<XT, NT, 4, GL, false>(g, p, st);
+    }
+    if constexpr (NT <= 2) {
+        if (p.r == 2) return launch_many<XT, NT, 2, GL, true>(g, p, st);
+        if (p.r == 4) return launch_many<XT, NT, 4, GL, true>(g, p, st);
+    }
+    return launch_many<XT, NT, 1, GL, true>(g, p, st);
+}
+
 template <typename XT, int GL>
-int launch_tiles(const GemvArgs& g, const Plan& p, hipStream_t st) {
-    if (p.staged) return launch<XT, 1, 1, GL, true>(g, p, st);
-    return p.nt == 2 ? launch<XT, 2, 2, GL, false>(g, p, st) : launch<XT, 4, 2, GL, false>(g, p, st);
+int launch_group(const GemvArgs& g, const Plan& p, bool tiled, hipStream_t st) {
+    if (p.staged) return p.u == 2 ? launch_staged<XT, GL, 2>(g, p, st) : launch_staged<XT, GL, 4>(g, p, st);
+    return p.nt == 1   ? launch_rows<XT, 1, GL>(g, p, tiled, st)
+           : p.nt == 2 ? launch_rows<XT, 2, GL>(g, p, tiled, st)
+                       : launch_rows<XT, 4, GL>(g, p, tiled, st);
 }
 
 template <typename XT>
 int launch_type(GemvArgs g, const Plan& p, int group, void* workspace, hipStream_t st) {
+    bool tiled = false;
     if (!p.staged) {
-        const dim3 grid((unsigned)((q4_padded(g.K) + 2047) / 2048), (unsigned)g.N);
-        hipLaunchKernelGGL(q4_split_kernel<XT>, grid, dim3(256), 0, st, g.x, g.K, g.ldx, g.whole, static_cast<uint16_t*>(workspace));
-        const int rc = hip_status(hipGetLastError());
-        if (rc != BS_OK) return rc;
-        g.x = workspace;
+        tiled = p.tiled || !g.whole || g.K % 8;
+        if (tiled) {
+            constexpr int TPT = 16 / XT::kSlots;
+            const dim3 grid((unsigned)(q4_padded(g.K) / kQ4Chunk), (unsigned)((g.N + TPT - 1) / TPT));
+            hipLaunchKernelGGL(q4_tiles_kernel<XT>, grid, dim3(16 * TPT), 0, st, g.x, g.K, g.N, g.ldx, g.whole,
+                               static_cast<uint16_t*>(workspace));
+            const int rc = hip_status(hipGetLastError());
+            if (rc != BS_OK) return rc;
+            g.x = workspace;
+        }
     }
     switch (q4_group_shift(group)) {
-        case 0: return launch_tiles<XT, 0>(g, p, st);
-        case 1: return launch_tiles<XT, 1>(g, p, st);
-        default: return launch_tiles<XT, 2>(g, p, st);
+        case 0: return launch_group<XT, 0>(g, p, tiled, st);
+        case 1: return launch_group<XT, 1>(g, p, tiled, st);
+        default: return launch_group<XT, 2>(g, p, tiled, st);
     }
 }
 
@@ -203,8 +288,8 @@ int launch_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int6
     const Plan p = plan_for(dtype, M, K, N);
     if (p.workspace && (!workspace || workspace_bytes < p.workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)))
         return BS_ERR_WORKSPACE;
-    GemvArgs g{codes, scales, M, K, N, ldx, ldy, x, y, p.ways, p.slab, false};
-    g.whole = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (N == 1 || ldx * dtype_bytes(dtype) % 16 == 0);
+    const bool whole = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (N == 1 || ldx * dtype_bytes(dtype) % 16 == 0);
+    const GemvArgs g{codes, scales, M, K, N, ldx, ldy, x, y, p.ways, p.tiles, p.slab, whole};
     switch (dtype) {
         case BS_F32: return launch_type<F32>(g, p, group, workspace, st);
         case BS_F16: return launch_type<F16>(g, p, group, workspace, st);

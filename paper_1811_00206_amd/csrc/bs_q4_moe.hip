@@ -16,9 +16,13 @@
 namespace bs {
 namespace {
 
-constexpr int kU = 4;
+constexpr int kU = 2;
 constexpr int kDownWaves = 16;
 constexpr int kMaxTokens = BS_MOE_TOKENS_MAX, kMaxExperts = BS_MOE_EXPERTS_MAX, kMaxTopK = BS_MOE_TOP_K_MAX;
+
+// Elements between virtual rows in the workspace: whole chunks and a cache line, so that rows a power of two long do not
+// meet in the same sets of the caches.
+__host__ __device__ constexpr int64_t row_pitch(int64_t columns) { return q4_padded(columns) + 64; }
 
 template <typename XT>
 struct Hidden {      // virtual rows of h
@@ -46,7 +50,7 @@ __global__ __launch_bounds__(1024) void moe_route_kernel(MoeArgs g) {
     __shared__ float logits[kMaxExperts];
     const int t = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const T* x = static_cast<const T*>(g.x) + t * g.ldx;
-    const int64_t dp = q4_padded(g.D);
+    const int64_t columns = q4_padded(g.D), dp = row_pitch(g.D);
     for (int e = wave * EB; e < g.E; e += waves * EB) {
         float sum[EB] = {};
         for (int k = 8 * lane; k < g.D; k += 512) {
@@ -66,7 +70,7 @@ __global__ __launch_bounds__(1024) void moe_route_kernel(MoeArgs g) {
             if (lane == 0 && e + i < g.E) logits[e + i] = s;
         }
     }
-    for (int64_t k = 8 * threadIdx.x; k < dp; k += 8 * blockDim.x) {
+    for (int64_t k = 8 * threadIdx.x; k < columns; k += 8 * blockDim.x) {
         uint4 p[P];
         pieces8<XT>(x, k, g.D, g.whole_x, p);
 #pragma unroll
@@ -135,32 +139,30 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
     }
     __syncthreads();
     const int tokens = found;
-    const int64_t fp = q4_padded(g.F), dp = q4_padded(g.D);
-    const int chunks = (int)(dp / kQ4Chunk);
+    const int64_t fp = row_pitch(g.F), dp = row_pitch(g.D);
+    const int chunks = (int)(q4_padded(g.D) / kQ4Chunk);
     const int64_t pitch = q4_row_bytes(g.D), groups = (g.D + (32 << GL) - 1) >> (5 + GL);
     constexpr int V = 4 / S, kOut = NT * TPT * 16;
     for (int n0 = 0; n0 < tokens; n0 += NT * TPT) {
         const int here = min(tokens - n0, NT * TPT);
         if (f0 < g.F) {
             Q4Walk<XT::kHalf, NT, 2, GL, kU> walk;
-            walk.kb = kb;
-            walk.blocks = (g.D + 31) / 32;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int64_t row = (int64_t)e * 2 * g.F + i * (int64_t)g.F + min(f0 + r, g.F - 1);
-                walk.rows(i, g.w1 + row * pitch, g.s1 + row * groups);
+                const int64_t first = ((int64_t)e * 2 + i) * g.F;      // of the expert's gate or up rows
+                walk.tile(i, g.w1 + first * pitch, g.s1 + first * groups, f0, g.F, g.D, lane);
             }
-            const uint16_t* at[NT];
+            RowsOfX<NT, kU> x;
+            x.kb = kb;
+            x.columns = chunks * kQ4Chunk;
+            x.last = chunks - 1;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int token = list[n0 + min(t * TPT + r / S, here - 1)] / g.top_k;
-                at[t] = g.xp + ((int64_t)token * P + min(r % S, P - 1)) * dp + 8 * kb;
+                x.at[t] = g.xp + ((int64_t)token * P + min(r % S, P - 1)) * dp;
             }
             f32x4 acc[2][NT] = {};
-            for (int c = wave; c < chunks; c += kU * g.ways) {
-                walk.load(c, g.ways, chunks);
-                walk.eat(c, g.ways, chunks, [&](int t, int k) { return *reinterpret_cast<const uint4*>(at[t] + k); }, acc);
-            }
+            walk.template walk<kU>(wave, g.ways, chunks, x, acc);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -226,10 +228,10 @@ __global__ __launch_bounds__(1024) void moe_down_kernel(MoeArgs g) {
     }
     __syncthreads();
     const int experts = __builtin_amdgcn_readfirstlane(*found);
-    const int64_t fp = q4_padded(g.F);
-    const int chunks = (int)(fp / kQ4Chunk);
+    const int64_t fp = row_pitch(g.F);
+    const int chunks = (int)(q4_padded(g.F) / kQ4Chunk);
     const int64_t pitch = q4_row_bytes(g.F), groups = (g.F + (32 << GL) - 1) >> (5 + GL);
-    const int ways = experts >= kDownWaves ? 1 : min(kDownWaves / experts, chunks);
+    const int ways = experts >= kDownWaves ? 1 : min(kDownWaves / experts, (chunks + kU - 1) / kU);
     float* mine = sums + wave * g.T * 16;
     int32_t* list = lists + wave * g.T;
     for (int item = wave; item < experts * ways; item += kDownWaves) {
@@ -238,18 +240,16 @@ __global__ __launch_bounds__(1024) void moe_down_kernel(MoeArgs g) {
         const int tokens = pairs_of(ids, g.pairs, first, e, list);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the list is written by some lanes and read by others
         Q4Walk<false, 1, 1, GL, kU> walk;
-        walk.kb = kb;
-        walk.blocks = (g.F + 31) / 32;
-        const int64_t row = (int64_t)e * g.D + min(d0 + r, g.D - 1);
-        walk.rows(0, g.w2 + row * pitch, g.s2 + row * groups);
+        walk.tile(0, g.w2 + (int64_t)e * g.D * pitch, g.s2 + (int64_t)e * g.D * groups, d0, g.D, g.F, lane);
         for (int n0 = 0; n0 < tokens; n0 += TPT) {
             const int here = min(tokens - n0, TPT);
-            const uint16_t* at = g.hp + ((int64_t)list[n0 + min(r / S, here - 1)] * P + min(r % S, P - 1)) * fp + 8 * kb;
+            RowsOfX<1, kU> x;
+            x.kb = kb;
+            x.columns = chunks * kQ4Chunk;
+            x.last = chunks - 1;
+            x.at[0] = g.hp + ((int64_t)list[n0 + min(r / S, here - 1)] * P + min(r % S, P - 1)) * fp;
             f32x4 acc[1][1] = {};
-            for (int c = c0; c < chunks; c += kU * ways) {
-                walk.load(c, ways, chunks);
-                walk.eat(c, ways, chunks, [&](int, int k) { return *reinterpret_cast<const uint4*>(at + k); }, acc);
-            }
+            walk.template walk<kU>(c0, ways, chunks, x, acc);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int n = kb * V + v;
@@ -308,12 +308,12 @@ int launch_group(const MoeArgs& g, int group, hipStream_t st) {
     }
 }
 
-size_t x_bytes(int dtype, int64_t T, int64_t D) { return (size_t)T * (dtype == BS_F32 ? 3 : 1) * q4_padded(D) * 2; }
+size_t x_bytes(int dtype, int64_t T, int64_t D) { return (size_t)T * (dtype == BS_F32 ? 3 : 1) * row_pitch(D) * 2; }
 
 }  // namespace
 
 size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int top_k) {
-    return x_bytes(dtype, T, D) + (size_t)T * top_k * (dtype == BS_F32 ? 3 : 2) * q4_padded(F) * 2;
+    return x_bytes(dtype, T, D) + (size_t)T * top_k * (dtype == BS_F32 ? 3 : 2) * row_pitch(F) * 2;
 }
 
 int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,
@@ -331,9 +331,8 @@ int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, c
     g.w1 = w1; g.w2 = w2; g.s1 = s1; g.s2 = s2; g.y = y; g.ids = ids; g.weights = weights;
     g.xp = static_cast<uint16_t*>(workspace);
     g.hp = g.xp + x_bytes(dtype, T, D) / 2;
-    const int64_t chunks = q4_padded(D) / kQ4Chunk;
-    g.ways = 1;
-    while (g.ways < 8 && g.ways * 2 <= chunks) g.ways *= 2;
+    const int64_t steps = (q4_padded(D) / kQ4Chunk + kU - 1) / kU;
+    g.ways = (int)(steps < 8 ? steps : 8);
     switch (dtype) {
         case BS_F32: return launch_group<F32>(g, group, st);
         case BS_F16: return launch_group<F16>(g, group, st);
