@@ -1,19 +1,21 @@
 // Log probabilities of given tokens, entropy and most likely alternatives of rows of logits, and their gradient
 // (bs.h: bs_logprobs, bs_logprobs_backward).  Bound: HBM, the logits once (the gradient: once in, once out).
 //
-// Softmax statistics in one pass: a thread keeps the largest logit m it has seen and, with u = (x - m) log2(e),
-//     s = sum 2^u,   t = sum u 2^u,   so that  lse = m + log s  and  entropy = ln2 (log2 s - t / s).
-// A batch of 32 elements moves m once.  u is cut off at -200, where 2^u is 0: a banned word, x = -inf, adds nothing to
-// either sum (and no 0 * inf), and what is no number stays so.  x - m comes first because it is exact where it matters: rows
-// whose logits are all a type's lowest value are uniform, and come out so.
+// Softmax statistics in one pass: a thread keeps the largest logit m it has seen and, with L = log2(e) and u = x L - c,
+// c = m L rounded,
+//     s = sum 2^u,   t = sum u 2^u,   so that  lse = ln2 (c + log2 s)  and  entropy = ln2 (log2 s - t / s):
+// c's rounding is no error, since c itself goes into the result.  A batch of 32 elements moves m once.  u is cut off at
+// -200, where 2^u is 0: a banned word, x = -inf, adds nothing to either sum (and no 0 * inf), and what is no number stays
+// so.  Where m L could overflow (masks of the lowest fp32 or bfloat16 value that leave nothing) u = (x - m) L and
+// lse = m + log s: such rows are uniform, and come out so.
 //
-// The n largest: a lower bound of the n-th largest comes out of the first batch of a slice (32 elements a thread): each of
-// the four wavefronts finds the ceil(n / 4)-th largest of its lanes' maxima, and at least n elements reach the least of
-// those.  Whatever reaches it is put into a list in LDS, a few times n elements of a row; a thread whose batch has no such
-// element, nearly every one, does one comparison for it.  In the end the list is ordered by counting, for every entry,
-// the entries before it.  Entries are 64-bit keys (value, then index), all different, so the order in which threads reach
-// the list does not matter.  Rows that flood the list (masks that leave fewer than n words, equal logits, rising ones) are
-// gone over once more with the strict bound, or n times, which is slow and right.
+// The n largest: each of the four wavefronts finds the ceil(n / 4)-th largest of its lanes' largest, and at least n elements
+// reach the least of those, the bound; few others do.  While the statistics are made a thread only keeps, in LDS, the
+// largest of every eight elements; the eights that reach the bound are listed and loaded once more, each by a thread of its
+// own, and their elements that reach it are ordered by counting, for every one, those before it.  They are 64-bit keys
+// (value, then index), all different, so the order in which threads reach a list does not matter.  Rows that flood the lists
+// (masks that leave fewer than n words, equal logits) are gone over once more with the strict bound, or n times, which is
+// slow and right.
 #include "bs_q4.h"
 
 namespace bs {
@@ -21,8 +23,11 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kBatch = 32;                     // elements of a thread
-constexpr int kList = 1024;                    // keys in LDS
-constexpr int kTidy = 256;                     // a longer list is cut to its n largest before the next batch
+constexpr int kSlices = 16;                    // of a row, at most
+constexpr int kList = 256;                     // keys in LDS
+constexpr int kEights = 256;                   // listed eights
+constexpr int kPlaces = 8;                     // in LDS for a thread's batches' largest; more batches share them
+constexpr int kParts = kBatch / 8;
 constexpr int kTopMax = BS_LOGPROBS_TOP_MAX;
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -33,22 +38,45 @@ struct Stats {
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // u, at least `least`; NaN where u is
 __device__ __forceinline__ float at_least(float u, float least) { return __builtin_elementwise_maximum(u, least); }
+// m so large that m * log2(e) is none (or no number): differences are taken first then
+__device__ __forceinline__ bool extreme(float m) { return !(fabsf(m) <= 1e37f); }
 
-__device__ __forceinline__ void raise(Stats& a, float m) {       // to a larger m
-    const float d = at_least((a.m - m) * kLog2e, -200.f), f = exp2_hw(d);
+// the power of two by which sums made with `from` are multiplied to go with `to` >= from, as an exponent
+__device__ __forceinline__ float exponent(float from, float to) {
+    const float d = extreme(from) || extreme(to) ? (from - to) * kLog2e : from * kLog2e - to * kLog2e;
+    return from == to ? 0.f : at_least(d, -200.f);
+}
+__device__ __forceinline__ void raise(Stats& a, float m) {
+    const float d = exponent(a.m, m), f = exp2_hw(d);
     a.t = fmaf(a.s, d, a.t) * f;
     a.s *= f;
     a.m = m;
 }
+
+// the largest of a wavefront's values, in every lane; what is no number counts only where nothing else does
+__device__ __forceinline__ float max_of_wave(float v) {
+    v = fmaxf(v, dpp_move<0xB1>(v));
+    v = fmaxf(v, dpp_move<0x4E>(v));
+    v = fmaxf(v, dpp_move<0x141>(v));
+    v = fmaxf(v, dpp_move<0x140>(v));
+    uint32_t a = __builtin_bit_cast(uint32_t, v), b = a;
+    swap_rows(a, b);
+    v = fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+    a = b = __builtin_bit_cast(uint32_t, v);
+    swap_halves(a, b);
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float sum_of_wave(float v) { return add_across_32(add_across_16(group_sum<16>(v))); }
+
 __device__ __forceinline__ Stats join(Stats a, Stats b) {
     const float m = fmaxf(a.m, b.m);
-    if (a.m != m) raise(a, m);
-    if (b.m != m) raise(b, m);
+    raise(a, m);
+    raise(b, m);
     return {m, a.s + b.s, a.t + b.t};
 }
-__device__ __forceinline__ Stats wave_join(Stats a) {
-    for (int o = 1; o < 64; o *= 2) a = join(a, Stats{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)});
-    return a;
+__device__ __forceinline__ Stats join_wave(Stats a) {
+    raise(a, max_of_wave(a.m));
+    return {a.m, sum_of_wave(a.s), sum_of_wave(a.t)};
 }
 
 struct Args {
@@ -57,6 +85,7 @@ struct Args {
     const int64_t* targets;
     int n, slices;
     int64_t slice_vectors;      // 16-byte pieces of a row in a slice
+    int sharing;                // batches of a place
     float *logprob, *entropy, *lse, *top_values;
     int32_t* top_ids;
     Stats* part_stats;          // [rows][slices]
@@ -92,22 +121,43 @@ struct Row {
     }
 };
 
-struct TopList {
-    uint64_t keys[kList];
+template <int LIST>
+struct KeyList {
+    alignas(16) uint64_t keys[LIST + 8];
     uint64_t sorted[kTopMax];
+    int count;
+};
+struct TopList : KeyList<kList> {
+    uint32_t eights[kEights];      // first piece of the eight elements
     float bound[kWaves];
-    int count, wave_count[kWaves];
+    int eight_count, wave_count[kWaves];
     uint64_t wave_best[kWaves];
 };
 
+// how many of the first `count` keys, a multiple of eight, are larger
+__device__ __forceinline__ int keys_before(const uint64_t* keys, int count, uint64_t key) {
+    int before = 0;
+    for (int j = 0; j < count; j += 8) {
+        uint64_t k[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] = keys[j + i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) before += k[i] > key;
+    }
+    return before;
+}
+
 // the n largest keys of the list, in order; entries behind the list's end become 0.  All threads, barriers inside.
-__device__ __forceinline__ void order_list(TopList& l, int count, int n) {
+template <int LIST>
+__device__ __forceinline__ void order_list(KeyList<LIST>& l, int count, int n) {
     for (int i = threadIdx.x; i < n; i += kThreads)
         if (i >= count) l.sorted[i] = 0;
+    const int padded = (count + 7) & ~7;       // the walk below takes eight at a time
+    if (threadIdx.x < 8 && count + (int)threadIdx.x < padded) l.keys[count + threadIdx.x] = 0;
+    __syncthreads();
     for (int i = threadIdx.x; i < count; i += kThreads) {
         const uint64_t key = l.keys[i];
-        int before = 0;
-        for (int j = 0; j < count; ++j) before += l.keys[j] > key;
+        const int before = keys_before(l.keys, padded, key);
         if (before < n) l.sorted[before] = key;
     }
     __syncthreads();
@@ -117,8 +167,7 @@ __device__ __forceinline__ void order_list(TopList& l, int count, int n) {
 __device__ __forceinline__ float kth_largest(float v, int k) {
     float most = v;
     for (int j = 0; j < k; ++j) {
-        most = v;
-        for (int o = 1; o < 64; o *= 2) most = fmaxf(most, __shfl_xor(most, o));
+        most = max_of_wave(v);
         const uint64_t m = __ballot(v == most);
         if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)m) - 1) v = -__builtin_inff();
     }
@@ -212,24 +261,29 @@ __device__ void fill(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, flo
     __syncthreads();
 }
 
-// what a log probability is made of: (x - m) - log s
+// what a log probability is made of
 struct Norm {
-    float m, log_s;
+    float m;
+    double log2_s;
 };
 
 __device__ __forceinline__ float logprob_of(float x, Norm z) {
-    if (z.log_s != z.log_s) return z.log_s;
-    return x == -__builtin_inff() ? x : (x - z.m) - z.log_s;      // a row without words: all are impossible
+    if (z.log2_s != z.log2_s) return __builtin_nanf("");
+    if (x == -__builtin_inff()) return x;      // a row without words: all are impossible
+    const double d = extreme(z.m) ? ((double)x - (double)z.m) * (double)kLog2e : fma((double)x, (double)kLog2e, -(double)(z.m * kLog2e));
+    return (float)((d - z.log2_s) * 0.69314718055994530942);
 }
 
 // a row's results, by one lane
 template <typename XT>
 __device__ __forceinline__ Norm finish(const Args& g, int64_t row, Stats st) {
-    const double log_s = log((double)st.s);
-    const Norm z{st.m, (float)log_s};
+    constexpr double kLn2 = 0.69314718055994530942;
+    const double log2_s = log2((double)st.s);
+    const Norm z{st.m, log2_s};
     const bool words = st.s != 0.f;
-    g.lse[row] = words ? (float)((double)st.m + log_s) : -__builtin_inff();
-    g.entropy[row] = words ? (float)(log_s - (double)st.t / (double)st.s * 0.69314718055994530942) : 0.f;
+    const double lse = extreme(st.m) ? (double)st.m + log2_s * kLn2 : ((double)(st.m * kLog2e) + log2_s) * kLn2;
+    g.lse[row] = words ? (float)lse : -__builtin_inff();
+    g.entropy[row] = words ? (float)((log2_s - (double)st.t / (double)st.s) * kLn2) : 0.f;
     const int64_t target = g.targets[row];
     float p = 0.f;
     if (target >= g.V) p = __builtin_nanf("");
@@ -247,7 +301,8 @@ __device__ __forceinline__ void write_top(const Args& g, int64_t row, const uint
 
 template <typename XT, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(Args g) {
-    constexpr int E = Row<XT>::E, U = kBatch / E;
+    constexpr int E = Row<XT>::E, U = kBatch / E, V8 = 8 / E;      // pieces of a thread, and of eight elements
+    extern __shared__ __align__(16) f32x4 largest[];               // [place][thread]: of the batches' four eights
     __shared__ TopList l;
     __shared__ Stats stats[kWaves];
     __shared__ Norm norm;
@@ -255,11 +310,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Args g) {
     const Row<XT> row(g.logits, row_no, g.ld, g.V);
     const int64_t v0 = slice * g.slice_vectors, v1 = min(row.vectors(), v0 + g.slice_vectors);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (TOP && threadIdx.x == 0) l.count = 0;
+    if (TOP && threadIdx.x == 0) l.count = l.eight_count = 0;
     Stats st{-__builtin_inff(), 0.f, 0.f};
-    float bound = 0.f;
-    bool flood = false;
-    for (int64_t b = v0; b < v1; b += kThreads * U) {
+    int batches = 0;
+    for (int64_t b = v0; b < v1; b += kThreads * U, ++batches) {
         float x[kBatch];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -269,102 +323,131 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Args g) {
 #pragma unroll
                 for (int i = 0; i < E; ++i) x[u * E + i] = -__builtin_inff();
         }
-        float most = x[0];
+        float part[kParts], most = -__builtin_inff();
 #pragma unroll
-        for (int i = 1; i < kBatch; ++i) most = fmaxf(most, x[i]);
+        for (int i = 0; i < kParts; ++i) {
+            part[i] = x[8 * i];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) part[i] = fmaxf(part[i], x[8 * i + j]);
+            most = fmaxf(most, part[i]);
+        }
+        if constexpr (TOP) {
+            f32x4& place = largest[batches / g.sharing * kThreads + threadIdx.x];
+            if (batches % g.sharing) {
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) part[i] = fmaxf(part[i], place[i]);
+            }
+            place = f32x4{part[0], part[1], part[2], part[3]};
+        }
         if (most > st.m) raise(st, most);
-        const float m = st.m == -__builtin_inff() ? 0.f : st.m;
         float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+        const bool none = st.m == -__builtin_inff();      // so far
+        if (none || !extreme(st.m)) {
+            const float c = none ? 0.f : st.m * kLog2e;
 #pragma unroll
-        for (int i = 0; i < kBatch; i += 2) {
-            const float u0 = at_least((x[i] - m) * kLog2e, -200.f), u1 = at_least((x[i + 1] - m) * kLog2e, -200.f);
-            const float p0 = exp2_hw(u0), p1 = exp2_hw(u1);
-            s0 += p0; s1 += p1;
-            t0 = fmaf(p0, u0, t0); t1 = fmaf(p1, u1, t1);
+            for (int i = 0; i < kBatch; i += 2) {
+                const float u0 = at_least(fmaf(x[i], kLog2e, -c), -200.f), u1 = at_least(fmaf(x[i + 1], kLog2e, -c), -200.f);
+                const float p0 = exp2_hw(u0), p1 = exp2_hw(u1);
+                s0 += p0; s1 += p1;
+                t0 = fmaf(p0, u0, t0); t1 = fmaf(p1, u1, t1);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < kBatch; ++i) {
+                float v = x[0];
+#pragma unroll
+                for (int j = 1; j < kBatch; ++j) v = i == j ? x[j] : v;
+                const float u0 = at_least((v - st.m) * kLog2e, -200.f), p0 = exp2_hw(u0);
+                s0 += p0;
+                t0 = fmaf(p0, u0, t0);
+            }
         }
         st.s += s0 + s1;
         st.t += t0 + t1;
-        if constexpr (TOP) {
-            if (b == v0) {
-                const float k = kth_largest(fmaxf(most, -__builtin_inff()), (g.n + kWaves - 1) / kWaves);
-                if (lane == 0) l.bound[wave] = k;
-                __syncthreads();
-                bound = l.bound[0];
-                for (int w = 1; w < kWaves; ++w) bound = fminf(bound, l.bound[w]);
-            } else {
-                __syncthreads();
-                const int count = l.count;
-                __syncthreads();
-                if (count > kList) flood = true;      // and nothing is put into the list any more
-                else if (count > kTidy) {
-                    order_list(l, count, g.n);
-                    if (threadIdx.x < g.n) l.keys[threadIdx.x] = l.sorted[threadIdx.x];
-                    if (threadIdx.x == 0) l.count = g.n;
-                    bound = fmaxf(bound, value_of_key(l.sorted[g.n - 1]));
-                    __syncthreads();
-                }
-            }
-            if (!flood && most >= bound && most > -__builtin_inff()) {
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i)
-                    if (x[i] >= bound && x[i] > -__builtin_inff()) {
-                        const int at = atomicAdd(&l.count, 1);
-                        const int64_t v = b + i / E * kThreads + threadIdx.x;
-                        if (at < kList) l.keys[at] = order_key(x[i], (uint32_t)(v * E - row.head + i % E));
-                    }
-            }
-        }
     }
-    st = wave_join(st);
+    float bound = 0.f;
+    if constexpr (TOP) {
+        const float k = kth_largest(st.m, (g.n + kWaves - 1) / kWaves);
+        if (lane == 0) l.bound[wave] = k;
+    }
+    st = join_wave(st);
     if (lane == 0) stats[wave] = st;
     __syncthreads();
     if constexpr (TOP) {
+        bound = l.bound[0];
+        for (int w = 1; w < kWaves; ++w) bound = fminf(bound, l.bound[w]);
+        for (int b = 0; b * g.sharing < batches; ++b) {
+            const f32x4 part = largest[b * kThreads + threadIdx.x];
+#pragma unroll
+            for (int i = 0; i < kParts; ++i)
+                if (part[i] >= bound && part[i] > -__builtin_inff()) {
+                    const int at = atomicAdd(&l.eight_count, 1);
+                    if (at < kEights) l.eights[at] = (uint32_t)(b * kParts + i) * kThreads + threadIdx.x;
+                }
+        }
+        __syncthreads();
+        const int eights = l.eight_count;
+        const int64_t pieces = (int64_t)min(eights, kEights) * V8 * g.sharing;
+        for (int64_t j = threadIdx.x; j < pieces; j += kThreads) {
+            const uint32_t eight = l.eights[j / (V8 * g.sharing)], place = eight / kThreads;
+            const int64_t batch = place / kParts * (int64_t)g.sharing + j / V8 % g.sharing;
+            const int64_t v = v0 + (batch * U + place % kParts * V8 + j % V8) * kThreads + eight % kThreads;
+            float x[E];
+            if (v < v1) row.load(v, x);
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (v < v1 && x[i] >= bound && x[i] > -__builtin_inff()) {
+                    const int at = atomicAdd(&l.count, 1);
+                    if (at < kList) l.keys[at] = order_key(x[i], (uint32_t)(v * E - row.head + i));
+                }
+        }
+        // meanwhile
+        if (threadIdx.x == kThreads - 64) {
+            for (int w = 0; w < kWaves - 1; ++w) st = join(st, stats[w]);
+            if (g.slices == 1) norm = finish<XT>(g, row_no, st);
+            else g.part_stats[blockIdx.x] = st;
+        }
+        __syncthreads();
         const int count = l.count;
-        if (flood || count > kList) flooded(l, row, v0, v1, bound, g.n);
+        if (eights > kEights || count > kList) flooded(l, row, v0, v1, bound, g.n);
         else order_list(l, count, g.n);
         // a slice can have fewer words than n that are larger than its bound
         if (!l.sorted[g.n - 1]) fill(l, row, v0, v1, bound, g.n);
-    }
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kWaves; ++w) st = join(st, stats[w]);
-        if (g.slices == 1) norm = finish<XT>(g, row_no, st);
-        else g.part_stats[blockIdx.x] = st;
-    }
-    if constexpr (TOP) {
-        if (g.slices == 1) {
-            __syncthreads();
-            write_top(g, row_no, l.sorted, norm);
-        } else {
+        if (g.slices == 1) write_top(g, row_no, l.sorted, norm);
+        else
             for (int i = threadIdx.x; i < g.n; i += kThreads) g.part_keys[(int64_t)blockIdx.x * g.n + i] = l.sorted[i];
-        }
+    } else if (threadIdx.x == 0) {
+        for (int w = 1; w < kWaves; ++w) st = join(st, stats[w]);
+        if (g.slices == 1) finish<XT>(g, row_no, st);
+        else g.part_stats[blockIdx.x] = st;
     }
 }
 
-// joins the slices of a row
+// joins the slices of a row: the bound is the least of the slices' ceil(n / slices)-th largest
 template <typename XT>
 __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(Args g) {
-    __shared__ uint64_t sorted[kTopMax];
+    __shared__ KeyList<kSlices * kTopMax> l;
     __shared__ Norm norm;
-    extern __shared__ uint64_t keys[];
     const int64_t row = g.first_row + blockIdx.x;
-    const int all = g.slices * g.n;
-    for (int i = threadIdx.x; i < all; i += kThreads) keys[i] = g.part_keys[(int64_t)blockIdx.x * all + i];
-    if (threadIdx.x < 64) {
-        Stats st{-__builtin_inff(), 0.f, 0.f};
-        for (int i = threadIdx.x; i < g.slices; i += 64) st = join(st, g.part_stats[(int64_t)blockIdx.x * g.slices + i]);
-        st = wave_join(st);
-        if (threadIdx.x == 0) norm = finish<XT>(g, row, st);
-    }
+    const int all = g.slices * g.n, lane = threadIdx.x & 63;
+    const uint64_t* keys = g.part_keys + (int64_t)blockIdx.x * all;
+    if (threadIdx.x == 0) l.count = 0;
+    uint64_t bound = lane < g.slices && g.n ? keys[lane * g.n + (g.n + g.slices - 1) / g.slices - 1] : ~(uint64_t)0;
+    bound = ~wave_max(~bound);
     __syncthreads();
     for (int i = threadIdx.x; i < all; i += kThreads) {
         const uint64_t key = keys[i];
-        if (!key) continue;                 // a slice with fewer elements than n
-        int before = 0;
-        for (int j = 0; j < all; ++j) before += keys[j] > key;
-        if (before < g.n) sorted[before] = key;
+        if (key && key >= bound) l.keys[atomicAdd(&l.count, 1)] = key;
+    }
+    if (threadIdx.x < 64) {
+        Stats st{-__builtin_inff(), 0.f, 0.f};
+        if (lane < g.slices) st = g.part_stats[(int64_t)blockIdx.x * g.slices + lane];
+        st = join_wave(st);
+        if (threadIdx.x == 0) norm = finish<XT>(g, row, st);
     }
     __syncthreads();
-    write_top(g, row, sorted, norm);
+    order_list(l, l.count, g.n);
+    write_top(g, row, l.sorted, norm);
 }
 
 struct BackArgs {
@@ -435,7 +518,9 @@ Plan plan_for(int dtype, int64_t T, int64_t V) {
     const int64_t vectors = (V + e - 1) / e + 1;      // one more for a row that starts between boundaries
     // workgroups for every compute unit, but not slices of less than two pieces a thread
     int64_t slices = 1;
-    while (slices < 32 && T * slices < 512 && vectors / (slices * 2) >= 2 * kThreads) slices *= 2;
+    while (slices < kSlices && T * slices < 512 && vectors / (slices * 2) >= 2 * kThreads) slices *= 2;
+    const int64_t most = kPlaces * kThreads * (kBatch / e);      // longer slices share places
+    while (slices < kSlices && slices * most < vectors) ++slices;
     Plan p;
     p.slice_vectors = (vectors + slices - 1) / slices;
     p.slices = (int)((vectors + p.slice_vectors - 1) / p.slice_vectors);
@@ -453,12 +538,18 @@ int launch(Args g, hipStream_t st) {
         g.first_row = r;
         g.part_stats = stats;
         const dim3 grid((unsigned)(rows * g.slices));
-        if (g.n) hipLaunchKernelGGL((logprobs_kernel<XT, true>), grid, dim3(kThreads), 0, st, g);
+        if (g.n) {
+            constexpr int per = kThreads * (kBatch / Row<XT>::E);
+            const int64_t batches = (g.slice_vectors + per - 1) / per;
+            g.sharing = (int)((batches + kPlaces - 1) / kPlaces);
+            const size_t lds = (size_t)((batches + g.sharing - 1) / g.sharing) * kThreads * sizeof(f32x4);
+            hipLaunchKernelGGL((logprobs_kernel<XT, true>), grid, dim3(kThreads), lds, st, g);
+        }
         else hipLaunchKernelGGL((logprobs_kernel<XT, false>), grid, dim3(kThreads), 0, st, g);
         int rc = hip_status(hipGetLastError());
         if (rc != BS_OK) return rc;
         if (g.slices == 1) continue;
-        hipLaunchKernelGGL(logprobs_join_kernel<XT>, dim3((unsigned)rows), dim3(kThreads), (size_t)g.slices * g.n * 8, st, g);
+        hipLaunchKernelGGL(logprobs_join_kernel<XT>, dim3((unsigned)rows), dim3(kThreads), 0, st, g);
         rc = hip_status(hipGetLastError());
         if (rc != BS_OK) return rc;
     }
