@@ -78,7 +78,7 @@ int launch_q4_pack(const void* W, int dtype, int64_t M, int64_t K, int group, ui
 size_t q4_gemv_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N);
 int launch_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t K, int group, const void* x, int dtype,
                    int64_t N, int64_t ldx, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, hipStream_t st);
-size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int top_k);
+size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k);
 int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,
                   const uint16_t* s1, const uint8_t* w2, const uint16_t* s2, int64_t F, int group, int top_k, int renormalise, void* y,
                   int64_t ldy, int32_t* ids, float* weights, void* workspace, size_t workspace_bytes, hipStream_t st);

@@ -80,7 +80,7 @@ int bs_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t 
 size_t bs_q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k, int group) {
     if (T < 1 || T > BS_MOE_TOKENS_MAX || !matrix_ok(D, F) || 2 * F > kMost || !limits_ok(D, F, group) || !type_ok(dtype)) return 0;
     if (E < 1 || E > BS_MOE_EXPERTS_MAX || top_k < 1 || top_k > E || top_k > BS_MOE_TOP_K_MAX) return 0;
-    return bs::q4_moe_workspace_bytes(dtype, T, D, F, top_k);
+    return bs::q4_moe_workspace_bytes(dtype, T, D, F, E, top_k);
 }
 
 int bs_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,

@@ -53,21 +53,6 @@ __device__ __forceinline__ void raise(Stats& a, float m) {
     a.m = m;
 }
 
-// the largest of a wavefront's values, in every lane; what is no number counts only where nothing else does
-__device__ __forceinline__ float max_of_wave(float v) {
-    v = fmaxf(v, dpp_move<0xB1>(v));
-    v = fmaxf(v, dpp_move<0x4E>(v));
-    v = fmaxf(v, dpp_move<0x141>(v));
-    v = fmaxf(v, dpp_move<0x140>(v));
-    uint32_t a = __builtin_bit_cast(uint32_t, v), b = a;
-    swap_rows(a, b);
-    v = fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
-    a = b = __builtin_bit_cast(uint32_t, v);
-    swap_halves(a, b);
-    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
-}
-__device__ __forceinline__ float sum_of_wave(float v) { return add_across_32(add_across_16(group_sum<16>(v))); }
-
 __device__ __forceinline__ Stats join(Stats a, Stats b) {
     const float m = fmaxf(a.m, b.m);
     raise(a, m);

@@ -261,32 +261,44 @@ struct Q4Walk {
     }
 };
 
-// x of a walk, read from memory: virtual rows at[t], 16-byte pieces from column 8 * kb on, zero behind `columns` (a multiple
-// of 8).  Chunks are read as far as there are any, and no further than `chunks`.
-template <int NT, int FETCH>
+__device__ __forceinline__ uint4 bits8(const uint16_t* row, int64_t k, int64_t K);
+
+// x of a walk, read from memory: virtual rows at[t], 16-byte pieces from column 8 * kb on, zero behind `columns`, which are
+// whole chunks unless RAGGED.  Chunks are read as far as there are any.  A lane without a virtual row loads nothing (few rows
+// cost few of the cache's cycles) and brings what its registers hold: that reaches sums of that row alone, which nobody reads.
+template <int NT, int FETCH, bool RAGGED>
 struct RowsOfX {
-    const uint16_t* at[NT];
+    const uint16_t* at[NT];     // nullptr: none
     int kb, columns, last;      // last: the last chunk
     uint4 v[NT][FETCH][4];
     __device__ __forceinline__ void fetch(int c, int u) {
         const int k = min(c + u, last) * kQ4Chunk;
-        if (k + kQ4Chunk <= columns) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+            uint4 (&w)[4] = v[t][u % FETCH];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[t][u % FETCH][i] = *reinterpret_cast<const uint4*>(at[t] + k + 32 * i + 8 * kb);
-        } else {
+            for (int i = 0; i < 4; ++i) asm volatile("" : "=v"(w[i].x), "=v"(w[i].y), "=v"(w[i].z), "=v"(w[i].w));
+            if (!at[t]) continue;
+            if (!RAGGED || k + kQ4Chunk <= columns) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+                for (int i = 0; i < 4; ++i) __builtin_memcpy(&w[i], at[t] + k + 32 * i + 8 * kb, 16);
+            } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int p = k + 32 * i + 8 * kb;
-                    const uint4 w = *reinterpret_cast<const uint4*>(at[t] + (p < columns ? p : 0));
-                    v[t][u % FETCH][i] = p < columns ? w : uint4{0, 0, 0, 0};
-                }
+                for (int i = 0; i < 4; ++i) w[i] = bits8(at[t], k + 32 * i + 8 * kb, columns);
+            }
         }
     }
     __device__ __forceinline__ uint4 operator()(int t, int, int u, int i) const { return v[t][u % FETCH][i]; }
+};
+
+// x of a walk in LDS: virtual rows at[t], zero behind K
+template <int NT>
+struct LdsRowsOfX {
+    const uint16_t* at[NT];      // the lane's piece of column 0
+    __device__ __forceinline__ void fetch(int, int) {}
+    __device__ __forceinline__ uint4 operator()(int t, int c, int u, int i) const {
+        return *reinterpret_cast<const uint4*>(at[t] + (c + u) * kQ4Chunk + 32 * i);
+    }
 };
 
 // x of a walk as the matrix unit takes it: 1 KB, the wavefront's 16-byte pieces side by side, for every tile, chunk and 32
@@ -307,22 +319,44 @@ struct TilesOfX {
     __device__ __forceinline__ uint4 operator()(int t, int, int u, int i) const { return v[t][u % FETCH][i]; }
 };
 
-// 8 activations from column k on; zero behind K.  `whole`: rows start on 16-byte boundaries.
+// 8 elements of a row from column k on, zero behind K; the row may start anywhere.  A piece that is not whole is the row's
+// last 8 elements, moved: no lane loads element by element, which would be eight trips to memory one after the other.
+__device__ __forceinline__ uint4 bits8(const uint16_t* row, int64_t k, int64_t K) {
+    uint4 v{0, 0, 0, 0};
+    if (K >= 8) {
+        const int64_t from = min(k, K - 8);
+        __builtin_memcpy(&v, row + from, 16);
+        if (k != from) v = k < K ? __builtin_bit_cast(uint4, __builtin_bit_cast(unsigned __int128, v) >> (16 * (int)(k - from))) : uint4{0, 0, 0, 0};
+    } else {
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = k + i < K ? row[k + i] : 0;
+        v = {h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+    }
+    return v;
+}
+
 template <typename XT>
-__device__ __forceinline__ void load8(const typename XT::type* row, int64_t k, int64_t K, bool whole, float (&v)[8]) {
-    if (whole && k + 8 <= K) {
-        if constexpr (sizeof(typename XT::type) == 4) {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(row + k), b = *reinterpret_cast<const f32x4*>(row + k + 4);
+__device__ __forceinline__ void load8(const typename XT::type* row, int64_t k, int64_t K, float (&v)[8]) {
+    if constexpr (sizeof(typename XT::type) == 2) {
+        const uint4 a = bits8(row, k, K);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-        } else {
-            const uint4 a = *reinterpret_cast<const uint4*>(row + k);
+        for (int i = 0; i < 8; ++i) v[i] = XT::load((uint16_t)(word_of(a, i >> 1) >> (16 * (i & 1))));
+    } else if (K >= 8) {
+        const int64_t from = min(k, K - 8);
+        __builtin_memcpy(v, row + from, 32);
+        if (k != from) {
+            const int by = (int)min(k - from, (int64_t)8);      // 3 bits of the distance, one after the other; 8: nothing is left
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = XT::load((uint16_t)(word_of(a, i >> 1) >> (16 * (i & 1))));
+            for (int step = 4; step; step /= 2)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = by & step ? (i + step < 8 ? v[i + step] : 0.f) : v[i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = by & 8 ? 0.f : v[i];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k + i < K ? XT::load(row[k + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : 0.f;
     }
 }
 
@@ -338,20 +372,30 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 (&p)[3]) {
 
 // 8 activations as the virtual rows' 16-byte pieces
 template <typename XT>
-__device__ __forceinline__ void pieces8(const typename XT::type* row, int64_t k, int64_t K, bool whole, uint4 (&p)[XT::kParts]) {
+__device__ __forceinline__ void pieces8(const typename XT::type* row, int64_t k, int64_t K, uint4 (&p)[XT::kParts]) {
     if constexpr (XT::kParts == 3) {
         float v[8];
-        load8<XT>(row, k, K, whole, v);
+        load8<XT>(row, k, K, v);
         split8(v, p);
-    } else if (whole && k + 8 <= K) {
-        p[0] = *reinterpret_cast<const uint4*>(row + k);
     } else {
-        uint32_t h[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = k + i < K ? row[k + i] : 0;
-        p[0] = {h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+        p[0] = bits8(row, k, K);
     }
 }
+
+// the largest of a wavefront's values, in every lane; what is no number counts only where nothing else does
+__device__ __forceinline__ float max_of_wave(float v) {
+    v = fmaxf(v, dpp_move<0xB1>(v));
+    v = fmaxf(v, dpp_move<0x4E>(v));
+    v = fmaxf(v, dpp_move<0x141>(v));
+    v = fmaxf(v, dpp_move<0x140>(v));
+    uint32_t a = __builtin_bit_cast(uint32_t, v), b = a;
+    swap_rows(a, b);
+    v = fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+    a = b = __builtin_bit_cast(uint32_t, v);
+    swap_halves(a, b);
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float sum_of_wave(float v) { return add_across_32(add_across_16(group_sum<16>(v))); }
 
 // 64-bit whole numbers in the order of what is chosen first: the larger value, then the lower index.  -0 counts as 0, a value
 // that is no number comes last.  None of them is 0, none is the largest 64-bit number.
@@ -365,12 +409,27 @@ __device__ __forceinline__ float value_of_key(uint64_t key) {
     const uint32_t o = (uint32_t)(key >> 32);
     return o ? __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o) : __builtin_nanf("");
 }
+// the largest of a wavefront's 64-bit numbers, in every lane
+template <int CTRL>
+__device__ __forceinline__ uint64_t max_moved(uint64_t v) {
+    const uint64_t other = (uint64_t)(uint32_t)dpp_move_i<CTRL>((int)(v >> 32)) << 32 | (uint32_t)dpp_move_i<CTRL>((int)v);
+    return other > v ? other : v;
+}
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-    for (int o = 1; o < 64; o *= 2) {
-        const uint64_t other = (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o) << 32 | (uint32_t)__shfl_xor((int)v, o);
-        v = other > v ? other : v;
-    }
-    return v;
+    v = max_moved<0xB1>(v);
+    v = max_moved<0x4E>(v);
+    v = max_moved<0x141>(v);
+    v = max_moved<0x140>(v);
+    uint32_t h0 = (uint32_t)(v >> 32), h1 = h0, l0 = (uint32_t)v, l1 = l0;
+    swap_rows(h0, h1);
+    swap_rows(l0, l1);
+    uint64_t a = (uint64_t)h0 << 32 | l0, b = (uint64_t)h1 << 32 | l1;
+    v = a > b ? a : b;
+    h0 = h1 = (uint32_t)(v >> 32), l0 = l1 = (uint32_t)v;
+    swap_halves(h0, h1);
+    swap_halves(l0, l1);
+    a = (uint64_t)h0 << 32 | l0, b = (uint64_t)h1 << 32 | l1;
+    return a > b ? a : b;
 }
 
 #endif  // __HIPCC__

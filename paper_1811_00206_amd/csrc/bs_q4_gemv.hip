@@ -6,9 +6,8 @@
 //
 // x comes to the matrix unit in two ways.  A few virtual rows (4: one fp32 vector, four in 16 bits) a workgroup brings to LDS
 // itself, in slabs of K, split into parts there; `tiles` groups of 16 rows share them.  More are read from memory by every
-// wavefront, 64 bytes of 16 rows at a time, which the caches hold: rows of 16-bit vectors as they are, where they start on
-// 16-byte boundaries and are whole pieces; else from the workspace, where a first kernel puts the parts of every vector,
-// padded with zeros.
+// wavefront, 64 bytes of 16 rows at a time, which the caches hold: rows of 16-bit vectors as they are, or tiles of parts that a
+// first kernel puts into the workspace.
 #include "bs_q4.h"
 
 namespace bs {
@@ -25,7 +24,6 @@ struct GemvArgs {
     void* y;
     int ways, tiles;    // wavefronts that share K; groups of wavefronts that share x in LDS
     int slab;           // columns of x in LDS at once
-    bool whole;         // rows of x start on 16-byte boundaries
 };
 
 // a wavefront's sums to LDS: [wave][R][NT][TPT][16]
@@ -73,19 +71,13 @@ __global__ __launch_bounds__(1024) void q4_gemv_kernel(GemvArgs g) {
             const T* row = static_cast<const T*>(g.x) + n * g.ldx;
             for (int j = threadIdx.x; j < pieces; j += blockDim.x) {
                 uint4 p[P];
-                pieces8<XT>(row, k0 + 8 * j, g.K, g.whole, p);
+                pieces8<XT>(row, k0 + 8 * j, g.K, p);
 #pragma unroll
                 for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(xs + (n * P + i) * xp + 8 * j) = p[i];
             }
         }
         __syncthreads();
-        struct {
-            const uint16_t* at;
-            __device__ __forceinline__ void fetch(int, int) {}
-            __device__ __forceinline__ uint4 operator()(int, int c, int u, int i) const {
-                return *reinterpret_cast<const uint4*>(at + (c + u) * kQ4Chunk + 32 * i);
-            }
-        } staged{mine - k0};
+        LdsRowsOfX<1> staged{{mine - k0}};
         walk.template rest<U>(c, g.ways, end, staged, acc);
     }
     __syncthreads();
@@ -127,13 +119,13 @@ __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(
         walk.template walk<kFetch>(wave, g.ways, chunks, x, acc);
     } else {
         static_assert(S == 1);
-        RowsOfX<NT, kFetch> x;
+        RowsOfX<NT, kFetch, true> x;
         x.kb = kb;
         x.columns = (int)g.K;
         x.last = chunks - 1;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)      // rows without a token repeat the last one
-            x.at[t] = static_cast<const uint16_t*>(g.x) + (n0 + min(t * TPT + r, tokens - 1)) * g.ldx;
+        for (int t = 0; t < NT; ++t)
+            x.at[t] = t * TPT + r < tokens ? static_cast<const uint16_t*>(g.x) + (n0 + t * TPT + r) * g.ldx : nullptr;
         walk.template walk<kFetch>(wave, g.ways, chunks, x, acc);
     }
     float* sums = reinterpret_cast<float*>(lds);
@@ -153,14 +145,14 @@ __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(
 // x as the matrix unit takes it (TilesOfX): a workgroup writes a chunk of a tile, 4 KB.  Columns behind K are zero, rows
 // without a token stay as they are.
 template <typename XT>
-__global__ __launch_bounds__(256) void q4_tiles_kernel(const void* x, int64_t K, int64_t N, int64_t ldx, bool whole, uint16_t* tiles) {
+__global__ __launch_bounds__(256) void q4_tiles_kernel(const void* x, int64_t K, int64_t N, int64_t ldx, uint16_t* tiles) {
     using T = typename XT::type;
     constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S;
     const int token = threadIdx.x % TPT, piece = threadIdx.x / TPT;
     const int64_t n = (int64_t)blockIdx.y * TPT + token, k = (int64_t)blockIdx.x * kQ4Chunk + 8 * piece;
     if (n >= N) return;
     uint4 p[P];
-    pieces8<XT>(static_cast<const T*>(x) + n * ldx, k, K, whole, p);
+    pieces8<XT>(static_cast<const T*>(x) + n * ldx, k, K, p);
     uint16_t* to = tiles + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2048 + 128 * piece + 8 * S * token;
 #pragma unroll
     for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(to + 8 * i) = p[i];
@@ -261,11 +253,11 @@ template <typename XT>
 int launch_type(GemvArgs g, const Plan& p, int group, void* workspace, hipStream_t st) {
     bool tiled = false;
     if (!p.staged) {
-        tiled = p.tiled || !g.whole || g.K % 8;
+        tiled = p.tiled;
         if (tiled) {
             constexpr int TPT = 16 / XT::kSlots;
             const dim3 grid((unsigned)(q4_padded(g.K) / kQ4Chunk), (unsigned)((g.N + TPT - 1) / TPT));
-            hipLaunchKernelGGL(q4_tiles_kernel<XT>, grid, dim3(16 * TPT), 0, st, g.x, g.K, g.N, g.ldx, g.whole,
+            hipLaunchKernelGGL(q4_tiles_kernel<XT>, grid, dim3(16 * TPT), 0, st, g.x, g.K, g.N, g.ldx,
                                static_cast<uint16_t*>(workspace));
             const int rc = hip_status(hipGetLastError());
             if (rc != BS_OK) return rc;
@@ -288,8 +280,7 @@ int launch_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int6
     const Plan p = plan_for(dtype, M, K, N);
     if (p.workspace && (!workspace || workspace_bytes < p.workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)))
         return BS_ERR_WORKSPACE;
-    const bool whole = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (N == 1 || ldx * dtype_bytes(dtype) % 16 == 0);
-    const GemvArgs g{codes, scales, M, K, N, ldx, ldy, x, y, p.ways, p.tiles, p.slab, whole};
+    const GemvArgs g{codes, scales, M, K, N, ldx, ldy, x, y, p.ways, p.tiles, p.slab};
     switch (dtype) {
         case BS_F32: return launch_type<F32>(g, p, group, workspace, st);
         case BS_F16: return launch_type<F16>(g, p, group, workspace, st);

@@ -1,23 +1,27 @@
 // A mixture-of-experts layer on 4-bit expert matrices for a few tokens (bs.h: bs_q4_moe), in three kernels:
 //
-//   route  one workgroup per token: router logits, the top_k largest, their weights; and the token's activations as
-//          virtual rows (bs_q4.h), padded with zeros, for the next kernel to read in whole pieces
-//   up     one workgroup per 16 hidden units of a chosen expert: gate and up rows against all tokens that chose it,
-//          h = silu(g) * u, written as virtual rows of the last kernel
-//   down   one workgroup per 16 outputs: its wavefronts share the chosen experts (and K, if the experts are fewer) and
-//          add weight * W2 h into sums of their own in LDS, which are added in the order of the wavefronts
+//   logits  a wavefront per token and four experts: router logits; and the token's activations as virtual rows (bs_q4.h),
+//           padded with zeros, for the next kernel to read in whole pieces
+//   up      every workgroup finds all tokens' top_k experts by itself (a fraction of a microsecond, against a kernel of its
+//           own), then has 16 or 64 hidden units of a chosen expert: gate and up rows against all tokens that chose it,
+//           h = silu(g) * u, written as virtual rows of the last kernel
+//   down    16 outputs a tile: the wavefronts of one or a few workgroups share steps of chosen experts and add weight * W2 h
+//           into sums of their own in LDS, which are added in the order of the wavefronts; of several workgroups the one that
+//           is done last adds their sums, in their order
 //
 // Bound: every chosen expert's codes once.  An expert is known by the first (token, choice) pair that chose it; the
-// workgroups of the other pairs end at once, so nothing is sorted or counted between the kernels.  No atomics: a result
-// has the same bits from every call.  Hidden values pass to `down` in two bfloat16 parts for 16-bit activations (16
+// workgroups of the other pairs end at once, so nothing is sorted between the kernels.  The order of all sums is fixed: a
+// result has the same bits from every call.  Hidden values pass to `down` in two bfloat16 parts for 16-bit activations (16
 // leading bits: their rounding is not seen behind the output's) and in three (all 24 bits) for fp32.
 #include "bs_q4.h"
+
+#include <type_traits>
 
 namespace bs {
 namespace {
 
-constexpr int kU = 2;
-constexpr int kDownWaves = 16;
+constexpr int kDownWaves = 8;
+constexpr size_t kLdsOfX = 40 * 1024, kLdsOfH = 64 * 1024;      // x and h are brought to LDS where they take no more
 constexpr int kMaxTokens = BS_MOE_TOKENS_MAX, kMaxExperts = BS_MOE_EXPERTS_MAX, kMaxTopK = BS_MOE_TOP_K_MAX;
 
 // Elements between virtual rows in the workspace: whole chunks and a cache line, so that rows a power of two long do not
@@ -33,51 +37,93 @@ struct MoeArgs {
     const void *x, *router;
     int64_t ldx, ldy;
     int T, D, E, F, top_k, pairs;
-    bool renormalise, whole_x, whole_router;
+    bool renormalise;
     const uint8_t *w1, *w2;
     const uint16_t *s1, *s2;
     void* y;
     int32_t* ids;
     float* weights;
     uint16_t *xp, *hp;      // [T][parts][D padded], [pairs][hidden parts][F padded]
-    int ways;
+    float* logits;          // [T][E]
+    float* parts;           // [down workgroups of a tile][D padded to tiles][T], if there are several
+    uint32_t* done;         // [tile]: those of them that are done
+    int32_t* leaders;       // number of chosen experts, then the first pair of each
+    uint32_t magic_x, magic_h;   // of the pieces of a row in LDS
+    int split, part_chunks;      // workgroups of a tile in `down`, and the chunks of F of each
+    int ways, tiles, rows;       // rows: tokens whose sums a wavefront of `up` keeps
 };
 
-template <typename XT>
-__global__ __launch_bounds__(1024) void moe_route_kernel(MoeArgs g) {
+// one wavefront: EB router rows (those that there are) times a token's activations
+template <typename XT, int EB>
+__device__ __forceinline__ void router_rows(const MoeArgs& g, const typename XT::type* x, int e, float* logits) {
     using T = typename XT::type;
-    constexpr int P = XT::kParts, EB = 4;
-    __shared__ float logits[kMaxExperts];
-    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const T* x = static_cast<const T*>(g.x) + t * g.ldx;
-    const int64_t columns = q4_padded(g.D), dp = row_pitch(g.D);
-    for (int e = wave * EB; e < g.E; e += waves * EB) {
-        float sum[EB] = {};
-        for (int k = 8 * lane; k < g.D; k += 512) {
-            float a[8], w[8];
-            load8<XT>(x, k, g.D, g.whole_x, a);
+    const int lane = threadIdx.x & 63;
+    float sum[EB] = {};
+    const T* row[EB];
 #pragma unroll
-            for (int i = 0; i < EB; ++i) {
-                const T* row = static_cast<const T*>(g.router) + (int64_t)min(e + i, g.E - 1) * g.D;
-                load8<XT>(row, k, g.D, g.whole_router, w);
+    for (int i = 0; i < EB; ++i) row[i] = static_cast<const T*>(g.router) + (int64_t)min(e + i, g.E - 1) * g.D;
+#pragma unroll 4
+    for (int k0 = 0; k0 < g.D; k0 += 512) {
+        float a[8], w[EB][8];
+        load8<XT>(x, k0 + 8 * lane, g.D, a);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[i] = fmaf(a[j], w[j], sum[i]);
-            }
-        }
+        for (int i = 0; i < EB; ++i) load8<XT>(row[i], k0 + 8 * lane, g.D, w[i]);
 #pragma unroll
-        for (int i = 0; i < EB; ++i) {
-            const float s = group_sum<64>(sum[i]);
-            if (lane == 0 && e + i < g.E) logits[e + i] = s;
-        }
+        for (int i = 0; i < EB; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[i] = fmaf(a[j], w[i][j], sum[i]);
     }
-    for (int64_t k = 8 * threadIdx.x; k < columns; k += 8 * blockDim.x) {
+#pragma unroll
+    for (int i = 0; i < EB; ++i) {
+        const float s = sum_of_wave(sum[i]);
+        if (lane == 0 && e + i < g.E) logits[e + i] = s;
+    }
+}
+
+// blockIdx: token, 16 experts.  A wavefront has four of them, and the first workgroup of a token its virtual rows.
+template <typename XT>
+__global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs g) {
+    constexpr int P = XT::kParts, EB = 4;
+    const int t = blockIdx.x, e = blockIdx.y * 16 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * EB;
+    const typename XT::type* x = static_cast<const typename XT::type*>(g.x) + t * g.ldx;
+    if (e < g.E) router_rows<XT, EB>(g, x, e, g.logits + t * g.E);
+    if (blockIdx.y) return;
+    const int64_t columns = q4_padded(g.D), dp = row_pitch(g.D);
+    for (int64_t k = 8 * threadIdx.x; k < columns; k += 8 * 256) {
         uint4 p[P];
-        pieces8<XT>(x, k, g.D, g.whole_x, p);
+        pieces8<XT>(x, k, g.D, p);
 #pragma unroll
         for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(g.xp + ((int64_t)t * P + i) * dp + k) = p[i];
     }
-    __syncthreads();
-    if (wave) return;
+}
+
+// One wavefront: a token's top_k experts and their weights.  Up to 64 experts are a lane's each: the largest logit of the free
+// lanes, and of lanes that have it the first.  (A logit that is no number is the lowest there is.)
+__device__ __forceinline__ void choose(const MoeArgs& g, const float* logits, int32_t* ids, float* weights) {
+    const int lane = threadIdx.x & 63;
+    if (g.E <= 64) {
+        float l = lane < g.E ? logits[lane] : 0.f;
+        const bool nan = l != l;
+        const float own = nan ? -__builtin_inff() : l;
+        uint64_t free = g.E == 64 ? ~(uint64_t)0 : ((uint64_t)1 << g.E) - 1;
+        int rank = -1;
+        float top = 0.f;
+        for (int j = 0; j < g.top_k; ++j) {
+            const float most = max_of_wave(free >> lane & 1 ? own : -__builtin_inff());
+            const uint64_t m = __ballot(own == most) & free;
+            const int first = __ffsll((unsigned long long)m) - 1;
+            if (lane == first) rank = j;
+            free &= ~((uint64_t)1 << first);
+            if (j == 0) top = most;
+        }
+        const float w = nan ? l : expf(own - top);
+        const float sum = sum_of_wave(lane < g.E && (!g.renormalise || rank >= 0) ? w : 0.f);
+        if (rank >= 0) {
+            ids[rank] = lane;
+            weights[rank] = w / sum;
+        }
+        return;
+    }
     float top = 0.f, mine = 0.f, all = 0.f, chosen = 0.f;      // lane j < top_k: its choice's exp(logit - top)
     int32_t id = 0;
     uint64_t last = ~(uint64_t)0;                              // the choice before: every key below it is still free
@@ -87,22 +133,39 @@ __global__ __launch_bounds__(1024) void moe_route_kernel(MoeArgs g) {
             const uint64_t key = order_key(logits[e], e);
             if (key < last && key > best) best = key;
         }
-        best = wave_max(best);
-        last = best;
-        const int e = (int)index_of_key(best);
-        const float l = logits[e];
+        last = wave_max(best);
+        const float l = value_of_key(last);
         if (j == 0) top = l;
         const float w = expf(l - top);
         chosen += w;
-        if (lane == j) { mine = w; id = e; }
+        if (lane == j) { mine = w; id = (int32_t)index_of_key(last); }
     }
     if (!g.renormalise) {
         for (int e = lane; e < g.E; e += 64) all += expf(logits[e] - top);
-        all = group_sum<64>(all);
+        all = sum_of_wave(all);
     }
     if (lane < g.top_k) {
-        g.ids[t * g.top_k + lane] = id;
-        g.weights[t * g.top_k + lane] = mine / (g.renormalise ? chosen : all);
+        ids[lane] = id;
+        weights[lane] = mine / (g.renormalise ? chosen : all);
+    }
+}
+
+// rows of `pieces` 16-byte pieces to LDS, `have` of which there are
+__device__ __forceinline__ void rows_to_lds(uint16_t* to, int to_pitch, const uint16_t* from, int64_t from_pitch, int rows, int pieces,
+                                            uint32_t magic, int have) {
+    const int all = rows * pieces, stride = blockDim.x;
+    const auto load = [&](int j, int& at) {      // (what is not there is read as what is, and not stored)
+        const int row = (int)div_magic_any(min(j, all - 1), pieces, magic), k = min(j, all - 1) - row * pieces;
+        at = j < all && k < have ? row * to_pitch + 8 * k : -1;
+        return *reinterpret_cast<const uint4*>(from + row * from_pitch + 8 * min(k, have - 1));
+    };
+    for (int j = threadIdx.x; j < all; j += 4 * stride) {      // four on their way together
+        int a0, a1, a2, a3;
+        const uint4 v0 = load(j, a0), v1 = load(j + stride, a1), v2 = load(j + 2 * stride, a2), v3 = load(j + 3 * stride, a3);
+        if (a0 >= 0) *reinterpret_cast<uint4*>(to + a0) = v0;
+        if (a1 >= 0) *reinterpret_cast<uint4*>(to + a1) = v1;
+        if (a2 >= 0) *reinterpret_cast<uint4*>(to + a2) = v2;
+        if (a3 >= 0) *reinterpret_cast<uint4*>(to + a3) = v3;
     }
 }
 
@@ -120,67 +183,120 @@ __device__ __forceinline__ int pairs_of(const int32_t* ids, int pairs, int first
     return n;
 }
 
-template <typename XT, int NT, int GL>
+// LDS of `down` before h.  (All LDS here is dynamic: the kernels' limits are raised to all that a compute unit has.)
+__host__ __device__ constexpr int down_small(int T, int pairs) { return (kDownWaves * T * 68 + pairs * 12 + 4 + 15) / 16 * 16; }
+// LDS of `up` before its sums
+__host__ __device__ constexpr int up_small(int T, int pairs, int E) { return (pairs * 8 + T * 4 + 4 + E * 4 + 15) / 16 * 16; }
+
+// 16 * tiles hidden units of a chosen expert.  Half of the wavefronts have the gate rows, half the up rows; each half shares
+// D, and a wavefront walks its columns of one tile after the other, the next one's codes on their way.  IN_LDS: the tokens' x
+// is brought to LDS, else read from memory.  ALONE: without the kernel of the logits, they are made here, by every workgroup.
+template <typename XT, int NT, int GL, bool IN_LDS, bool ALONE>
 __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
-    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S, HP = Hidden<XT>::kParts;
+    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S, HP = Hidden<XT>::kParts, U = IN_LDS ? 4 : 2;
     extern __shared__ __align__(16) uint8_t lds[];
-    float* sums = reinterpret_cast<float*>(lds);        // [wave][gate, up][NT][TPT][16]
-    __shared__ int32_t list[kMaxTokens];
-    __shared__ int found;
+    int32_t* ids = reinterpret_cast<int32_t*>(lds);                                         // [pairs]
+    float* weights = reinterpret_cast<float*>(ids + g.pairs);                               // [pairs]
+    int32_t* list = reinterpret_cast<int32_t*>(weights + g.pairs);                          // [T], then their number
+    int32_t* first_of = list + g.T + 1;                                                     // [E]
+    float* sums = reinterpret_cast<float*>(lds + up_small(g.T, g.pairs, g.E));      // [way][gate, up][tile][rows][16]
+    uint16_t* xs = reinterpret_cast<uint16_t*>(sums + 2 * g.ways * g.tiles * g.rows * 16);         // [rows * parts][D padded + 8]
     const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int pair = blockIdx.y, f0 = 16 * blockIdx.x;
-    const int e = g.ids[pair];
-    int earlier = 0;
-    for (int p = threadIdx.x; p < pair; p += blockDim.x) earlier |= g.ids[p] == e;
-    if (__syncthreads_or(earlier)) return;
-    if (wave == 0) {
-        const int n = pairs_of(g.ids, g.pairs, pair, e, list);
-        if (lane == 0) found = n;
-    }
-    __syncthreads();
-    const int tokens = found;
+    const int pair = blockIdx.y, f0 = 16 * g.tiles * blockIdx.x, half = wave & 1, way = wave >> 1;
     const int64_t fp = row_pitch(g.F), dp = row_pitch(g.D);
     const int chunks = (int)(q4_padded(g.D) / kQ4Chunk);
+    const int xp = chunks * kQ4Chunk + 8;
+    if constexpr (ALONE) {
+        float* logits = sums;      // [T][E], before the sums
+        for (int i = wave; i < g.T * g.E; i += 2 * g.ways)
+            router_rows<XT, 1>(g, static_cast<const typename XT::type*>(g.x) + i / g.E * g.ldx, i % g.E, logits + i / g.E * g.E);
+        for (int t = 0; t < g.T; ++t)
+            for (int j = threadIdx.x; j < chunks * (kQ4Chunk / 8); j += blockDim.x) {
+                uint4 p[P];
+                pieces8<XT>(static_cast<const typename XT::type*>(g.x) + t * g.ldx, 8 * j, g.D, p);
+#pragma unroll
+                for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(xs + (t * P + i) * xp + 8 * j) = p[i];
+            }
+        __syncthreads();
+        for (int t = wave; t < g.T; t += 2 * g.ways) choose(g, logits + t * g.E, ids + t * g.top_k, weights + t * g.top_k);
+    } else {
+        for (int t = wave; t < g.T; t += 2 * g.ways) choose(g, g.logits + t * g.E, ids + t * g.top_k, weights + t * g.top_k);
+    }
+    __syncthreads();
+    const int e = __builtin_amdgcn_readfirstlane(ids[pair]);
+    for (int b = 0; b < pair; b += 64)      // every wavefront by itself: the expert is an earlier pair's
+        if (__any(b + lane < pair && ids[min(b + lane, pair)] == e)) return;
     const int64_t pitch = q4_row_bytes(g.D), groups = (g.D + (32 << GL) - 1) >> (5 + GL);
-    constexpr int V = 4 / S, kOut = NT * TPT * 16;
+    const int64_t first = ((int64_t)e * 2 + half) * g.F;      // of the expert's gate or up rows
+    Q4Walk<XT::kHalf, NT, 1, GL, U> walk;
+    const auto start = [&](int tile) {
+        walk.tile(0, g.w1 + first * pitch, g.s1 + first * groups, f0 + 16 * tile, g.F, g.D, lane);
+        walk.load(way * U);
+    };
+    start(0);
+    // x of all tokens while the first codes are on their way
+    if constexpr (IN_LDS && !ALONE) rows_to_lds(xs, xp, g.xp, dp, g.T * P, chunks * (kQ4Chunk / 8), g.magic_x, chunks * (kQ4Chunk / 8));
+    if (wave == 0) {
+        const int n = pairs_of(ids, g.pairs, pair, e, list);
+        if (lane == 0) list[g.T] = n;
+    }
+    __syncthreads();
+    const int tokens = list[g.T];
+    constexpr int V = 4 / S;
+    const int out = g.tiles * g.rows * 16;      // sums of a wavefront
     for (int n0 = 0; n0 < tokens; n0 += NT * TPT) {
         const int here = min(tokens - n0, NT * TPT);
-        if (f0 < g.F) {
-            Q4Walk<XT::kHalf, NT, 2, GL, kU> walk;
+        std::conditional_t<IN_LDS, LdsRowsOfX<NT>, RowsOfX<NT, U, false>> x;
+        if constexpr (IN_LDS) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int64_t first = ((int64_t)e * 2 + i) * g.F;      // of the expert's gate or up rows
-                walk.tile(i, g.w1 + first * pitch, g.s1 + first * groups, f0, g.F, g.D, lane);
-            }
-            RowsOfX<NT, kU> x;
+            for (int t = 0; t < NT; ++t)      // rows without a token repeat the last one
+                x.at[t] = xs + (list[n0 + min(t * TPT + r / S, here - 1)] / g.top_k * P + min(r % S, P - 1)) * xp + 8 * kb;
+        } else {
             x.kb = kb;
             x.columns = chunks * kQ4Chunk;
             x.last = chunks - 1;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const int token = list[n0 + min(t * TPT + r / S, here - 1)] / g.top_k;
-                x.at[t] = g.xp + ((int64_t)token * P + min(r % S, P - 1)) * dp;
+                const int n = t * TPT + r / S;
+                const bool row = n < here && r % S < P;
+                x.at[t] = row ? g.xp + ((int64_t)(list[n0 + n] / g.top_k) * P + r % S) * dp : nullptr;
             }
-            f32x4 acc[2][NT] = {};
-            walk.template walk<kU>(wave, g.ways, chunks, x, acc);
+        }
+        if (n0) start(0);
+        for (int tile = 0; tile < g.tiles; ++tile) {
+            f32x4 acc[1][NT] = {};
+            for (int c = way * U; c < chunks;) {
+                const int now = c;
+                walk.take();
+                c += g.ways * U;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int u = 0; u < U; ++u) x.fetch(now, u);
+                if (c < chunks) walk.load(c);
+                else if (tile + 1 < g.tiles) start(tile + 1);
+                uint32_t sc[1][decltype(walk)::kWords][4];
+                walk.spread(sc);
+                walk.template eat<0, U>(now, chunks, x, sc, acc);
+            }
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        float sum = acc[i][t][v];
-                        if constexpr (S == 4) sum = acc[i][t][0] + (acc[i][t][1] + acc[i][t][2]);
-                        sums[((wave * 2 + i) * NT * TPT + t * TPT + kb * V + v) * 16 + r] = sum;
-                    }
+                for (int v = 0; v < V; ++v) {
+                    const f32x4& a = acc[0][t];
+                    float sum = a[v];
+                    if constexpr (S == 4) sum = a[0] + (a[1] + a[2]);
+                    const int n = t * TPT + kb * V + v;
+                    if (n < here) sums[wave * out + (tile * g.rows + n) * 16 + r] = sum;
+                }
         }
         __syncthreads();
-        for (int o = threadIdx.x; o < here * 16; o += blockDim.x) {
-            const int f = f0 + o % 16;
+        for (int o = threadIdx.x; o < g.tiles * here * 16; o += blockDim.x) {
+            const int tile = o / (here * 16), n = o / 16 % here, f = f0 + 16 * tile + o % 16;
+            if (f >= fp) continue;
             float h = 0.f;      // behind F: zeros up to whole chunks
             if (f < g.F) {
-                float gate = sums[o], up = sums[kOut + o];
-                for (int w = 1; w < g.ways; ++w) { gate += sums[2 * w * kOut + o]; up += sums[(2 * w + 1) * kOut + o]; }
+                const float* from = sums + (tile * g.rows + n) * 16 + o % 16;
+                float gate = from[0], up = from[out];
+                for (int w = 1; w < g.ways; ++w) { gate += from[2 * w * out]; up += from[(2 * w + 1) * out]; }
                 h = gate / (1.f + expf(-gate)) * up;
             }
             uint32_t part[3];
@@ -189,67 +305,106 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
                 const float rest = __builtin_bit_cast(float, part[1]) + __builtin_bit_cast(float, part[2]);
                 part[1] = (uint32_t)BF16::store(rest) << 16;
             }
-            uint16_t* to = g.hp + (int64_t)list[n0 + o / 16] * HP * fp + f;
+            uint16_t* to = g.hp + (int64_t)list[n0 + n] * HP * fp + f;
 #pragma unroll
             for (int i = 0; i < HP; ++i) to[i * fp] = (uint16_t)(part[i] >> 16);
         }
         __syncthreads();
     }
+    if (blockIdx.x || pair) return;
+    // the first workgroup says what was chosen, and for `down` the first pair of every chosen expert, and their number
+    for (int i = threadIdx.x; i < g.E; i += blockDim.x) first_of[i] = g.pairs;
+    if (g.split > 1)
+        for (int i = threadIdx.x; i < (g.D + 15) / 16; i += blockDim.x) g.done[i] = 0;
+    __syncthreads();
+    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) {
+        g.ids[p] = ids[p];
+        g.weights[p] = weights[p];
+        atomicMin(first_of + ids[p], p);
+    }
+    __syncthreads();
+    if (wave) return;
+    int n = 0;
+    for (int b = 0; b < g.pairs; b += 64) {
+        const int p = b + lane;
+        const bool leads = p < g.pairs && first_of[ids[min(p, g.pairs - 1)]] == p;
+        const uint64_t m = __ballot(leads);
+        if (leads) g.leaders[1 + n + lanes_below(m)] = p;
+        n += __popcll(m);
+    }
+    if (lane == 0) g.leaders[0] = n;
 }
 
-template <typename XT, int GL>
-__global__ __launch_bounds__(1024) void moe_down_kernel(MoeArgs g) {
-    constexpr int P = Hidden<XT>::kParts, S = Hidden<XT>::kSlots, TPT = 16 / S, V = 4 / S;
+// Workgroup z of a tile has a part of F, two chunks at least; a wavefront's work is one step of one chosen expert after the
+// other: (expert, two chunks).  While a step is multiplied the codes of its next one, of whatever expert, are on their way.
+// IN_LDS: the part's h of all pairs is brought to LDS, else read from memory.
+template <typename XT, int GL, bool IN_LDS>
+__global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
+    constexpr int P = Hidden<XT>::kParts, S = Hidden<XT>::kSlots, TPT = 16 / S, V = 4 / S, U = 2;
     extern __shared__ __align__(16) uint8_t lds[];
     float* sums = reinterpret_cast<float*>(lds);                                     // [wave][T][16]
     int32_t* ids = reinterpret_cast<int32_t*>(sums + kDownWaves * g.T * 16);         // [pairs]
-    int32_t* leaders = ids + g.pairs;                                                // [pairs]
-    int32_t* first_of = leaders + g.pairs;                                           // [E]
-    int32_t* lists = first_of + g.E;                                                 // [wave][T]
+    float* weights = reinterpret_cast<float*>(ids + g.pairs);                        // [pairs]
+    int32_t* leaders = reinterpret_cast<int32_t*>(weights + g.pairs);                // [pairs]
+    int32_t* lists = leaders + g.pairs;                                              // [wave][T]
     int32_t* found = lists + kDownWaves * g.T;
+    uint16_t* xs = reinterpret_cast<uint16_t*>(lds + down_small(g.T, g.pairs));      // [pairs * parts][columns + 8]
     const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int d0 = 16 * blockIdx.x;
-    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) ids[p] = g.ids[p];
-    for (int i = threadIdx.x; i < kDownWaves * g.T * 16; i += blockDim.x) sums[i] = 0.f;
-    for (int i = threadIdx.x; i < g.E; i += blockDim.x) first_of[i] = g.pairs;
-    __syncthreads();
-    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) atomicMin(first_of + ids[p], p);
-    __syncthreads();
-    if (wave == 0) {      // the first pair of every chosen expert
-        int n = 0;
-        for (int b = 0; b < g.pairs; b += 64) {
-            const int p = b + lane;
-            const bool first = p < g.pairs && first_of[ids[p]] == p;
-            const uint64_t m = __ballot(first);
-            if (first) leaders[n + lanes_below(m)] = p;
-            n += __popcll(m);
-        }
-        if (lane == 0) *found = n;
-    }
-    __syncthreads();
-    const int experts = __builtin_amdgcn_readfirstlane(*found);
     const int64_t fp = row_pitch(g.F);
-    const int chunks = (int)(q4_padded(g.F) / kQ4Chunk);
+    const int chunks = (int)(q4_padded(g.F) / kQ4Chunk), first_chunk = blockIdx.y * g.part_chunks;
+    const int end = min(chunks, first_chunk + g.part_chunks), steps = (end - first_chunk + U - 1) / U;
+    const int xp = g.part_chunks * kQ4Chunk + 8;
+    if constexpr (IN_LDS)
+        rows_to_lds(xs, xp, g.hp + first_chunk * kQ4Chunk, fp, g.pairs * P, g.part_chunks * (kQ4Chunk / 8), g.magic_h,
+                    (end - first_chunk) * (kQ4Chunk / 8));
+    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) {
+        ids[p] = g.ids[p];
+        weights[p] = g.weights[p];
+        leaders[p] = g.leaders[1 + p];      // (behind the last one: not looked at)
+    }
+    const int experts = g.leaders[0];
+    for (int i = threadIdx.x; i < kDownWaves * g.T * 16; i += blockDim.x) sums[i] = 0.f;
+    __syncthreads();
+    const int items = experts * steps;
     const int64_t pitch = q4_row_bytes(g.F), groups = (g.F + (32 << GL) - 1) >> (5 + GL);
-    const int ways = experts >= kDownWaves ? 1 : min(kDownWaves / experts, (chunks + kU - 1) / kU);
     float* mine = sums + wave * g.T * 16;
     int32_t* list = lists + wave * g.T;
-    for (int item = wave; item < experts * ways; item += kDownWaves) {
-        const int first = __builtin_amdgcn_readfirstlane(leaders[item / ways]), c0 = item % ways;
-        const int e = __builtin_amdgcn_readfirstlane(ids[first]);
-        const int tokens = pairs_of(ids, g.pairs, first, e, list);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the list is written by some lanes and read by others
-        Q4Walk<false, 1, 1, GL, kU> walk;
-        walk.tile(0, g.w2 + (int64_t)e * g.D * pitch, g.s2 + (int64_t)e * g.D * groups, d0, g.D, g.F, lane);
+    Q4Walk<false, 1, 1, GL, U> walk;
+    int next = -1, listed = -1, tokens = 0;      // pairs that stand for the expert being loaded, and that of the list
+    const auto load = [&](int item) {
+        next = __builtin_amdgcn_readfirstlane(leaders[item / steps]);
+        const int64_t e = __builtin_amdgcn_readfirstlane(ids[next]);
+        walk.tile(0, g.w2 + e * g.D * pitch, g.s2 + e * g.D * groups, d0, g.D, g.F, lane);
+        walk.load(first_chunk + item % steps * U);
+    };
+    if (wave < items) load(wave);
+    for (int item = wave; item < items; item += kDownWaves) {
+        const int c = first_chunk + item % steps * U;
+        if (next != listed) {
+            listed = next;
+            tokens = pairs_of(ids, g.pairs, listed, ids[listed], list);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the list is written by some lanes and read by others
+        }
+        walk.take();
+        uint32_t sc[1][decltype(walk)::kWords][4];
+        walk.spread(sc);
         for (int n0 = 0; n0 < tokens; n0 += TPT) {
             const int here = min(tokens - n0, TPT);
-            RowsOfX<1, kU> x;
-            x.kb = kb;
-            x.columns = chunks * kQ4Chunk;
-            x.last = chunks - 1;
-            x.at[0] = g.hp + ((int64_t)list[n0 + min(r / S, here - 1)] * P + min(r % S, P - 1)) * fp;
+            std::conditional_t<IN_LDS, LdsRowsOfX<1>, RowsOfX<1, U, false>> x;
+            if constexpr (IN_LDS) {
+                x.at[0] = xs + (list[n0 + min(r / S, here - 1)] * P + min(r % S, P - 1)) * xp + 8 * kb - first_chunk * kQ4Chunk;
+            } else {
+                x.kb = kb;
+                x.columns = chunks * kQ4Chunk;
+                x.last = chunks - 1;
+                x.at[0] = r / S < here && r % S < P ? g.hp + ((int64_t)list[n0 + r / S] * P + r % S) * fp : nullptr;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) x.fetch(c, u);
+            if (n0 + TPT >= tokens && item + kDownWaves < items) load(item + kDownWaves);
             f32x4 acc[1][1] = {};
-            walk.template walk<kU>(c0, ways, chunks, x, acc);
+            walk.template eat<0, U>(c, end, x, sc, acc);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int n = kb * V + v;
@@ -259,44 +414,88 @@ __global__ __launch_bounds__(1024) void moe_down_kernel(MoeArgs g) {
                 if constexpr (S == 4) sum = acc[0][0][0] + (acc[0][0][1] + acc[0][0][2]);
                 else sum = acc[0][0][2 * v] + acc[0][0][2 * v + 1];
                 float* to = mine + pair / g.top_k * 16 + r;
-                *to = fmaf(g.weights[pair], sum, *to);
+                *to = fmaf(weights[pair], sum, *to);
             }
         }
     }
     __syncthreads();
-    for (int o = threadIdx.x; o < g.T * 16; o += blockDim.x) {
-        const int t = o / 16, d = d0 + o % 16;
-        if (d >= g.D) continue;
+    const int all = g.T * 16;
+    float* parts = g.parts + (int64_t)blockIdx.x * g.split * all;      // of this tile
+    for (int o = threadIdx.x; o < all; o += blockDim.x) {
         float sum = sums[o];
-        for (int w = 1; w < kDownWaves; ++w) sum += sums[w * g.T * 16 + o];
-        static_cast<typename XT::type*>(g.y)[t * g.ldy + d] = XT::store(sum);
+        for (int w = 1; w < kDownWaves; ++w) sum += sums[w * all + o];
+        if (g.split == 1) {
+            if (d0 + o % 16 < g.D) static_cast<typename XT::type*>(g.y)[o / 16 * g.ldy + d0 + o % 16] = XT::store(sum);
+        } else {      // past the caches that other compute units do not look into; see below
+            __hip_atomic_store(parts + blockIdx.y * all + o, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    if (g.split == 1) return;
+    // The sums were stored, and are loaded, with the scope of the whole GPU, so that they are where everybody sees them as soon
+    // as each lane has waited for its own.  A fence of that scope would write back all that the cache holds: 16 us here.
+    wait_vm_and_lds<0>();
+    pin_order();
+    __syncthreads();
+    if (threadIdx.x == 0) *found = (int)__hip_atomic_fetch_add(g.done + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (*found != g.split - 1) return;      // another workgroup will be last
+    for (int o = threadIdx.x; o < all; o += blockDim.x) {
+        float sum = __hip_atomic_load(parts + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int z = 1; z < g.split; ++z) sum += __hip_atomic_load(parts + z * all + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (d0 + o % 16 < g.D) static_cast<typename XT::type*>(g.y)[o / 16 * g.ldy + d0 + o % 16] = XT::store(sum);
     }
 }
 
-// all of it dynamic: the kernel's limit is raised to all that a compute unit has
-size_t down_lds(const MoeArgs& g) { return (size_t)kDownWaves * g.T * 68 + (size_t)g.pairs * 8 + (size_t)g.E * 4 + 4; }
+template <typename XT, int GL, int NT, bool IN_LDS, bool ALONE>
+int launch_up_rows(const MoeArgs& g, size_t lds, hipStream_t st) {
+    using Reg = LdsKernelOf<moe_up_kernel<XT, NT, GL, IN_LDS, ALONE>>;
+    if (lds > kLdsWithoutLimit) {
+        const int rc = ensure_lds_limit(Reg::reg, st);
+        if (rc != BS_OK) return rc;
+    }
+    const dim3 grid((unsigned)((q4_padded(g.F) + 16 * g.tiles - 1) / (16 * g.tiles)), (unsigned)g.pairs);
+    hipLaunchKernelGGL((moe_up_kernel<XT, NT, GL, IN_LDS, ALONE>), grid, dim3(128 * g.ways), lds, st, g);
+    return hip_status(hipGetLastError());
+}
+
+template <typename XT, int GL>
+int launch_up(MoeArgs g, hipStream_t st) {
+    constexpr int TPT = 16 / XT::kSlots;
+    // four tiles a workgroup where that still leaves two workgroups for a compute unit
+    g.tiles = g.pairs * (q4_padded(g.F) / 16) >= 2048 ? 4 : 1;
+    g.rows = g.T < TPT ? g.T : g.T < 2 * TPT ? g.T : 2 * TPT;
+    const int small = up_small(g.T, g.pairs, g.E), sums = 2 * g.ways * g.tiles * g.rows * 64;
+    const size_t lds_x = (size_t)g.rows * XT::kParts * (q4_padded(g.D) + 8) * 2;
+    // The logits by every workgroup itself where they are few (1 token, 8 experts, 1500 columns: 12.4 us in two kernels against
+    // 16.8 in three); 64 experts of 2048 columns would have each read 256 KB.
+    if (g.T <= TPT && lds_x <= kLdsOfX && (int64_t)g.T * g.E * g.D <= 32768 && g.T * g.E * 4 <= sums)
+        return launch_up_rows<XT, GL, 1, true, true>(g, small + sums + lds_x, st);
+    hipLaunchKernelGGL(moe_logits_kernel<XT>, dim3(g.T, (g.E + 15) / 16), dim3(256), 0, st, g);
+    const int rc = hip_status(hipGetLastError());
+    if (rc != BS_OK) return rc;
+    if (g.T > TPT) return launch_up_rows<XT, GL, 2, false, false>(g, small + sums, st);
+    return lds_x <= kLdsOfX ? launch_up_rows<XT, GL, 1, true, false>(g, small + sums + lds_x, st)
+                            : launch_up_rows<XT, GL, 1, false, false>(g, small + sums, st);
+}
+
+template <typename XT, int GL, bool IN_LDS>
+int launch_down(const MoeArgs& g, size_t lds, hipStream_t st) {
+    using Reg = LdsKernelOf<moe_down_kernel<XT, GL, IN_LDS>>;
+    if (lds > kLdsWithoutLimit) {
+        const int rc = ensure_lds_limit(Reg::reg, st);
+        if (rc != BS_OK) return rc;
+    }
+    const dim3 grid((unsigned)((g.D + 15) / 16), (unsigned)g.split);
+    hipLaunchKernelGGL((moe_down_kernel<XT, GL, IN_LDS>), grid, dim3(64 * kDownWaves), lds, st, g);
+    return hip_status(hipGetLastError());
+}
 
 template <typename XT, int GL>
 int launch(const MoeArgs& g, hipStream_t st) {
-    constexpr int TPT = 16 / XT::kSlots;
-    using Down = LdsKernelOf<moe_down_kernel<XT, GL>>;
-    const size_t lds = down_lds(g);
-    if (lds > kLdsWithoutLimit) {
-        const int rc = ensure_lds_limit(Down::reg, st);
-        if (rc != BS_OK) return rc;
-    }
-    const int route_waves = g.E > 32 ? 16 : g.E > 16 ? 8 : 4;
-    hipLaunchKernelGGL(moe_route_kernel<XT>, dim3(g.T), dim3(64 * route_waves), 0, st, g);
-    int rc = hip_status(hipGetLastError());
+    const int rc = launch_up<XT, GL>(g, st);
     if (rc != BS_OK) return rc;
-    const dim3 up((unsigned)(q4_padded(g.F) / 16), (unsigned)g.pairs);
-    const auto sums = [&](int nt) { return (size_t)g.ways * 2 * nt * TPT * 16 * 4; };
-    if (g.T <= TPT) hipLaunchKernelGGL((moe_up_kernel<XT, 1, GL>), up, dim3(64 * g.ways), sums(1), st, g);
-    else hipLaunchKernelGGL((moe_up_kernel<XT, 2, GL>), up, dim3(64 * g.ways), sums(2), st, g);
-    rc = hip_status(hipGetLastError());
-    if (rc != BS_OK) return rc;
-    hipLaunchKernelGGL((moe_down_kernel<XT, GL>), dim3((unsigned)((g.D + 15) / 16)), dim3(64 * kDownWaves), lds, st, g);
-    return hip_status(hipGetLastError());
+    const size_t small = down_small(g.T, g.pairs), h = (size_t)g.pairs * Hidden<XT>::kParts * (g.part_chunks * kQ4Chunk + 8) * 2;
+    return h <= kLdsOfH ? launch_down<XT, GL, true>(g, small + h, st) : launch_down<XT, GL, false>(g, small, st);
 }
 
 template <typename XT>
@@ -308,31 +507,66 @@ int launch_group(const MoeArgs& g, int group, hipStream_t st) {
     }
 }
 
-size_t x_bytes(int dtype, int64_t T, int64_t D) { return (size_t)T * (dtype == BS_F32 ? 3 : 1) * row_pitch(D) * 2; }
+// the workspace: x's rows, h's rows, logits, sums of down's workgroups, their counts
+struct Space {
+    size_t h, logits, leaders, parts, done, all;
+    int split, part_chunks;
+};
+
+Space space_for(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
+    Space s;
+    // Workgroups of a tile of outputs: as many as let h of a part of F fit LDS, or give the chip four each, and no fewer steps
+    // than wavefronts for each.
+    const int64_t tiles = (D + 15) / 16, chunks = q4_padded(F) / kQ4Chunk, pairs = T * top_k, experts = pairs < E ? pairs : E;
+    const int parts = dtype == BS_F32 ? 3 : 2;
+    s.split = 1;
+    s.part_chunks = (int)chunks;
+    while (s.split < 16 && s.part_chunks > 2) {
+        const bool fits = pairs * parts * (s.part_chunks * kQ4Chunk + 8) * 2 <= (int64_t)kLdsOfH;
+        const int64_t steps = (s.part_chunks + 1) / 2 * experts;
+        if (fits && (tiles * s.split >= 512 || steps < 4 * kDownWaves)) break;
+        s.split *= 2;
+        s.part_chunks = (int)((chunks + s.split - 1) / s.split + 1) / 2 * 2;
+    }
+    s.split = (int)((chunks + s.part_chunks - 1) / s.part_chunks);
+    const auto up16 = [](size_t n) { return (n + 15) / 16 * 16; };
+    s.h = (size_t)T * (dtype == BS_F32 ? 3 : 1) * row_pitch(D) * 2;
+    s.logits = s.h + (size_t)pairs * parts * row_pitch(F) * 2;
+    s.leaders = s.logits + up16((size_t)T * E * 4);
+    s.parts = s.leaders + up16((size_t)(pairs + 1) * 4);
+    s.done = s.parts + (s.split > 1 ? (size_t)tiles * s.split * T * 64 : 0);
+    s.all = s.done + (s.split > 1 ? (size_t)tiles * 4 : 0);
+    return s;
+}
 
 }  // namespace
 
-size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int top_k) {
-    return x_bytes(dtype, T, D) + (size_t)T * top_k * (dtype == BS_F32 ? 3 : 2) * row_pitch(F) * 2;
-}
+size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) { return space_for(dtype, T, D, F, E, top_k).all; }
 
 int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,
                   const uint16_t* s1, const uint8_t* w2, const uint16_t* s2, int64_t F, int group, int top_k, int renormalise, void* y,
                   int64_t ldy, int32_t* ids, float* weights, void* workspace, size_t workspace_bytes, hipStream_t st) {
-    if (!workspace || workspace_bytes < q4_moe_workspace_bytes(dtype, T, D, F, top_k) || (reinterpret_cast<uintptr_t>(workspace) & 15))
+    const Space s = space_for(dtype, T, D, F, E, top_k);
+    if (!workspace || workspace_bytes < s.all || (reinterpret_cast<uintptr_t>(workspace) & 15))
         return BS_ERR_WORKSPACE;
     MoeArgs g{};
     g.x = x; g.router = router; g.ldx = ldx; g.ldy = ldy;
     g.T = (int)T; g.D = (int)D; g.E = E; g.F = (int)F; g.top_k = top_k; g.pairs = (int)T * top_k;
     g.renormalise = renormalise != 0;
-    const int size = dtype_bytes(dtype);
-    g.whole_x = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (T == 1 || ldx * size % 16 == 0);
-    g.whole_router = (reinterpret_cast<uintptr_t>(router) & 15) == 0 && D * size % 16 == 0;
     g.w1 = w1; g.w2 = w2; g.s1 = s1; g.s2 = s2; g.y = y; g.ids = ids; g.weights = weights;
-    g.xp = static_cast<uint16_t*>(workspace);
-    g.hp = g.xp + x_bytes(dtype, T, D) / 2;
-    const int64_t steps = (q4_padded(D) / kQ4Chunk + kU - 1) / kU;
-    g.ways = (int)(steps < 8 ? steps : 8);
+    char* const base = static_cast<char*>(workspace);
+    g.xp = reinterpret_cast<uint16_t*>(base);
+    g.hp = reinterpret_cast<uint16_t*>(base + s.h);
+    g.logits = reinterpret_cast<float*>(base + s.logits);
+    g.parts = reinterpret_cast<float*>(base + s.parts);
+    g.done = reinterpret_cast<uint32_t*>(base + s.done);
+    g.split = s.split;
+    g.part_chunks = s.part_chunks;
+    g.leaders = reinterpret_cast<int32_t*>(base + s.leaders);
+    g.magic_x = magic_u32((uint32_t)(q4_padded(D) / 8));
+    g.magic_h = magic_u32((uint32_t)(s.part_chunks * (kQ4Chunk / 8)));
+    const int64_t steps = (q4_padded(D) / kQ4Chunk + 1) / 2;
+    g.ways = (int)(steps < 4 ? steps : 4);
     switch (dtype) {
         case BS_F32: return launch_group<F32>(g, group, st);
         case BS_F16: return launch_group<F16>(g, group, st);

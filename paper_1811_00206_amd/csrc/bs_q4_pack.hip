@@ -29,14 +29,14 @@ __device__ __forceinline__ void piece_of(uint32_t pieces, uint32_t magic, int64_
 }
 
 template <typename XT, int GL>
-__global__ __launch_bounds__(256) void q4_pack_kernel(const typename XT::type* W, int64_t M, int64_t K, bool whole, uint32_t pieces,
+__global__ __launch_bounds__(256) void q4_pack_kernel(const typename XT::type* W, int64_t M, int64_t K, uint32_t pieces,
                                                       uint32_t magic, uint8_t* codes, uint16_t* scales) {
     int64_t row;
     uint32_t piece;
     piece_of(pieces, magic, row, piece);
     float v[8] = {};
     const int64_t k = (int64_t)piece * 8;
-    if (row < M) load8<XT>(W + row * K, k, K, whole, v);
+    if (row < M) load8<XT>(W + row * K, k, K, v);
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const typename XT::type* W
 }
 
 template <typename XT, int GL>
-__global__ __launch_bounds__(256) void q4_unpack_kernel(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t K, bool whole,
+__global__ __launch_bounds__(256) void q4_unpack_kernel(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t K,
                                                         uint32_t pieces, uint32_t magic, typename XT::type* W) {
     int64_t row;
     uint32_t piece;
@@ -80,13 +80,8 @@ __global__ __launch_bounds__(256) void q4_unpack_kernel(const uint8_t* codes, co
 #pragma unroll
     for (int i = 0; i < 8; ++i) out[i] = XT::store(p[i / 2][i % 2] * s);
     typename XT::type* to = W + row * K + k;
-    if (whole && k + 8 <= K) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(out) / 16; ++i) {
-            uint4 w;
-            __builtin_memcpy(&w, reinterpret_cast<const char*>(out) + 16 * i, 16);
-            reinterpret_cast<uint4*>(to)[i] = w;
-        }
+    if (k + 8 <= K) {
+        __builtin_memcpy(to, out, sizeof(out));      // wherever the row starts
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -99,7 +94,6 @@ int launch(const void* W, int64_t M, int64_t K, uint8_t* codes, uint16_t* scales
     const int group = 32 << GL;
     const uint32_t pieces = (uint32_t)(q4_groups(K, group) * (group / 8));
     using T = typename XT::type;
-    const bool whole = K * sizeof(T) % 16 == 0;
     const int64_t most = ((int64_t)1 << 31) / pieces;      // rows of a launch: a grid has fewer than 2^32 lanes
     for (int64_t r = 0; r < M; r += most) {
         const int64_t rows = M - r < most ? M - r : most;
@@ -107,11 +101,11 @@ int launch(const void* W, int64_t M, int64_t K, uint8_t* codes, uint16_t* scales
         uint8_t* const c = codes + r * q4_row_bytes(K);
         uint16_t* const s = scales + r * q4_groups(K, group);
         if (out)
-            hipLaunchKernelGGL((q4_unpack_kernel<XT, GL>), grid, dim3(256), 0, st, c, s, rows, K, whole, pieces, magic_u32(pieces),
+            hipLaunchKernelGGL((q4_unpack_kernel<XT, GL>), grid, dim3(256), 0, st, c, s, rows, K, pieces, magic_u32(pieces),
                                static_cast<T*>(out) + r * K);
         else
-            hipLaunchKernelGGL((q4_pack_kernel<XT, GL>), grid, dim3(256), 0, st, static_cast<const T*>(W) + r * K, rows, K, whole,
-                               pieces, magic_u32(pieces), c, s);
+            hipLaunchKernelGGL((q4_pack_kernel<XT, GL>), grid, dim3(256), 0, st, static_cast<const T*>(W) + r * K, rows, K, pieces,
+                               magic_u32(pieces), c, s);
         const int rc = hip_status(hipGetLastError());
         if (rc != BS_OK) return rc;
     }
