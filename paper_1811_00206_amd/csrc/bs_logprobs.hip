@@ -9,8 +9,8 @@
 // so.  Where m L could overflow (masks of the lowest fp32 or bfloat16 value that leave nothing) u = (x - m) L and
 // lse = m + log s: such rows are uniform, and come out so.
 //
-// The n largest: each of the four wavefronts finds the ceil(n / 4)-th largest of its lanes' largest, and at least n elements
-// reach the least of those, the bound; few others do.  While the statistics are made a thread only keeps, in LDS, the
+// The n largest: each of the four wavefronts finds the k-th largest of its lanes' largest, k being its share of n (a quarter,
+// where all lanes have words), and at least n elements reach the least of those, the bound; few others do.  While the statistics are made a thread only keeps, in LDS, the
 // largest of every eight elements; the eights that reach the bound are listed and loaded once more, each by a thread of its
 // own, and their elements that reach it are ordered by counting, for every one, those before it.  They are 64-bit keys
 // (value, then index), all different, so the order in which threads reach a list does not matter.  Rows that flood the lists
@@ -159,10 +159,22 @@ __device__ __forceinline__ float kth_largest(float v, int k) {
     return most;
 }
 
-// The list flooded.  First what is larger than the bound; if that is too many too, the n largest one after the other.
-// Then, where the list is short, the first elements of the row that are not larger than `fill`.
+// how many of the list's keys are not below `least`; all threads
+__device__ __forceinline__ int keys_from(TopList& l, const uint64_t* keys, int count, uint64_t least) {
+    int n = 0;
+    for (int i = threadIdx.x; i < (count + 63) / 64 * 64; i += kThreads) n += __popcll(__ballot(i < count && keys[i] >= least));
+    if ((threadIdx.x & 63) == 0) l.wave_count[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = 0;
+    for (int w = 0; w < kWaves; ++w) n += l.wave_count[w];
+    __syncthreads();
+    return n;
+}
+
+// The list flooded.  First what is larger than the bound, into the room of the eights' largest (`most` keys), out of which the
+// n-th largest key is found bit by bit; if that is too many too, the n largest one after the other.
 template <typename XT>
-__device__ void flooded(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, float bound, int n) {
+__device__ void flooded(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, float bound, int n, uint64_t* keys, int most) {
     constexpr int E = Row<XT>::E;
     __syncthreads();
     if (threadIdx.x == 0) l.count = 0;
@@ -173,13 +185,23 @@ __device__ void flooded(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, 
         for (int i = 0; i < E; ++i)
             if (x[i] > bound) {
                 const int at = atomicAdd(&l.count, 1);
-                if (at < kList) l.keys[at] = order_key(x[i], (uint32_t)(v * E - row.head + i));
+                if (at < most) keys[at] = order_key(x[i], (uint32_t)(v * E - row.head + i));
             }
     }
     __syncthreads();
     const int count = l.count;
-    if (count <= kList) {
-        order_list(l, count, n);
+    if (count <= most) {
+        uint64_t least = 0;
+        if (count > n)
+            for (int bit = 63; bit >= 0; --bit)
+                if (keys_from(l, keys, count, least | (uint64_t)1 << bit) >= n) least |= (uint64_t)1 << bit;
+        __syncthreads();
+        if (threadIdx.x == 0) l.count = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < count; i += kThreads)
+            if (keys[i] >= least) l.keys[atomicAdd(&l.count, 1)] = keys[i];      // n at most: keys are different
+        __syncthreads();
+        order_list(l, min(count, n), n);
         return;
     }
     uint64_t last = ~(uint64_t)0;
@@ -352,8 +374,15 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Args g) {
     }
     float bound = 0.f;
     if constexpr (TOP) {
-        const float k = kth_largest(st.m, (g.n + kWaves - 1) / kWaves);
-        if (lane == 0) l.bound[wave] = k;
+        const int with_words = __popcll(__ballot(st.m > -__builtin_inff()));
+        if (lane == 0) l.wave_count[wave] = with_words;
+        __syncthreads();
+        // of the n, every wavefront answers for its share of the lanes that have words
+        int mine = l.wave_count[wave], lanes = 0;
+        for (int w = 0; w < kWaves; ++w) lanes += l.wave_count[w];
+        const int k = lanes < g.n ? -1 : (g.n * mine + lanes - 1) / lanes;
+        const float bound_here = k < 0 ? -__builtin_inff() : k ? kth_largest(st.m, k) : __builtin_inff();
+        if (lane == 0) l.bound[wave] = bound_here;
     }
     st = join_wave(st);
     if (lane == 0) stats[wave] = st;
@@ -394,7 +423,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Args g) {
         }
         __syncthreads();
         const int count = l.count;
-        if (eights > kEights || count > kList) flooded(l, row, v0, v1, bound, g.n);
+        if (eights > kEights || count > kList)
+            flooded(l, row, v0, v1, bound, g.n, reinterpret_cast<uint64_t*>(largest), (batches + g.sharing - 1) / g.sharing * (kThreads * 2));
         else order_list(l, count, g.n);
         // a slice can have fewer words than n that are larger than its bound
         if (!l.sorted[g.n - 1]) fill(l, row, v0, v1, bound, g.n);

@@ -104,6 +104,19 @@ def test_rows_that_flood_the_list(V, dtype):
         check(x, targets, n)
 
 
+@pytest.mark.parametrize("V,n", [(64, 64), (300, 64), (1483, 43), (2049, 64), (9000, 64), (70000, 50)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_words_that_lie_together(V, n, dtype):
+    """Few words that a mask leaves in a row, fewer threads than n that have any, and short rows."""
+    x, targets = rows(5, V, dtype, V + n)
+    for i, left in enumerate((V, 600, 420, 65, 9)):
+        first = (V - left) // 3 if left < V else 0
+        x[i, :first] = -INF
+        x[i, first + left:] = -INF
+        targets[i] = max(0, first)
+    check(x, targets, n)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_rows_of_a_wider_tensor(dtype):
     """Rows that start anywhere between the boundaries of loads; what lies beside them is not looked at."""
