@@ -225,6 +225,65 @@ def test_gradient_in_place_and_of_empty_rows():
         assert not bool(grad.any())
 
 
+@pytest.mark.parametrize("dtype,shift", [("f32", 5e4), ("f32", -1e9), ("f32", 1e20), ("f16", -65504.0), ("bf16", -1e9), ("bf16", 3e4)])
+def test_gradient_of_rows_whose_lse_is_large(dtype, shift):
+    """lse as it is rounded says little of the differences there.  Half of the words are at the shift or a few above, the others
+    far below; against the softmax in 64 bits of the logits as they are."""
+    V = 9000
+    x = torch.full((3, V), shift, device="cuda")
+    x[1, ::2] = -INF
+    x[2, 5:40] = shift + abs(shift) / 64
+    x = x.to(TYPES[dtype])
+    targets = torch.tensor([3, 1, 7]).cuda()
+    gl, gh = torch.tensor([0.5, -1.0, 2.0]), torch.tensor([0.25, 1.0, -0.5])
+    _, entropy, lse, _, _ = bs.bs_logprobs(x, targets)
+    got = bs.bs_logprobs_backward(x, targets, lse, entropy, gl.cuda(), gh.cuda()).cpu().double()
+    room = x.clone()
+    assert torch.equal(bs.bs_logprobs_backward(room, targets, lse, entropy, gl.cuda(), gh.cuda(), out=room).cpu().double(), got)
+    logp = torch.log_softmax(x.cpu().double(), -1)
+    p = logp.exp()
+    H = torch.special.entr(p).sum(-1, keepdim=True)
+    want = -p * gl.double().unsqueeze(-1) - gh.double().unsqueeze(-1) * torch.where(p > 0, p * (logp + H), torch.zeros_like(p))
+    want[torch.arange(3), targets.cpu()] += gl.double()
+    # entropy and log p are each off by 1e-5 of what they are; then the result's own rounding
+    allowed = p * 1e-5 * (gl.abs().unsqueeze(-1) + gh.abs().unsqueeze(-1) * (2 + 2 * H + torch.where(p > 0, logp.abs(), torch.zeros_like(p))))
+    allowed = allowed + ROUNDING[TYPES[dtype]] * want.abs() * 1.001 + 2.0**-23 * gl.abs().unsqueeze(-1) + (2.0**-25 if dtype == "f16" else 2.0**-126)
+    off = (got - want).abs()
+    assert bool((off <= allowed).all()), float((off / allowed).max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [700, 9000, 70000])
+def test_rows_of_large_logits(V, dtype):
+    """Rows that lie far from 0, words of which are masked with what is large only, and rows across 2^20, where sums are made
+    in another way.  An entropy and a log probability do not depend on where the row lies."""
+    g = torch.Generator().manual_seed(V)
+    rows_ = []
+    for at in (-1e9, -1e10, 1e12, -1e30, 2.0**20 - 3, -(2.0**20), 3e6, 1e4):
+        x = torch.randint(-8, 9, (V,), generator=g).double()
+        step = max(1.0, abs(at) * 2.0**-7 if dtype == "bf16" else abs(at) * 2.0**-23)
+        rows_.append((at + x * step).to(TYPES[dtype]))
+    some = torch.full((V,), -1e9)
+    some[::97] = torch.randn(some[::97].shape, generator=g)
+    rows_.append(some.to(TYPES[dtype]))
+    x = torch.stack(rows_).cuda()
+    targets = torch.randint(0, V, (len(rows_),), generator=g).cuda()
+    targets[-1] = 97
+    got = check(x, targets, 9)
+    logprob, entropy, _, values, _, _ = definition(x, targets, 9)
+    near(got[0], logprob, 1e-5 * (1 + logprob.abs()))
+    near(got[1], entropy, 1e-5 * (2 + entropy))
+    near(got[3], values, 1e-5 * (1 + values.abs()))
+
+
+def test_gradient_of_a_target_that_is_none():
+    x, targets = rows(3, 500, "f32", 9)
+    targets[1] = 500
+    _, entropy, lse, _, _ = bs.bs_logprobs(x, targets)
+    got = bs.bs_logprobs_backward(x, targets, lse, entropy, torch.ones(3).cuda(), torch.ones(3).cuda())
+    assert bool(torch.isnan(got[1]).all()) and bool(torch.isfinite(got[[0, 2]]).all())
+
+
 def test_graph_replays():
     x, targets = rows(2, 50000, "f32", 3)
     bs.bs_init()
