@@ -342,8 +342,8 @@ int bs_lstm_sequence_plan(int dtype, int64_t H, int64_t I, int bank, int k, int 
  * magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6.  Element k of a row is in byte k / 2, in the low half
  * for even k.  A row takes 16 * ceil(K / 32) bytes, codes behind K are 0.  A group of `group`
  * (32, 64 or 128) consecutive elements of a row has one binary16 scale, [M][ceil(K / group)]:
- * a code stands for its number times its group's scale.  M, K <= 2^24.  Codes must be 16-byte
- * aligned, scales 4-byte; other pointers only as their type asks.
+ * a code stands for its number times its group's scale.  M, K <= 2^24.  Codes and workspaces must
+ * be 16-byte aligned; all other pointers of this section only as their type asks.
  */
 size_t bs_q4_codes_bytes(int64_t M, int64_t K);                /* 0 if the shape is invalid */
 size_t bs_q4_scales_bytes(int64_t M, int64_t K, int group);
@@ -379,10 +379,10 @@ int bs_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t 
  * w1, s1   DEVICE in   E 4-bit matrices of 2F x D: the rows of G_e, then those of U_e
  * w2, s2   DEVICE in   E 4-bit matrices of D x F
  * ids      DEVICE out  T x top_k chosen experts, largest weight first     weights  DEVICE out  their p, fp32
- * T <= BS_MOE_TOKENS_MAX, E <= BS_MOE_EXPERTS_MAX, top_k <= min(E, BS_MOE_TOP_K_MAX).
+ * T <= BS_MOE_TOKENS_MAX, which pass 64 by 64; E <= BS_MOE_EXPERTS_MAX, top_k <= min(E, BS_MOE_TOP_K_MAX).
  * workspace: bs_q4_moe_workspace_bytes(...) bytes, 16-byte aligned, as for bs_spmm.
  */
-#define BS_MOE_TOKENS_MAX 64
+#define BS_MOE_TOKENS_MAX 65536
 #define BS_MOE_EXPERTS_MAX 1024
 #define BS_MOE_TOP_K_MAX 32
 size_t bs_q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k, int group);
@@ -413,7 +413,7 @@ int bs_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
  * lse, entropy  DEVICE in   as bs_logprobs gave them          g_logprob, g_entropy  DEVICE in  T fp32 each
  * grad          DEVICE out  T rows of V, same type as the logits, ldg >= V apart; may be the logits themselves
  * entropy and g_entropy may both be NULL: the log probability's gradient alone.  A row without a target has that of its
- * entropy alone; a row in which nothing is left (lse <= -1e30: all words -inf, or all the lowest fp32 / bfloat16 number) 0.
+ * entropy alone, one with a target that is not below V NaN; a row in which nothing is left (lse <= -1e30: all words -inf, or all the lowest fp32 / bfloat16 number) 0.
  */
 int bs_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets,
                          const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,

@@ -703,15 +703,14 @@ def bs_q4_pack(W, group: int = 64):
 
 def bs_q4_unpack(codes, scales, K: int, group: int = 64, dtype=torch.float32, out=None):
     """The values [.., M, K] that a 4-bit matrix stands for, rounded to dtype (of `out`, if it is given)."""
-    if out is None and isinstance(codes, torch.Tensor):
-        if dtype not in _TYPES:
-            raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
-        _codes(codes, scales, K, group)
-        out = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
-    done = (_native or _calls()).q4_unpack(codes, scales, K, group, out)
+    done = (_native or _calls()).q4_unpack(codes, scales, K, group, _TYPES.get(dtype), out)
     if done is not None:
         return done
     M = _codes(codes, scales, K, group)
+    if out is None:
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+        out = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
     code = _type_code(_dev(out, "out"), "out")
     if out.numel() != M * K:
         raise ValueError(f"out must be {[*codes.shape[:-1], K]}")

@@ -417,20 +417,29 @@ PyObject* q4_pack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// (codes, scales, K, group, out) -> out
+// (codes, scales, K, group, dtype code, out) -> W
 PyObject* q4_unpack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    int group, K;
+    int group, K, dtype;
     Q4 w;
-    if (n != 5 || !int_arg(args[2], K) || !group_arg(args[3], group) || !w.read(args[0], args[1], K, group)) Py_RETURN_NONE;
-    const at::Tensor* out = gpu_tensor(args[4]);
-    if (!out || !out->is_contiguous() || out->numel() != w.M * K) Py_RETURN_NONE;
-    const int dtype = any_dtype(*out);
-    if (dtype < 0) Py_RETURN_NONE;
-    const int status = enqueue([&](void* st) { return bs_q4_unpack(w.c(), w.s(), w.M, K, group, out->mutable_data_ptr(), dtype, st); });
+    if (n != 6 || !int_arg(args[2], K) || !group_arg(args[3], group) || !w.read(args[0], args[1], K, group)) Py_RETURN_NONE;
+    at::Tensor W;
+    const at::Tensor* out = &W;
+    if (args[5] != Py_None) {
+        if (!(out = gpu_tensor(args[5])) || !out->is_contiguous() || out->numel() != w.M * K || (dtype = any_dtype(*out)) < 0) Py_RETURN_NONE;
+    } else if (!int_arg(args[4], dtype)) {
+        Py_RETURN_NONE;
+    }
+    const int status = enqueue([&](void* st) {
+        if (out == &W) {
+            at::DimVector size(w.codes->sizes());
+            size.back() = K;
+            W = at::empty(size, w.codes->options().dtype(dtype == BS_F32 ? at::kFloat : dtype == BS_F16 ? at::kHalf : at::kBFloat16));
+        }
+        return bs_q4_unpack(w.c(), w.s(), w.M, K, group, out->mutable_data_ptr(), dtype, st);
+    });
     if (status != BS_OK) return failed(self, status, "bs_q4_unpack");
-    Py_INCREF(args[4]);
-    return args[4];
+    return result(args[5], W);
     END_HANDLE_TH_ERRORS
 }
 

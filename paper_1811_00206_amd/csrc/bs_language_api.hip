@@ -14,7 +14,7 @@ int check_codes(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t
     if (!codes || !scales) return BS_ERR_NULL;
     if (!matrix_ok(M, K)) return BS_ERR_SHAPE;
     if (!limits_ok(M, K, group)) return BS_ERR_UNSUPPORTED;
-    return aligned(codes, 16) && aligned(scales, 4) ? BS_OK : BS_ERR_ALIGN;
+    return aligned(codes, 16) && aligned(scales, 2) ? BS_OK : BS_ERR_ALIGN;
 }
 
 int check_logits(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets) {
@@ -45,7 +45,7 @@ int bs_q4_pack(const void* W, int dtype, int64_t M, int64_t K, int group, uint8_
     const int st = check_codes(codes, scales, M, K, group);
     if (st) return st;
     if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
-    if (!aligned(W, 16)) return BS_ERR_ALIGN;
+    if (!aligned(W, bs::dtype_bytes(dtype))) return BS_ERR_ALIGN;
     return bs::launch_q4_pack(W, dtype, M, K, group, codes, scales, nullptr, static_cast<hipStream_t>(stream));
 }
 
@@ -54,7 +54,7 @@ int bs_q4_unpack(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_
     const int st = check_codes(codes, scales, M, K, group);
     if (st) return st;
     if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
-    if (!aligned(W, 16)) return BS_ERR_ALIGN;
+    if (!aligned(W, bs::dtype_bytes(dtype))) return BS_ERR_ALIGN;
     return bs::launch_q4_pack(nullptr, dtype, M, K, group, const_cast<uint8_t*>(codes), const_cast<uint16_t*>(scales), W,
                               static_cast<hipStream_t>(stream));
 }
@@ -93,7 +93,7 @@ int bs_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const
         return BS_ERR_UNSUPPORTED;
     const size_t size = bs::dtype_bytes(dtype);
     if (!aligned(x, size) || !aligned(router, size) || !aligned(y, size) || !aligned(w1, 16) || !aligned(w2, 16) ||
-        !aligned4(s1, s2, ids, weights))
+        !aligned(s1, 2) || !aligned(s2, 2) || !aligned(ids, 4) || !aligned(weights, 4))
         return BS_ERR_ALIGN;
     return bs::launch_q4_moe(x, dtype, T, ldx, D, router, E, w1, s1, w2, s2, F, group, top_k, renormalise, y, ldy, ids, weights,
                              workspace, workspace_bytes, static_cast<hipStream_t>(stream));

@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kDownWaves = 8;
 constexpr size_t kLdsOfX = 40 * 1024, kLdsOfH = 64 * 1024;      // x and h are brought to LDS where they take no more
-constexpr int kMaxTokens = BS_MOE_TOKENS_MAX, kMaxExperts = BS_MOE_EXPERTS_MAX, kMaxTopK = BS_MOE_TOP_K_MAX;
+constexpr int kTokens = 64;      // that pass together; more pass 64 by 64
 
 // Elements between virtual rows in the workspace: whole chunks and a cache line, so that rows a power of two long do not
 // meet in the same sets of the caches.
@@ -466,8 +466,8 @@ int launch_up(MoeArgs g, hipStream_t st) {
     g.rows = g.T < TPT ? g.T : g.T < 2 * TPT ? g.T : 2 * TPT;
     const int small = up_small(g.T, g.pairs, g.E), sums = 2 * g.ways * g.tiles * g.rows * 64;
     const size_t lds_x = (size_t)g.rows * XT::kParts * (q4_padded(g.D) + 8) * 2;
-    // The logits by every workgroup itself where they are few (1 token, 8 experts, 1500 columns: 12.4 us in two kernels against
-    // 16.8 in three); 64 experts of 2048 columns would have each read 256 KB.
+    // The logits by every workgroup itself where they are few (1 token, 8 experts, 1500 columns: 14.7 us in two kernels against
+    // 18 in three); 64 experts of 2048 columns would have each read 256 KB.
     if (g.T <= TPT && lds_x <= kLdsOfX && (int64_t)g.T * g.E * g.D <= 32768 && g.T * g.E * 4 <= sums)
         return launch_up_rows<XT, GL, 1, true, true>(g, small + sums + lds_x, st);
     hipLaunchKernelGGL(moe_logits_kernel<XT>, dim3(g.T, (g.E + 15) / 16), dim3(256), 0, st, g);
@@ -515,8 +515,9 @@ struct Space {
 
 Space space_for(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
     Space s;
-    // Workgroups of a tile of outputs: as many as let h of a part of F fit LDS, or give the chip four each, and no fewer steps
-    // than wavefronts for each.
+    // Workgroups of a tile of outputs: as many as let h of a part of F fit LDS, and then as many as give every compute unit two
+    // (more where their wavefronts have four steps each).  7 tokens of 2048 x 1024, 64 experts, 6 of them each: `down` 14.8 us with
+    // four workgroups a tile, 34 with one.
     const int64_t tiles = (D + 15) / 16, chunks = q4_padded(F) / kQ4Chunk, pairs = T * top_k, experts = pairs < E ? pairs : E;
     const int parts = dtype == BS_F32 ? 3 : 2;
     s.split = 1;
@@ -541,14 +542,19 @@ Space space_for(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
 
 }  // namespace
 
-size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) { return space_for(dtype, T, D, F, E, top_k).all; }
+size_t q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
+    const size_t rest = T % kTokens ? space_for(dtype, T % kTokens, D, F, E, top_k).all : 0;
+    if (T < kTokens) return rest;
+    const size_t whole = space_for(dtype, kTokens, D, F, E, top_k).all;
+    return whole > rest ? whole : rest;
+}
 
-int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,
+namespace {
+
+int launch_tokens(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,
                   const uint16_t* s1, const uint8_t* w2, const uint16_t* s2, int64_t F, int group, int top_k, int renormalise, void* y,
-                  int64_t ldy, int32_t* ids, float* weights, void* workspace, size_t workspace_bytes, hipStream_t st) {
+                  int64_t ldy, int32_t* ids, float* weights, void* workspace, hipStream_t st) {
     const Space s = space_for(dtype, T, D, F, E, top_k);
-    if (!workspace || workspace_bytes < s.all || (reinterpret_cast<uintptr_t>(workspace) & 15))
-        return BS_ERR_WORKSPACE;
     MoeArgs g{};
     g.x = x; g.router = router; g.ldx = ldx; g.ldy = ldy;
     g.T = (int)T; g.D = (int)D; g.E = E; g.F = (int)F; g.top_k = top_k; g.pairs = (int)T * top_k;
@@ -572,6 +578,23 @@ int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, c
         case BS_F16: return launch_group<F16>(g, group, st);
         default: return launch_group<BF16>(g, group, st);
     }
+}
+
+}  // namespace
+
+int launch_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const void* router, int E, const uint8_t* w1,
+                  const uint16_t* s1, const uint8_t* w2, const uint16_t* s2, int64_t F, int group, int top_k, int renormalise, void* y,
+                  int64_t ldy, int32_t* ids, float* weights, void* workspace, size_t workspace_bytes, hipStream_t st) {
+    if (!workspace || workspace_bytes < q4_moe_workspace_bytes(dtype, T, D, F, E, top_k) || (reinterpret_cast<uintptr_t>(workspace) & 15))
+        return BS_ERR_WORKSPACE;
+    const int64_t size = dtype_bytes(dtype);
+    for (int64_t t = 0; t < T; t += kTokens) {
+        const int rc = launch_tokens(static_cast<const char*>(x) + t * ldx * size, dtype, T - t < kTokens ? T - t : kTokens, ldx, D, router,
+                                     E, w1, s1, w2, s2, F, group, top_k, renormalise, static_cast<char*>(y) + t * ldy * size, ldy,
+                                     ids + t * top_k, weights + t * top_k, workspace, st);
+        if (rc != BS_OK) return rc;
+    }
+    return BS_OK;
 }
 
 }  // namespace bs

@@ -73,7 +73,7 @@ def check(got, want, dtype):
 @pytest.mark.parametrize("T,D,F,E,top_k,group,renormalise", [
     (1, 1, 1, 1, 1, 32, True), (1, 64, 32, 4, 2, 32, False), (3, 100, 75, 5, 3, 64, True), (1, 1500, 300, 8, 2, 32, True),
     (5, 129, 257, 3, 3, 128, False), (16, 96, 64, 60, 8, 32, True), (17, 160, 48, 4, 1, 64, False), (9, 256, 130, 300, 4, 128, True),
-    (64, 70, 40, 6, 5, 32, True), (40, 48, 33, 40, 32, 64, False)])
+    (64, 70, 40, 6, 5, 32, True), (40, 48, 33, 40, 32, 64, False), (65, 72, 40, 6, 2, 32, True), (201, 64, 48, 20, 3, 64, False)])
 def test_layer(T, D, F, E, top_k, group, renormalise, dtype):
     p = layer(T, D, F, E, group, dtype, T + D + F)
     got = call(p, top_k, renormalise)
@@ -143,7 +143,7 @@ def test_refusals():
     args = lambda **k: {**dict(x=x, router=r, w1=p["c1"], s1=p["s1"], w2=p["c2"], s2=p["s2"], group=32, top_k=2), **k}
     for change, error, status in (
             (dict(top_k=0), bs.BsError, 2), (dict(top_k=5), bs.BsError, 2), (dict(x=x[:0]), bs.BsError, 1),
-            (dict(x=torch.zeros((65, 64), device="cuda")), bs.BsError, 3), (dict(x=x.half()), TypeError, None),
+            (dict(x=torch.zeros((65537, 64), device="cuda")), bs.BsError, 3), (dict(x=x.half()), TypeError, None),
             (dict(x=x[:, :60]), ValueError, None), (dict(router=r[:3]), ValueError, None), (dict(w1=p["c1"][:, 1:].contiguous()), ValueError, None),
             (dict(w2=p["c1"]), ValueError, None), (dict(group=16), ValueError, None), (dict(x=x.cpu()), TypeError, None),
             (dict(workspace=torch.zeros(16, dtype=torch.uint8, device="cuda")), bs.BsError, 6)):

@@ -195,6 +195,30 @@ def test_gemv_on_another_stream_and_in_a_graph():
         assert torch.equal(out, eager)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_matrices_that_start_anywhere(dtype):
+    """W and scales are only as aligned as their types; what lies beside an unpacked matrix stays."""
+    M, K, group = 7, 99, 32
+    g = torch.Generator().manual_seed(3)
+    W = torch.randn((M, K), generator=g).to(TYPES[dtype]).cuda()
+    codes, scales = bs.bs_q4_pack(W, group)
+    want = bs.bs_q4_unpack(codes, scales, K, group, dtype=TYPES[dtype])
+    x = torch.randn((1, K), generator=g).to(TYPES[dtype]).cuda()
+    for first in (1, 2, 3, 5):
+        room = torch.zeros(M * K + 8, dtype=W.dtype, device="cuda")
+        room[first:first + M * K] = W.flatten()
+        c, s = bs.bs_q4_pack(room[first:first + M * K].view(M, K), group)
+        assert torch.equal(c, codes) and torch.equal(s, scales)
+        wide = torch.zeros(scales.numel() + 8, dtype=torch.float16, device="cuda")
+        wide[first:first + scales.numel()] = scales.flatten()
+        s = wide[first:first + scales.numel()].view(scales.shape)
+        room.fill_(3.0)
+        out = bs.bs_q4_unpack(codes, s, K, group, out=room[first:first + M * K].view(M, K))
+        assert torch.equal(out, want)
+        assert bool((room[:first] == 3).all()) and bool((room[first + M * K:] == 3).all())
+        assert torch.equal(bs.bs_q4_gemv(codes, s, group, x), bs.bs_q4_gemv(codes, scales, group, x))
+
+
 def test_refusals():
     codes, scales, _ = packed(8, 64, 32, 1)
     x = torch.zeros((2, 64), device="cuda")
