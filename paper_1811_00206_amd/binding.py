@@ -639,6 +639,7 @@ def bs_reprune(vals, idx, bank: int, k2: int, out=None):
 
 # ---- language models: 4-bit matrices, expert layers, log probabilities
 
+MOE_TOKENS_MAX, MOE_TOP_K_MAX, LOGPROBS_TOP_MAX = 65536, 32, 64      # as in bs.h
 _TYPES = {torch.float32: BS_F32, torch.float16: BS_F16, torch.bfloat16: BS_BF16}
 
 
@@ -737,12 +738,12 @@ def bs_q4_gemv(codes, scales, group: int, x, out=None, workspace=None):
     M = _codes(codes, scales, K, group)
     if codes.dim() != 2:
         raise ValueError("codes must be [M, ..]")
-    y = torch.empty((*x.shape[:-1], M), dtype=x.dtype, device=x.device) if out is None else out
-    if not isinstance(y, torch.Tensor) or tuple(y.shape) != (*x.shape[:-1], M):
+    if out is not None and (not isinstance(out, torch.Tensor) or tuple(out.shape) != (*x.shape[:-1], M)):
         raise ValueError(f"out must be {[*x.shape[:-1], M]}")
-    ldy = _rows(y if x.dim() == 2 else _dev(y, "out").unsqueeze(0), "out", x.dtype)
     lib = load_library()
     workspace, ws_bytes = _own_workspace(workspace, lib.bs_q4_gemv_workspace_bytes(code, M, K, group, N), x.device)
+    y = torch.empty((*x.shape[:-1], M), dtype=x.dtype, device=x.device) if out is None else out
+    ldy = _rows(y if x.dim() == 2 else _dev(y, "out").unsqueeze(0), "out", x.dtype)
     _check(lib.bs_q4_gemv(_ptr(codes), _ptr(scales), M, K, group, _ptr(x), code, N, ldx, _ptr(y), ldy, _ptr(workspace), ws_bytes,
                           _stream()), "bs_q4_gemv")
     return y
@@ -753,7 +754,7 @@ def bs_q4_moe_workspace_bytes(dtype: int, T: int, D: int, F: int, E: int, top_k:
 
 
 def bs_q4_moe(x, router, w1, s1, w2, s2, group: int, top_k: int, renormalise: bool = True, workspace=None):
-    """A mixture-of-experts layer for a few tokens: x [T, D] -> (y [T, D], ids int32 [T, top_k], weights float32
+    """A mixture-of-experts layer, made for few tokens (64 pass together): x [T, D] -> (y [T, D], ids int32 [T, top_k], weights float32
     [T, top_k]).  router [E, D] has x's type; w1, s1 are the experts' 4-bit gate and up matrices [E, 2F, D] (gate rows
     first), w2, s2 their down matrices [E, D, F]."""
     done = (_native or _calls()).q4_moe(x, router, w1, s1, w2, s2, group, top_k, bool(renormalise), workspace)
@@ -773,13 +774,14 @@ def bs_q4_moe(x, router, w1, s1, w2, s2, group: int, top_k: int, renormalise: bo
     if w2.dim() != 3 or tuple(w2.shape[:2]) != (E, D):
         raise ValueError(f"w2 must be [{E}, {D}, ..]")
     top_k = int(top_k)
-    y = torch.empty((T, D), dtype=x.dtype, device=x.device)
-    ids = torch.empty((T, max(top_k, 0)), dtype=torch.int32, device=x.device)
-    weights = torch.empty((T, max(top_k, 0)), dtype=torch.float32, device=x.device)
     if top_k < 1:
         raise BsError(2, "bs_q4_moe")
     lib = load_library()
     workspace, ws_bytes = _own_workspace(workspace, lib.bs_q4_moe_workspace_bytes(code, T, D, F, E, top_k, group), x.device)
+    y = torch.empty((T, D), dtype=x.dtype, device=x.device)
+    width = min(top_k, MOE_TOP_K_MAX)      # more are refused
+    ids = torch.empty((T, width), dtype=torch.int32, device=x.device)
+    weights = torch.empty((T, width), dtype=torch.float32, device=x.device)
     _check(lib.bs_q4_moe(_ptr(x), code, T, ldx, D, _ptr(router), E, _ptr(w1), _ptr(s1), _ptr(w2), _ptr(s2), F, group, top_k,
                          int(bool(renormalise)), _ptr(y), D, _ptr(ids), _ptr(weights), _ptr(workspace), ws_bytes, _stream()), "bs_q4_moe")
     return y, ids, weights
@@ -808,11 +810,12 @@ def bs_logprobs(logits, targets, top_n: int = 0, workspace=None):
     top_n = int(top_n)
     if top_n < 0:
         raise BsError(2, "bs_logprobs")
-    logprob, entropy, lse = (torch.empty(T, dtype=torch.float32, device=logits.device) for _ in range(3))
-    values = torch.empty((T, top_n), dtype=torch.float32, device=logits.device)
-    ids = torch.empty((T, top_n), dtype=torch.int32, device=logits.device)
     lib = load_library()
     workspace, ws_bytes = _own_workspace(workspace, lib.bs_logprobs_workspace_bytes(code, T, V, top_n), logits.device)
+    logprob, entropy, lse = (torch.empty(T, dtype=torch.float32, device=logits.device) for _ in range(3))
+    width = min(top_n, LOGPROBS_TOP_MAX)      # more are refused
+    values = torch.empty((T, width), dtype=torch.float32, device=logits.device)
+    ids = torch.empty((T, width), dtype=torch.int32, device=logits.device)
     _check(lib.bs_logprobs(_ptr(logits), code, T, V, ld, _ptr(targets), top_n, _ptr(logprob), _ptr(entropy), _ptr(lse),
                            _ptr(values), _ptr(ids), _ptr(workspace), ws_bytes, _stream()), "bs_logprobs")
     return logprob, entropy, lse, values, ids

@@ -15,6 +15,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+
 #include "../../include/bs.h"
 
 namespace {
@@ -501,8 +503,9 @@ PyObject* q4_moe(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     const size_t need = bs_q4_moe_workspace_bytes(dtype, T, D, F, (int)E, top_k, group);
     const int status = enqueue([&](void* st) {
         out[0] = at::empty({T, D}, x->options());
-        out[1] = at::empty({T, top_k}, x->options().dtype(at::kInt));
-        out[2] = at::empty({T, top_k}, x->options().dtype(at::kFloat));
+        const int width = std::min(top_k, BS_MOE_TOP_K_MAX);      // more are refused
+        out[1] = at::empty({T, width}, x->options().dtype(at::kInt));
+        out[2] = at::empty({T, width}, x->options().dtype(at::kFloat));
         ws.allocate(need, *x);
         return bs_q4_moe(x->const_data_ptr(), dtype, T, ldx, D, router->const_data_ptr(), (int)E, w1.c(), w1.s(), w2.c(), w2.s(), F, group,
                          top_k, args[8] == Py_True, out[0].mutable_data_ptr(), D, static_cast<int32_t*>(out[1].mutable_data_ptr()),
@@ -542,8 +545,9 @@ PyObject* logprobs(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     const int status = enqueue([&](void* st) {
         const at::TensorOptions f = g.x->options().dtype(at::kFloat);
         for (int i = 0; i < 3; ++i) out[i] = at::empty({g.T}, f);
-        out[3] = at::empty({g.T, top}, f);
-        out[4] = at::empty({g.T, top}, f.dtype(at::kInt));
+        const int width = std::min(top, BS_LOGPROBS_TOP_MAX);      // more are refused
+        out[3] = at::empty({g.T, width}, f);
+        out[4] = at::empty({g.T, width}, f.dtype(at::kInt));
         ws.allocate(need, *g.x);
         float* p[4];
         for (int i = 0; i < 4; ++i) p[i] = static_cast<float*>(out[i].mutable_data_ptr());
