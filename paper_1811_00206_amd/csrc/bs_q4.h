@@ -397,6 +397,18 @@ __device__ __forceinline__ float max_of_wave(float v) {
 }
 __device__ __forceinline__ float sum_of_wave(float v) { return add_across_32(add_across_16(group_sum<16>(v))); }
 
+// Of `all` workgroups that have stored their sums with the scope of the whole GPU, by all threads: whether this one is the last,
+// and may load all of them with that scope.  Sums stored that way are where everybody sees them as soon as each lane has waited
+// for its own; a fence of that scope would write back all that the cache holds, which took 16 us.  `found`: a word of LDS.
+__device__ __forceinline__ bool last_of(uint32_t* done, int all, int* found) {
+    wait_vm_and_lds<0>();
+    pin_order();
+    __syncthreads();
+    if (threadIdx.x == 0) *found = (int)__hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return *found == all - 1;
+}
+
 // 64-bit whole numbers in the order of what is chosen first: the larger value, then the lower index.  -0 counts as 0, a value
 // that is no number comes last.  None of them is 0, none is the largest 64-bit number.
 __device__ __forceinline__ uint64_t order_key(float v, uint32_t index) {

@@ -15,6 +15,7 @@ namespace {
 
 constexpr size_t kSlabBytes = 64 * 1024;    // of x in LDS
 constexpr int kStagedRows = 4;              // virtual rows that are brought to LDS
+constexpr int kSplitMost = 16;              // workgroups that share K
 
 struct GemvArgs {
     const uint8_t* codes;
@@ -24,6 +25,9 @@ struct GemvArgs {
     void* y;
     int ways, tiles;    // wavefronts that share K; groups of wavefronts that share x in LDS
     int slab;           // columns of x in LDS at once
+    int split, part_chunks;      // workgroups that share K, and the chunks of each
+    float* parts;       // [tile of rows and tokens][split][its sums], if there are several
+    uint32_t* done;     // [tile]: those of them that are done
 };
 
 // a wavefront's sums to LDS: [wave][R][NT][TPT][16]
@@ -99,13 +103,14 @@ __global__ __launch_bounds__(1024) void q4_gemv_kernel(GemvArgs g) {
 template <typename XT, int NT, int R, int GL, bool TILED>
 __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(GemvArgs g) {
     using T = typename XT::type;
-    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S, U = 2;     // TPT: tokens per tile of virtual rows
+    constexpr int S = XT::kSlots, TPT = 16 / S, U = 2;     // TPT: tokens per tile of virtual rows
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row0 = (int64_t)blockIdx.x * (16 * R), n0 = (int64_t)blockIdx.y * (NT * TPT);
     const int tokens = (int)min(g.N - n0, (int64_t)(NT * TPT));
     const int chunks = (int)((g.K + kQ4Chunk - 1) / kQ4Chunk);
+    const int first = TILED ? blockIdx.z * g.part_chunks : 0, end = TILED ? min(chunks, first + g.part_chunks) : chunks;
     Q4Walk<XT::kHalf, NT, R, GL, U> walk;
 #pragma unroll
     for (int i = 0; i < R; ++i) walk.tile(i, g.codes, g.scales, row0 + 16 * i, g.M, g.K, lane);
@@ -116,7 +121,8 @@ __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(
         x.tile = (int64_t)chunks * 2048;
         x.at = static_cast<const uint16_t*>(g.x) + blockIdx.y * NT * x.tile + 8 * lane;
         x.last = chunks - 1;
-        walk.template walk<kFetch>(wave, g.ways, chunks, x, acc);
+        walk.load(first + wave * U);
+        walk.template rest<kFetch>(first + wave * U, g.ways, end, x, acc);
     } else {
         static_assert(S == 1);
         RowsOfX<NT, kFetch, true> x;
@@ -126,28 +132,48 @@ __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(
 #pragma unroll
         for (int t = 0; t < NT; ++t)
             x.at[t] = t * TPT + r < tokens ? static_cast<const uint16_t*>(g.x) + (n0 + t * TPT + r) * g.ldx : nullptr;
-        walk.template walk<kFetch>(wave, g.ways, chunks, x, acc);
+        walk.load(wave * U);
+        walk.template rest<kFetch>(wave * U, g.ways, end, x, acc);
     }
     float* sums = reinterpret_cast<float*>(lds);
     put_sums<S>(sums, wave, lane, acc);
     __syncthreads();
     constexpr int kOut = R * NT * TPT * 16;
+    const auto store = [&](int o, float sum) {
+        const int64_t row = row0 + o / (NT * TPT * 16) * 16 + o % 16;
+        static_cast<T*>(g.y)[(n0 + o / 16 % (NT * TPT)) * g.ldy + row] = XT::store(sum);
+    };
+    const auto wanted = [&](int o) { return o / 16 % (NT * TPT) < tokens && row0 + o / (NT * TPT * 16) * 16 + o % 16 < g.M; };
+    const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    float* parts = TILED ? g.parts + tile * g.split * kOut : nullptr;
     for (int o = threadIdx.x; o < kOut; o += blockDim.x) {
-        const int i = o / (NT * TPT * 16), n = o / 16 % (NT * TPT);
-        const int64_t row = row0 + 16 * i + o % 16;
-        if (n >= tokens || row >= g.M) continue;
+        if (!wanted(o)) continue;
         float sum = sums[o];
         for (int w = 1; w < g.ways; ++w) sum += sums[w * kOut + o];
-        static_cast<T*>(g.y)[(n0 + n) * g.ldy + row] = XT::store(sum);
+        if (!TILED || g.split == 1) store(o, sum);
+        else __hip_atomic_store(parts + blockIdx.z * kOut + o, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if constexpr (TILED) {
+        if (g.split == 1 || !last_of(g.done + tile, g.split, reinterpret_cast<int*>(lds))) return;
+        for (int o = threadIdx.x; o < kOut; o += blockDim.x) {
+            if (!wanted(o)) continue;
+            float sum = __hip_atomic_load(parts + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int z = 1; z < g.split; ++z) sum += __hip_atomic_load(parts + z * kOut + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            store(o, sum);
+        }
     }
 }
 
 // x as the matrix unit takes it (TilesOfX): a workgroup writes a chunk of a tile, 4 KB.  Columns behind K are zero, rows
 // without a token stay as they are.
 template <typename XT>
-__global__ __launch_bounds__(256) void q4_tiles_kernel(const void* x, int64_t K, int64_t N, int64_t ldx, uint16_t* tiles) {
+__global__ __launch_bounds__(256) void q4_tiles_kernel(const void* x, int64_t K, int64_t N, int64_t ldx, uint16_t* tiles, uint32_t* done,
+                                                       int64_t counts) {
     using T = typename XT::type;
     constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S;
+    for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x; i < counts;
+         i += (int64_t)gridDim.x * gridDim.y * blockDim.x)
+        done[i] = 0;
     const int token = threadIdx.x % TPT, piece = threadIdx.x / TPT;
     const int64_t n = (int64_t)blockIdx.y * TPT + token, k = (int64_t)blockIdx.x * kQ4Chunk + 8 * piece;
     if (n >= N) return;
@@ -161,8 +187,9 @@ __global__ __launch_bounds__(256) void q4_tiles_kernel(const void* x, int64_t K,
 struct Plan {
     bool staged;
     bool tiled;
-    int nt, r, u, ways, tiles, slab;
-    size_t lds, workspace;
+    int nt, r, u, ways, tiles, slab, split, part_chunks;
+    int64_t counts;
+    size_t lds, parts, done, workspace;
 };
 
 Plan plan_for(int dtype, int64_t M, int64_t K, int64_t N) {
@@ -192,13 +219,31 @@ Plan plan_for(int dtype, int64_t M, int64_t K, int64_t N) {
     p.nt = N <= tpt ? 1 : N <= 2 * tpt ? 2 : 4;
     p.r = p.nt == 4 || tiles < 320 ? 1 : tiles < 1024 ? 2 : 4;
     const int most = p.r == 4 ? 4 : 8;
-    const int64_t steps = (chunks + 1) / 2;
-    p.ways = (int)(steps < most ? steps : most);
+    // Workgroups that share K, where they are few or leave most of the chip without one at the end: what the busiest compute unit
+    // does, a step of a wavefront being about 1 us and 0.5 for every 16 rows by 16 virtual rows, 2 us to begin and end, and 2 to join the
+    // sums.
+    // 698 x 7877 for 21 bfloat16 vectors 10.1 us alone, 8.0 / 6.6 / 9.9 with 2 / 4 / 8; 9409 x 22330 for 6 in fp32 67, 54.5 / 53 /
+    // 62; 5000 x 5000 for 4 in fp32 8.0, 8.9 / 8.8 / 11.6; 4096 x 25088 for 13 in binary16 17.4, 19.5 / 18.9 / 20.5.
+    const int64_t groups = (tiles + p.r - 1) / p.r * ((N + p.nt * tpt - 1) / (p.nt * tpt));
+    double least = 0;
+    for (int split = 1; split <= kSplitMost && split <= (chunks + 1) / 2; ++split) {
+        const int part = (int)((chunks + split - 1) / split + 1) / 2 * 2, parts = (int)((chunks + part - 1) / part);
+        const int steps = part / 2, ways = steps < most ? steps : most;
+        const double cost = (double)((groups * parts + 255) / 256) * ((steps + ways - 1) / ways * (1 + 0.5 * p.r * p.nt) + 2) + (parts > 1 ? 2 : 0);
+        if (split > 1 && cost >= least) continue;
+        least = cost;
+        p.ways = ways;
+        p.split = parts;
+        p.part_chunks = part;
+    }
     // 16-bit vectors as they are, unless rows a power of two apart and half lines cost more than a kernel that lays them out
     // (about 3 us): 16384 x 8192 for 32 vectors 32 us as they are, 23 + 3 as tiles; 6000 x 3000 for 16 vectors 5.5 and 5.6 + 2.
-    p.tiled = dtype == BS_F32 || p.nt == 4 || M * K >= ((int64_t)1 << 26);
+    p.tiled = dtype == BS_F32 || p.nt == 4 || p.split > 1 || M * K >= ((int64_t)1 << 26);
     p.lds = (size_t)p.ways * p.r * p.nt * tpt * 16 * 4;
-    p.workspace = (size_t)((N + tpt - 1) / tpt) * 32 * q4_padded(K);
+    p.parts = (size_t)((N + tpt - 1) / tpt) * 32 * q4_padded(K);
+    p.counts = p.split > 1 ? groups : 0;
+    p.done = p.parts + (size_t)p.counts * p.split * p.r * p.nt * tpt * 64;
+    p.workspace = p.done + (size_t)p.counts * 4;
     return p;
 }
 
@@ -222,7 +267,7 @@ int launch_many(const GemvArgs& g, const Plan& p, hipStream_t st) {
         if (rc != BS_OK) return rc;
     }
     const int per = NT * (16 / XT::kSlots);
-    const dim3 grid((unsigned)((g.M + 16 * R - 1) / (16 * R)), (unsigned)((g.N + per - 1) / per));
+    const dim3 grid((unsigned)((g.M + 16 * R - 1) / (16 * R)), (unsigned)((g.N + per - 1) / per), (unsigned)g.split);
     hipLaunchKernelGGL((q4_gemv_many_kernel<XT, NT, R, GL, TILED>), grid, dim3(64 * p.ways), p.lds, st, g);
     return hip_status(hipGetLastError());
 }
@@ -253,12 +298,13 @@ template <typename XT>
 int launch_type(GemvArgs g, const Plan& p, int group, void* workspace, hipStream_t st) {
     bool tiled = false;
     if (!p.staged) {
-        tiled = p.tiled;
+        // rows that do not start where a load does: 698 x 7877 for 21 vectors 30 us as they are, 10 + 2.5 as tiles
+        tiled = p.tiled || g.ldx % 8 || (reinterpret_cast<uintptr_t>(g.x) & 15);
         if (tiled) {
             constexpr int TPT = 16 / XT::kSlots;
             const dim3 grid((unsigned)(q4_padded(g.K) / kQ4Chunk), (unsigned)((g.N + TPT - 1) / TPT));
             hipLaunchKernelGGL(q4_tiles_kernel<XT>, grid, dim3(16 * TPT), 0, st, g.x, g.K, g.N, g.ldx,
-                               static_cast<uint16_t*>(workspace));
+                               static_cast<uint16_t*>(workspace), g.done, p.counts);
             const int rc = hip_status(hipGetLastError());
             if (rc != BS_OK) return rc;
             g.x = workspace;
@@ -280,7 +326,9 @@ int launch_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int6
     const Plan p = plan_for(dtype, M, K, N);
     if (p.workspace && (!workspace || workspace_bytes < p.workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)))
         return BS_ERR_WORKSPACE;
-    const GemvArgs g{codes, scales, M, K, N, ldx, ldy, x, y, p.ways, p.tiles, p.slab};
+    char* const base = static_cast<char*>(workspace);
+    const GemvArgs g{codes, scales, M, K, N, ldx, ldy, x, y, p.ways, p.tiles, p.slab, p.split, p.part_chunks,
+                     reinterpret_cast<float*>(base + p.parts), reinterpret_cast<uint32_t*>(base + p.done)};
     switch (dtype) {
         case BS_F32: return launch_type<F32>(g, p, group, workspace, st);
         case BS_F16: return launch_type<F16>(g, p, group, workspace, st);

@@ -426,19 +426,11 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
         for (int w = 1; w < kDownWaves; ++w) sum += sums[w * all + o];
         if (g.split == 1) {
             if (d0 + o % 16 < g.D) static_cast<typename XT::type*>(g.y)[o / 16 * g.ldy + d0 + o % 16] = XT::store(sum);
-        } else {      // past the caches that other compute units do not look into; see below
+        } else {
             __hip_atomic_store(parts + blockIdx.y * all + o, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
-    if (g.split == 1) return;
-    // The sums were stored, and are loaded, with the scope of the whole GPU, so that they are where everybody sees them as soon
-    // as each lane has waited for its own.  A fence of that scope would write back all that the cache holds: 16 us here.
-    wait_vm_and_lds<0>();
-    pin_order();
-    __syncthreads();
-    if (threadIdx.x == 0) *found = (int)__hip_atomic_fetch_add(g.done + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (*found != g.split - 1) return;      // another workgroup will be last
+    if (g.split == 1 || !last_of(g.done + blockIdx.x, g.split, found)) return;
     for (int o = threadIdx.x; o < all; o += blockDim.x) {
         float sum = __hip_atomic_load(parts + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         for (int z = 1; z < g.split; ++z) sum += __hip_atomic_load(parts + z * all + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

@@ -195,6 +195,26 @@ def test_gemv_on_another_stream_and_in_a_graph():
         assert torch.equal(out, eager)
 
 
+def test_gemv_whose_workgroups_share_k_in_a_graph():
+    """Few rows, many columns, several vectors: sums are joined, and counted anew on every replay."""
+    M, K, N, group = 40, 12000, 9, 64
+    codes, scales, W = packed(M, K, group, 8)
+    x = torch.zeros((N, K), dtype=torch.bfloat16, device="cuda")
+    bs.bs_init()
+    bs.bs_q4_gemv(codes, scales, group, x)
+    workspace = torch.full((bs.bs_q4_gemv_workspace_bytes(bs.BS_BF16, M, K, group, N),), 255, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = bs.bs_q4_gemv(codes, scales, group, x, workspace=workspace)
+    for seed in range(3):
+        x.copy_(torch.randn((N, K), generator=torch.Generator().manual_seed(seed)))
+        want = bs.bs_q4_gemv(codes, scales, group, x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+        check_product(y, W, x.cpu())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_matrices_that_start_anywhere(dtype):
     """W and scales are only as aligned as their types; what lies beside an unpacked matrix stays."""
