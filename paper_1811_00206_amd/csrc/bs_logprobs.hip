@@ -17,10 +17,10 @@
 // does not matter.  Rows that flood the lists (masks that leave fewer than n words, equal logits) are gone over once more with
 // the strict bound, or n times, which is slow and right.
 //
-// Measured: 4096 rows of 32003 bfloat16 logits with the 5 largest in 65 us (4.1 TB/s; 45 at the rate of reads), 58 without
-// alternatives: the vector ALU is what is busy, with two instructions to convert, one for the maximum, three for u, one
-// exponential (a quarter of the rate) and two sums an element.  One row of 131072 fp32 logits: 8.4 us in 16 slices, 4.7 to join
-// them.  The gradient of 4096 x 32003: 106 us, 102 at the rate of a copy.
+// Measured: 4096 rows of 32003 bfloat16 logits with the 5 largest in 59 us (4.4 TB/s; 45 at the rate of reads), 56 without
+// alternatives: an element takes the vector ALU ten cycles' worth of instructions (conversion, maximum, two for u, an exponential
+// of four, two sums), 32 us of the whole, and the loads of the next batch hide the rest only in part.  One row of 131072 fp32
+// logits: 8.2 us in 16 slices, 4.6 to join them.  The gradient of 4096 x 32003: 106 us, 102 at the rate of a copy.
 #include "bs_q4.h"
 
 namespace bs {
@@ -78,7 +78,7 @@ struct Args {
     const int64_t* targets;
     int n, slices;
     int64_t slice_vectors;      // 16-byte pieces of a row in a slice
-    int sharing;                // batches of a place
+    int sharing, places;        // batches of a place, places of a thread
     float *logprob, *entropy, *lse, *top_values;
     int32_t* top_ids;
     Stats* part_stats;          // [rows][slices]
@@ -98,19 +98,47 @@ struct Row {
         head = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
     }
     __device__ __forceinline__ int64_t vectors() const { return (V + head + E - 1) / E; }
+    // Piece v as it lies in memory, if it is one of the whole ones, first .. last; else one of those
+    __device__ __forceinline__ int first() const { return head ? 1 : 0; }
+    __device__ __forceinline__ int last() const { return (int)((V + head) / E) - 1; }
+    __device__ __forceinline__ uint4 raw(int v) const { return reinterpret_cast<const uint4*>(p - head)[min(max(v, first()), last())]; }
+    // a piece that is not whole, -inf where it has no elements
+    __device__ __forceinline__ uint4 edge(int64_t v) const {
+        const int64_t e = v * E - head;
+        T out[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) out[i] = e + i >= 0 && e + i < V ? p[e + i] : XT::store(-__builtin_inff());
+        uint4 a;
+        __builtin_memcpy(&a, out, 16);
+        return a;
+    }
+    static __device__ __forceinline__ void values(uint4 a, float* out) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            if constexpr (sizeof(T) == 4) out[i] = __builtin_bit_cast(float, word_of(a, i));
+            else out[i] = XT::load((uint16_t)(word_of(a, i >> 1) >> (16 * (i & 1))));
+        }
+    }
     __device__ __forceinline__ void load(int64_t v, float* out) const {
         const int64_t e = v * E - head;
         if (e >= 0 && e + E <= V) {
-            const uint4 a = *reinterpret_cast<const uint4*>(p + e);
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                if constexpr (sizeof(T) == 4) out[i] = __builtin_bit_cast(float, word_of(a, i));
-                else out[i] = XT::load((uint16_t)(word_of(a, i >> 1) >> (16 * (i & 1))));
-            }
+            values(*reinterpret_cast<const uint4*>(p + e), out);
         } else {
 #pragma unroll
             for (int i = 0; i < E; ++i) out[i] = e + i >= 0 && e + i < V ? XT::load(p[e + i]) : -__builtin_inff();
         }
+    }
+};
+
+// The threads of a row: a workgroup, or a wavefront of one
+template <int THREADS>
+struct Group {
+    static constexpr int kWaves = THREADS / 64;
+    static __device__ __forceinline__ int thread() { return threadIdx.x % THREADS; }
+    static __device__ __forceinline__ int wave() { return thread() >> 6; }
+    static __device__ __forceinline__ void sync() {
+        if constexpr (THREADS == kThreads) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // LDS serves a wavefront in order
     }
 };
 
@@ -141,24 +169,37 @@ __device__ __forceinline__ int keys_before(const uint64_t* keys, int count, uint
 }
 
 // the n largest keys of the list, in order; entries behind the list's end become 0.  All threads, barriers inside.
-template <int LIST>
+template <int THREADS, int LIST>
 __device__ __forceinline__ void order_list(KeyList<LIST>& l, int count, int n) {
-    for (int i = threadIdx.x; i < n; i += kThreads)
+    using G = Group<THREADS>;
+    const int me = G::thread();
+    for (int i = me; i < n; i += THREADS)
         if (i >= count) l.sorted[i] = 0;
     const int padded = (count + 7) & ~7;       // the walk below takes eight at a time
-    if (threadIdx.x < 8 && count + (int)threadIdx.x < padded) l.keys[count + threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < count; i += kThreads) {
+    if (me < 8 && count + me < padded) l.keys[count + me] = 0;
+    G::sync();
+    for (int i = me; i < count; i += THREADS) {
         const uint64_t key = l.keys[i];
         const int before = keys_before(l.keys, padded, key);
         if (before < n) l.sorted[before] = key;
     }
-    __syncthreads();
+    G::sync();
 }
 
-// the k-th largest of the lanes' values
+// the k-th largest of the lanes' values.  One after the other is about 100 cycles each, all ranks at once 800.
 __device__ __forceinline__ float kth_largest(float v, int k) {
     float most = v;
+    if (k > 8) {
+        const int lane = threadIdx.x & 63;
+        int rank = 0;
+#pragma unroll
+        for (int j = 0; j < 64; ++j) {
+            const float other = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), j));
+            rank += other > v || (other == v && j < lane);
+        }
+        const int at = __ffsll((unsigned long long)__ballot(rank == k - 1)) - 1;
+        return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), __builtin_amdgcn_readfirstlane(at)));
+    }
     for (int j = 0; j < k; ++j) {
         most = max_of_wave(v);
         const uint64_t m = __ballot(v == most);
@@ -168,26 +209,29 @@ __device__ __forceinline__ float kth_largest(float v, int k) {
 }
 
 // how many of the list's keys are not below `least`; all threads
+template <int THREADS>
 __device__ __forceinline__ int keys_from(TopList& l, const uint64_t* keys, int count, uint64_t least) {
+    const int me = Group<THREADS>::thread();
     int n = 0;
-    for (int i = threadIdx.x; i < (count + 63) / 64 * 64; i += kThreads) n += __popcll(__ballot(i < count && keys[i] >= least));
-    if ((threadIdx.x & 63) == 0) l.wave_count[threadIdx.x >> 6] = n;
-    __syncthreads();
+    for (int i = me; i < (count + 63) / 64 * 64; i += THREADS) n += __popcll(__ballot(i < count && keys[i] >= least));
+    if ((me & 63) == 0) l.wave_count[me >> 6] = n;
+    Group<THREADS>::sync();
     n = 0;
-    for (int w = 0; w < kWaves; ++w) n += l.wave_count[w];
-    __syncthreads();
+    for (int w = 0; w < Group<THREADS>::kWaves; ++w) n += l.wave_count[w];
+    Group<THREADS>::sync();
     return n;
 }
 
 // The list flooded.  First what is larger than the bound, into the room of the eights' largest (`most` keys), out of which the
 // n-th largest key is found bit by bit; if that is too many too, the n largest one after the other.
-template <typename XT>
+template <typename XT, int THREADS>
 __device__ void flooded(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, float bound, int n, uint64_t* keys, int most) {
     constexpr int E = Row<XT>::E;
-    __syncthreads();
-    if (threadIdx.x == 0) l.count = 0;
-    __syncthreads();
-    for (int64_t v = v0 + threadIdx.x; v < v1; v += kThreads) {
+    const int me = Group<THREADS>::thread();
+    Group<THREADS>::sync();
+    if (me == 0) l.count = 0;
+    Group<THREADS>::sync();
+    for (int64_t v = v0 + me; v < v1; v += THREADS) {
         float x[E];
         row.load(v, x);
         for (int i = 0; i < E; ++i)
@@ -196,26 +240,26 @@ __device__ void flooded(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, 
                 if (at < most) keys[at] = order_key(x[i], (uint32_t)(v * E - row.head + i));
             }
     }
-    __syncthreads();
+    Group<THREADS>::sync();
     const int count = l.count;
     if (count <= most) {
         uint64_t least = 0;
         if (count > n)
             for (int bit = 63; bit >= 0; --bit)
-                if (keys_from(l, keys, count, least | (uint64_t)1 << bit) >= n) least |= (uint64_t)1 << bit;
-        __syncthreads();
-        if (threadIdx.x == 0) l.count = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < count; i += kThreads)
+                if (keys_from<THREADS>(l, keys, count, least | (uint64_t)1 << bit) >= n) least |= (uint64_t)1 << bit;
+        Group<THREADS>::sync();
+        if (me == 0) l.count = 0;
+        Group<THREADS>::sync();
+        for (int i = me; i < count; i += THREADS)
             if (keys[i] >= least) l.keys[atomicAdd(&l.count, 1)] = keys[i];      // n at most: keys are different
-        __syncthreads();
-        order_list(l, min(count, n), n);
+        Group<THREADS>::sync();
+        order_list<THREADS>(l, min(count, n), n);
         return;
     }
     uint64_t last = ~(uint64_t)0;
     for (int j = 0; j < n; ++j) {
         uint64_t best = 0;
-        for (int64_t v = v0 + threadIdx.x; v < v1; v += kThreads) {
+        for (int64_t v = v0 + me; v < v1; v += THREADS) {
             float x[E];
             row.load(v, x);
             for (int i = 0; i < E; ++i) {
@@ -225,27 +269,28 @@ __device__ void flooded(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, 
             }
         }
         best = wave_max(best);
-        if ((threadIdx.x & 63) == 0) l.wave_best[threadIdx.x >> 6] = best;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w) best = l.wave_best[w] > best ? l.wave_best[w] : best;
+        if ((me & 63) == 0) l.wave_best[me >> 6] = best;
+        Group<THREADS>::sync();
+        for (int w = 0; w < Group<THREADS>::kWaves; ++w) best = l.wave_best[w] > best ? l.wave_best[w] : best;
         last = best;
-        if (threadIdx.x == 0) l.sorted[j] = best;
-        __syncthreads();
+        if (me == 0) l.sorted[j] = best;
+        Group<THREADS>::sync();
     }
 }
 
 // Entries of sorted[] that are still 0: the first elements of the slice that are not larger than `bound` (all that are
 // larger are there already)
-template <typename XT>
+template <typename XT, int THREADS>
 __device__ void fill(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, float bound, int n) {
     constexpr int E = Row<XT>::E;
+    const int me = Group<THREADS>::thread();
     int have = 0;
     while (have < n && l.sorted[have]) ++have;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = me & 63, wave = me >> 6;
     // the equals of the bound, in order of their index; then, lower than any number, what is none
     for (int pass = 0; pass < 2 && have < n; ++pass) {
-        for (int64_t b = v0; b < v1 && have < n; b += kThreads) {
-            const int64_t v = b + threadIdx.x;
+        for (int64_t b = v0; b < v1 && have < n; b += THREADS) {
+            const int64_t v = b + me;
             float x[E];
             uint32_t mine = 0;
             if (v < v1) {
@@ -258,9 +303,9 @@ __device__ void fill(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, flo
             const int c = __popc(mine);
             const int before = group_prefix_i<64>(c, lane);
             if (lane == 63) l.wave_count[wave] = before + c;
-            __syncthreads();
+            Group<THREADS>::sync();
             int at = have + before, all = 0;
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < Group<THREADS>::kWaves; ++w) {
                 if (w < wave) at += l.wave_count[w];
                 all += l.wave_count[w];
             }
@@ -270,10 +315,10 @@ __device__ void fill(TopList& l, const Row<XT>& row, int64_t v0, int64_t v1, flo
                     ++at;
                 }
             have += all;
-            __syncthreads();
+            Group<THREADS>::sync();
         }
     }
-    __syncthreads();
+    Group<THREADS>::sync();
 }
 
 // what a log probability is made of
@@ -289,9 +334,19 @@ __device__ __forceinline__ float logprob_of(float x, Norm z) {
     return (float)((d - z.log2_s) * 0.69314718055994530942);
 }
 
-// a row's results, by one lane
+// a row's target and its logit, which are asked for long before they are needed
+struct Target {
+    int64_t at;
+    float x;
+};
 template <typename XT>
-__device__ __forceinline__ Norm finish(const Args& g, int64_t row, Stats st) {
+__device__ __forceinline__ Target target_of(const Args& g, int64_t row) {
+    const int64_t at = g.targets[row];
+    return {at, at >= 0 && at < g.V ? XT::load(static_cast<const typename XT::type*>(g.logits)[row * g.ld + at]) : 0.f};
+}
+
+// a row's results, by one lane
+__device__ __forceinline__ Norm finish(const Args& g, int64_t row, Stats st, Target target) {
     constexpr double kLn2 = 0.69314718055994530942;
     const double log2_s = log2((double)st.s);
     const Norm z{st.m, log2_s};
@@ -299,44 +354,81 @@ __device__ __forceinline__ Norm finish(const Args& g, int64_t row, Stats st) {
     const double lse = extreme(st.m) ? (double)st.m + log2_s * kLn2 : ((double)(st.m * kLog2e) + log2_s) * kLn2;
     g.lse[row] = words ? (float)lse : -__builtin_inff();
     g.entropy[row] = words ? (float)((log2_s - (double)st.t / (double)st.s) * kLn2) : 0.f;
-    const int64_t target = g.targets[row];
     float p = 0.f;
-    if (target >= g.V) p = __builtin_nanf("");
-    else if (target >= 0) p = logprob_of(XT::load(static_cast<const typename XT::type*>(g.logits)[row * g.ld + target]), z);
+    if (target.at >= g.V) p = __builtin_nanf("");
+    else if (target.at >= 0) p = logprob_of(target.x, z);
     g.logprob[row] = p;
     return z;
 }
 
+template <int THREADS>
 __device__ __forceinline__ void write_top(const Args& g, int64_t row, const uint64_t* sorted, Norm z) {
-    for (int i = threadIdx.x; i < g.n; i += kThreads) {
+    for (int i = Group<THREADS>::thread(); i < g.n; i += THREADS) {
         g.top_values[row * g.n + i] = logprob_of(value_of_key(sorted[i]), z);
         g.top_ids[row * g.n + i] = (int32_t)index_of_key(sorted[i]);
     }
 }
 
-template <typename XT, bool TOP>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8))) void logprobs_kernel(Args g) {
-    constexpr int E = Row<XT>::E, U = kBatch / E, V8 = 8 / E;      // pieces of a thread, and of eight elements
-    extern __shared__ __align__(16) f32x4 largest[];               // [place][thread]: of the batches' four eights
-    __shared__ TopList l;
-    __shared__ Stats stats[kWaves];
-    __shared__ Norm norm;
-    const int64_t r = blockIdx.x / g.slices, slice = blockIdx.x % g.slices, row_no = g.first_row + r;
-    const Row<XT> row(g.logits, row_no, g.ld, g.V);
+// THREADS: a workgroup for a row (or a slice of one), or a wavefront
+template <typename XT, bool TOP, int THREADS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(typename XT::type) == 2 ? 7 : 8))) void logprobs_kernel(Args g) {
+    using G = Group<THREADS>;
+    using R = Row<XT>;
+    constexpr int E = R::E, U = kBatch / E, V8 = 8 / E, kRows = kThreads / THREADS;      // pieces of a thread, and of eight elements
+    extern __shared__ __align__(16) f32x4 all_largest[];           // [row][place][thread]: of the batches' four eights
+    __shared__ TopList lists[kRows];
+    __shared__ Stats all_stats[kWaves];
+    __shared__ Norm norms[kRows];
+    const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS), me = G::thread(), wave = G::wave(), lane = threadIdx.x & 63;
+    const int64_t r = kRows > 1 ? (int64_t)blockIdx.x * kRows + mine : blockIdx.x / g.slices, slice = kRows > 1 ? 0 : blockIdx.x % g.slices;
+    const int64_t row_no = g.first_row + r;
+    if (kRows > 1 && row_no >= g.T) return;
+    TopList& l = lists[mine];
+    Stats* const stats = all_stats + mine * G::kWaves;
+    f32x4* const largest = all_largest + mine * g.places * THREADS;
+    const R row(g.logits, row_no, g.ld, g.V);
     const int64_t v0 = slice * g.slice_vectors, v1 = min(row.vectors(), v0 + g.slice_vectors);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (TOP && threadIdx.x == 0) l.count = l.eight_count = 0;
+    if (TOP && me == 0) l.count = l.eight_count = 0;
+    const Target target = g.slices == 1 ? target_of<XT>(g, row_no) : Target{-1, 0.f};
     Stats st{-__builtin_inff(), 0.f, 0.f};
     int batches = 0;
-    for (int64_t b = v0; b < v1; b += kThreads * U, ++batches) {
+    // 16-bit rows: the next batch's pieces are held while one is added up (16 registers; fp32's would be 32)
+    constexpr bool kAhead = E == 8;
+    const int first = row.first(), last = (int)min(v1, (int64_t)row.last() + 1) - 1;      // whole pieces
+    const bool any = row.last() >= first;
+    uint4 next[kAhead ? U : 1];
+    const auto load = [&](int64_t b) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u] = row.raw((int)b + u * THREADS + me);
+    };
+    if constexpr (kAhead) {
+        if (any) load(v0);
+    }
+    for (int64_t b = v0; b < v1; b += THREADS * U, ++batches) {
         float x[kBatch];
+        if constexpr (kAhead) {
+            uint4 now[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t v = b + u * kThreads + threadIdx.x;
-            if (v < v1) row.load(v, x + u * E);
-            else
+            for (int u = 0; u < U; ++u) {
+                now[u] = next[u];
+                asm volatile("" : "+v"(now[u].x), "+v"(now[u].y), "+v"(now[u].z), "+v"(now[u].w));
+            }
+            if (b + THREADS * U < v1 && any) load(b + THREADS * U);
 #pragma unroll
-                for (int i = 0; i < E; ++i) x[u * E + i] = -__builtin_inff();
+            for (int u = 0; u < U; ++u) {
+                const int v = (int)b + u * THREADS + me;
+                if (v < first || v > last) now[u] = row.edge(v < v1 ? v : row.vectors());
+                R::values(now[u], x + u * E);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t v = b + u * THREADS + me;
+                if (v < v1) row.load(v, x + u * E);
+                else
+#pragma unroll
+                    for (int i = 0; i < E; ++i) x[u * E + i] = -__builtin_inff();
+            }
         }
         float part[kParts], most = -__builtin_inff();
 #pragma unroll
@@ -347,7 +439,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8))) v
             most = fmaxf(most, part[i]);
         }
         if constexpr (TOP) {
-            f32x4& place = largest[batches / g.sharing * kThreads + threadIdx.x];
+            f32x4& place = largest[batches / g.sharing * THREADS + me];
             if (batches % g.sharing) {
 #pragma unroll
                 for (int i = 0; i < kParts; ++i) part[i] = fmaxf(part[i], place[i]);
@@ -364,11 +456,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8))) v
             for (int i = 0; i < kBatch; ++i) x[i] -= st.m;
         }
 #pragma unroll
-        for (int i = 0; i < kBatch; i += 2) {
-            const float u0 = at_least(fmaf(x[i], kLog2e, -c), -200.f), u1 = at_least(fmaf(x[i + 1], kLog2e, -c), -200.f);
-            const float p0 = exp2_hw(u0), p1 = exp2_hw(u1);
-            s0 += p0; s1 += p1;
-            t0 = fmaf(p0, u0, t0); t1 = fmaf(p1, u1, t1);
+        for (int j = 0; j < kParts; ++j) {
+            if (b + j * V8 * THREADS >= v1) break;      // no thread has more
+#pragma unroll
+            for (int i = 8 * j; i < 8 * j + 8; i += 2) {
+                const float u0 = at_least(fmaf(x[i], kLog2e, -c), -200.f), u1 = at_least(fmaf(x[i + 1], kLog2e, -c), -200.f);
+                const float p0 = exp2_hw(u0), p1 = exp2_hw(u1);
+                s0 += p0; s1 += p1;
+                t0 = fmaf(p0, u0, t0); t1 = fmaf(p1, u1, t1);
+            }
         }
         st.s += s0 + s1;
         st.t += t0 + t1;
@@ -377,36 +473,36 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8))) v
     if constexpr (TOP) {
         const int with_words = __popcll(__ballot(st.m > -__builtin_inff()));
         if (lane == 0) l.wave_count[wave] = with_words;
-        __syncthreads();
+        G::sync();
         // of the n, every wavefront answers for its share of the lanes that have words
-        int mine = l.wave_count[wave], lanes = 0;
-        for (int w = 0; w < kWaves; ++w) lanes += l.wave_count[w];
-        const int k = lanes < g.n ? -1 : (g.n * mine + lanes - 1) / lanes;
+        int here = l.wave_count[wave], lanes = 0;
+        for (int w = 0; w < G::kWaves; ++w) lanes += l.wave_count[w];
+        const int k = lanes < g.n ? -1 : (g.n * here + lanes - 1) / lanes;
         const float bound_here = k < 0 ? -__builtin_inff() : k ? kth_largest(st.m, k) : __builtin_inff();
         if (lane == 0) l.bound[wave] = bound_here;
     }
     st = join_wave(st);
     if (lane == 0) stats[wave] = st;
-    __syncthreads();
+    G::sync();
     if constexpr (TOP) {
         bound = l.bound[0];
-        for (int w = 1; w < kWaves; ++w) bound = fminf(bound, l.bound[w]);
+        for (int w = 1; w < G::kWaves; ++w) bound = fminf(bound, l.bound[w]);
         for (int b = 0; b * g.sharing < batches; ++b) {
-            const f32x4 part = largest[b * kThreads + threadIdx.x];
+            const f32x4 part = largest[b * THREADS + me];
 #pragma unroll
             for (int i = 0; i < kParts; ++i)
                 if (part[i] >= bound && part[i] > -__builtin_inff()) {
                     const int at = atomicAdd(&l.eight_count, 1);
-                    if (at < kEights) l.eights[at] = (uint32_t)(b * kParts + i) * kThreads + threadIdx.x;
+                    if (at < kEights) l.eights[at] = (uint32_t)(b * kParts + i) * THREADS + me;
                 }
         }
-        __syncthreads();
+        G::sync();
         const int eights = l.eight_count;
         const int64_t pieces = (int64_t)min(eights, kEights) * V8 * g.sharing;
-        for (int64_t j = threadIdx.x; j < pieces; j += kThreads) {
-            const uint32_t eight = l.eights[j / (V8 * g.sharing)], place = eight / kThreads;
+        for (int64_t j = me; j < pieces; j += THREADS) {
+            const uint32_t eight = l.eights[j / (V8 * g.sharing)], place = eight / THREADS;
             const int64_t batch = place / kParts * (int64_t)g.sharing + j / V8 % g.sharing;
-            const int64_t v = v0 + (batch * U + place % kParts * V8 + j % V8) * kThreads + eight % kThreads;
+            const int64_t v = v0 + (batch * U + place % kParts * V8 + j % V8) * THREADS + eight % THREADS;
             float x[E];
             if (v < v1) row.load(v, x);
 #pragma unroll
@@ -417,24 +513,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8))) v
                 }
         }
         // meanwhile
-        if (threadIdx.x == kThreads - 64) {
-            for (int w = 0; w < kWaves - 1; ++w) st = join(st, stats[w]);
-            if (g.slices == 1) norm = finish<XT>(g, row_no, st);
+        if (me == THREADS - 64) {
+            for (int w = 0; w < G::kWaves - 1; ++w) st = join(st, stats[w]);
+            if (g.slices == 1) norms[mine] = finish(g, row_no, st, target);
             else g.part_stats[blockIdx.x] = st;
         }
-        __syncthreads();
+        G::sync();
         const int count = l.count;
         if (eights > kEights || count > kList)
-            flooded(l, row, v0, v1, bound, g.n, reinterpret_cast<uint64_t*>(largest), (batches + g.sharing - 1) / g.sharing * (kThreads * 2));
-        else order_list(l, count, g.n);
+            flooded<XT, THREADS>(l, row, v0, v1, bound, g.n, reinterpret_cast<uint64_t*>(largest),
+                                 (batches + g.sharing - 1) / g.sharing * (THREADS * 2));
+        else order_list<THREADS>(l, count, g.n);
         // a slice can have fewer words than n that are larger than its bound
-        if (!l.sorted[g.n - 1]) fill(l, row, v0, v1, bound, g.n);
-        if (g.slices == 1) write_top(g, row_no, l.sorted, norm);
+        if (!l.sorted[g.n - 1]) fill<XT, THREADS>(l, row, v0, v1, bound, g.n);
+        if (g.slices == 1) write_top<THREADS>(g, row_no, l.sorted, norms[mine]);
         else
-            for (int i = threadIdx.x; i < g.n; i += kThreads) g.part_keys[(int64_t)blockIdx.x * g.n + i] = l.sorted[i];
-    } else if (threadIdx.x == 0) {
-        for (int w = 1; w < kWaves; ++w) st = join(st, stats[w]);
-        if (g.slices == 1) finish<XT>(g, row_no, st);
+            for (int i = me; i < g.n; i += THREADS) g.part_keys[(int64_t)blockIdx.x * g.n + i] = l.sorted[i];
+    } else if (me == 0) {
+        for (int w = 1; w < G::kWaves; ++w) st = join(st, stats[w]);
+        if (g.slices == 1) finish(g, row_no, st, target);
         else g.part_stats[blockIdx.x] = st;
     }
 }
@@ -448,6 +545,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(Args g) {
     const int all = g.slices * g.n, lane = threadIdx.x & 63;
     const uint64_t* keys = g.part_keys + (int64_t)blockIdx.x * all;
     if (threadIdx.x == 0) l.count = 0;
+    const Target target = target_of<XT>(g, row);
     uint64_t bound = lane < g.slices && g.n ? keys[lane * g.n + (g.n + g.slices - 1) / g.slices - 1] : ~(uint64_t)0;
     bound = ~wave_max(~bound);
     __syncthreads();
@@ -459,11 +557,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(Args g) {
         Stats st{-__builtin_inff(), 0.f, 0.f};
         if (lane < g.slices) st = g.part_stats[(int64_t)blockIdx.x * g.slices + lane];
         st = join_wave(st);
-        if (threadIdx.x == 0) norm = finish<XT>(g, row, st);
+        if (threadIdx.x == 0) norm = finish(g, row, st, target);
     }
     __syncthreads();
-    order_list(l, l.count, g.n);
-    write_top(g, row, l.sorted, norm);
+    order_list<kThreads>(l, l.count, g.n);
+    write_top<kThreads>(g, row, l.sorted, norm);
 }
 
 struct BackArgs {
@@ -559,44 +657,55 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(BackArgs g)
 }
 
 struct Plan {
+    bool waves;      // a wavefront for a row
     int slices;
     int64_t slice_vectors;
 };
 
 Plan plan_for(int dtype, int64_t T, int64_t V) {
-    const int e = 16 / dtype_bytes(dtype);
+    const int e = 16 / dtype_bytes(dtype), batch = kThreads * (kBatch / e);
     const int64_t vectors = (V + e - 1) / e + 1;      // one more for a row that starts between boundaries
-    // workgroups for every compute unit, but not slices of less than two pieces a thread
+    // A wavefront for a row where there are many that are not long: no thread without words, no barriers.  4096 rows of 2100 fp32
+    // words with the 5 largest 14.9 us instead of 19.7, of 8200 bfloat16 words 23.9 instead of 34.1; 4096 x 32003 69 instead of
+    // 62, 1024 x 4100 equal, 1024 x 1100 8.4 instead of 10.7, 256 x 1100 7.8 instead of 6.4.
+    if (V <= 16384 && T >= (V <= 2048 ? 1024 : 2048)) return {true, 1, vectors};
+    // Several workgroups for a row only where it is long, since their sums take a second kernel to join (4 us and the launch):
+    // 206 rows of 12635 fp32 words 9.6 us alone, 8.3 + 4.2 halved; one of 131072 8.2 + 4.6 in 16 slices, 13.4 + 4 in 4.
     int64_t slices = 1;
-    while (slices < kSlices && T * slices < 512 && vectors / (slices * 2) >= 2 * kThreads) slices *= 2;
-    const int64_t most = kPlaces * kThreads * (kBatch / e);      // longer slices share places
-    while (slices < kSlices && slices * most < vectors) ++slices;
-    Plan p;
-    p.slice_vectors = (vectors + slices - 1) / slices;
+    if (vectors >= 6 * batch)
+        while (slices < kSlices && T * slices < 512 && vectors / (slices * 2) >= 2 * kThreads) slices *= 2;
+    while (slices < kSlices && slices * kPlaces * batch < vectors) ++slices;      // (longer slices share places)
+    Plan p{false, 1, (vectors + slices - 1) / slices};
     p.slices = (int)((vectors + p.slice_vectors - 1) / p.slice_vectors);
     return p;
 }
 
 size_t stats_bytes(int64_t T, const Plan& p) { return ((size_t)T * p.slices * sizeof(Stats) + 15) / 16 * 16; }
 
+template <typename XT, int THREADS>
+int launch_rows(Args g, int64_t rows, hipStream_t st) {
+    constexpr int kRows = kThreads / THREADS, per = THREADS * (kBatch / Row<XT>::E);
+    const dim3 grid((unsigned)((rows * g.slices + kRows - 1) / kRows));
+    if (g.n) {
+        const int64_t batches = (g.slice_vectors + per - 1) / per;
+        g.sharing = (int)((batches + kPlaces - 1) / kPlaces);
+        g.places = (int)((batches + g.sharing - 1) / g.sharing);
+        hipLaunchKernelGGL((logprobs_kernel<XT, true, THREADS>), grid, dim3(kThreads), (size_t)g.places * kThreads * sizeof(f32x4), st, g);
+    } else {
+        hipLaunchKernelGGL((logprobs_kernel<XT, false, THREADS>), grid, dim3(kThreads), 0, st, g);
+    }
+    return hip_status(hipGetLastError());
+}
+
 template <typename XT>
-int launch(Args g, hipStream_t st) {
+int launch(Args g, bool waves, hipStream_t st) {
     const int64_t most = ((int64_t)1 << 23) / g.slices;      // rows of a launch: a grid has fewer than 2^32 lanes
-    Stats* const stats = g.part_stats;
-    for (int64_t r = 0; r < g.T; r += most) {
-        const int64_t rows = g.T - r < most ? g.T - r : most;
+    const int64_t T = g.T;
+    for (int64_t r = 0; r < T; r += most) {
+        const int64_t rows = T - r < most ? T - r : most;
         g.first_row = r;
-        g.part_stats = stats;
-        const dim3 grid((unsigned)(rows * g.slices));
-        if (g.n) {
-            constexpr int per = kThreads * (kBatch / Row<XT>::E);
-            const int64_t batches = (g.slice_vectors + per - 1) / per;
-            g.sharing = (int)((batches + kPlaces - 1) / kPlaces);
-            const size_t lds = (size_t)((batches + g.sharing - 1) / g.sharing) * kThreads * sizeof(f32x4);
-            hipLaunchKernelGGL((logprobs_kernel<XT, true>), grid, dim3(kThreads), lds, st, g);
-        }
-        else hipLaunchKernelGGL((logprobs_kernel<XT, false>), grid, dim3(kThreads), 0, st, g);
-        int rc = hip_status(hipGetLastError());
+        g.T = r + rows;
+        int rc = waves ? launch_rows<XT, 64>(g, rows, st) : launch_rows<XT, kThreads>(g, rows, st);
         if (rc != BS_OK) return rc;
         if (g.slices == 1) continue;
         hipLaunchKernelGGL(logprobs_join_kernel<XT>, dim3((unsigned)rows), dim3(kThreads), 0, st, g);
@@ -641,9 +750,9 @@ int launch_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t
     g.part_stats = static_cast<Stats*>(workspace);
     g.part_keys = need ? reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + stats_bytes(T, p)) : nullptr;
     switch (dtype) {
-        case BS_F32: return launch<F32>(g, st);
-        case BS_F16: return launch<F16>(g, st);
-        default: return launch<BF16>(g, st);
+        case BS_F32: return launch<F32>(g, p.waves, st);
+        case BS_F16: return launch<F16>(g, p.waves, st);
+        default: return launch<BF16>(g, p.waves, st);
     }
 }
 

@@ -118,6 +118,37 @@ def test_words_that_lie_together(V, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,V,n", [(1025, 1, 1), (1100, 7, 7), (2100, 9, 4), (1030, 64, 64), (1105, 1105, 27), (2049, 2051, 64), (2050, 5003, 0),
+                                   (2047, 3000, 2), (2048, 9001, 3)])
+def test_many_rows(T, V, n, dtype):
+    check(*rows(T, V, dtype, T + V), n)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V,n", [(70, 64), (1500, 20), (9001, 64)])
+def test_many_rows_with_masks_and_equals(V, n, dtype):
+    """The rows that are hard by themselves, many times over: what each gives alone."""
+    x, targets = rows(9, V, dtype, V)
+    lowest = float(torch.finfo(TYPES[dtype]).min)
+    few = (torch.arange(V) % 7).to(TYPES[dtype]).cuda()
+    for i, row in enumerate((0, few, -INF, lowest, -1000.0)):
+        x[i] = row
+    x[5, V // 3:] = -INF
+    x[6, : V - 5] = -INF
+    x[7, 3] = math.nan
+    x[8] = few * 1e4 - 6e4
+    targets[5:7] = torch.tensor([0, V - 1])
+    want = bs.bs_logprobs(x, targets, top_n=n)
+    many = 2052 // 9 * 9
+    got = bs.bs_logprobs(x.repeat(many // 9, 1), targets.repeat(many // 9), top_n=n)
+    for a, b in zip(got[:4], want[:4]):
+        torch.testing.assert_close(a, b.repeat(many // 9, *(1,) * (b.dim() - 1)), rtol=1e-5, atol=1e-5, equal_nan=True)
+    assert torch.equal(got[4], want[4].repeat(many // 9, 1))
+    keep = [i for i in range(9) if i != 7]
+    check(x[keep], targets[keep], n)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_rows_of_a_wider_tensor(dtype):
     """Rows that start anywhere between the boundaries of loads; what lies beside them is not looked at."""
     V = 1003
