@@ -1,27 +1,35 @@
-// A mixture-of-experts layer on 4-bit expert matrices for a few tokens (bs.h: bs_q4_moe), in three kernels:
+// A mixture-of-experts layer on 4-bit expert matrices for a few tokens (bs.h: bs_q4_moe), 64 at a time, in two to four kernels:
 //
 //   logits  a wavefront per token and four experts: router logits; and the token's activations as virtual rows (bs_q4.h),
-//           padded with zeros, for the next kernel to read in whole pieces
-//   up      every workgroup finds all tokens' top_k experts by itself (a fraction of a microsecond, against a kernel of its
-//           own), then has 16 or 64 hidden units of a chosen expert: gate and up rows against all tokens that chose it,
+//           padded with zeros, for `up` to read in whole pieces
+//   route   one workgroup: every token's top_k experts and their weights, and the pairs (token, choice) expert by expert
+//   up      some tiles of 16 hidden units of a chosen expert: gate and up rows against all tokens that chose it,
 //           h = silu(g) * u, written as virtual rows of the last kernel
 //   down    16 outputs a tile: the wavefronts of one or a few workgroups share steps of chosen experts and add weight * W2 h
 //           into sums of their own in LDS, which are added in the order of the wavefronts; of several workgroups the one that
 //           is done last adds their sums, in their order
 //
-// Bound: every chosen expert's codes once.  An expert is known by the first (token, choice) pair that chose it; the
-// workgroups of the other pairs end at once, so nothing is sorted between the kernels.  The order of all sums is fixed: a
-// result has the same bits from every call.  Hidden values pass to `down` in two bfloat16 parts for 16-bit activations (16
-// leading bits: their rounding is not seen behind the output's) and in three (all 24 bits) for fp32.
+// Bound: every chosen expert's codes once.  What it takes above that is latency, four kernels that wait for one another, and
+// the beginning and end of the workgroups of `up` and `down`.  For up to three tokens every workgroup of `up` finds its expert by
+// itself, without `route` (which is 3 to 5 us; 7 tokens, 64 experts of 2048 x 1024, 6 each: 41.9 us with it, 47.6 without;
+// 2 tokens, 32 experts of 1004 x 415, 8 each: kernels of 26.9 with it, 22.4 without), and where the logits are few they are made
+// there too.  The order of all sums is fixed: a result has the same bits from every call.  Hidden values pass to `down` in two
+// bfloat16 parts for 16-bit activations (16 leading bits: their rounding is not seen behind the output's) and in three (all 24
+// bits) for fp32.
+//
+// Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 42 us (logits 6.4, route 4.7, up 18 to 21, down 15; 18.4
+// at the rate of a copy).  16 tokens, 8 each: up 31, down 30.  One token of 1500 x 1500 in fp32, 2 of 8: up 10.3, down 5.6.
 #include "bs_q4.h"
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace bs {
 namespace {
 
 constexpr int kDownWaves = 8;
-constexpr size_t kLdsOfX = 40 * 1024, kLdsOfH = 64 * 1024;      // x and h are brought to LDS where they take no more
+constexpr size_t kLdsOfX = 32 * 1024, kLdsOfH = 64 * 1024;      // x (twice that, if need be) and h are brought to LDS where they take no more
 constexpr int kTokens = 64;      // that pass together; more pass 64 by 64
 
 // Elements between virtual rows in the workspace: whole chunks and a cache line, so that rows a power of two long do not
@@ -47,7 +55,9 @@ struct MoeArgs {
     float* logits;          // [T][E]
     float* parts;           // [down workgroups of a tile][D padded to tiles][T], if there are several
     uint32_t* done;         // [tile]: those of them that are done
-    int32_t* leaders;       // number of chosen experts, then the first pair of each
+    int4* groups;           // x of the first: number of chosen experts; then of each: expert, first place in `order`, pairs
+    int32_t* order;         // [pairs]: the pairs, expert by expert
+    bool routed;            // groups are known before `up`
     uint32_t magic_x, magic_h;   // of the pieces of a row in LDS
     int split, part_chunks;      // workgroups of a tile in `down`, and the chunks of F of each
     int ways, tiles, rows;       // rows: tokens whose sums a wavefront of `up` keeps
@@ -77,23 +87,6 @@ __device__ __forceinline__ void router_rows(const MoeArgs& g, const typename XT:
     for (int i = 0; i < EB; ++i) {
         const float s = sum_of_wave(sum[i]);
         if (lane == 0 && e + i < g.E) logits[e + i] = s;
-    }
-}
-
-// blockIdx: token, 16 experts.  A wavefront has four of them, and the first workgroup of a token its virtual rows.
-template <typename XT>
-__global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs g) {
-    constexpr int P = XT::kParts, EB = 4;
-    const int t = blockIdx.x, e = blockIdx.y * 16 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * EB;
-    const typename XT::type* x = static_cast<const typename XT::type*>(g.x) + t * g.ldx;
-    if (e < g.E) router_rows<XT, EB>(g, x, e, g.logits + t * g.E);
-    if (blockIdx.y) return;
-    const int64_t columns = q4_padded(g.D), dp = row_pitch(g.D);
-    for (int64_t k = 8 * threadIdx.x; k < columns; k += 8 * 256) {
-        uint4 p[P];
-        pieces8<XT>(x, k, g.D, p);
-#pragma unroll
-        for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(g.xp + ((int64_t)t * P + i) * dp + k) = p[i];
     }
 }
 
@@ -150,14 +143,71 @@ __device__ __forceinline__ void choose(const MoeArgs& g, const float* logits, in
     }
 }
 
-// rows of `pieces` 16-byte pieces to LDS, `have` of which there are
-__device__ __forceinline__ void rows_to_lds(uint16_t* to, int to_pitch, const uint16_t* from, int64_t from_pitch, int rows, int pieces,
-                                            uint32_t magic, int have) {
+// How many experts are chosen before expert e, whose logit is le, by one wavefront: what choose() goes by.
+__device__ __forceinline__ int experts_before(const MoeArgs& g, const float* logits, int e, float le) {
+    const int lane = threadIdx.x & 63;
+    if (g.E <= 64) {
+        const float l = lane < g.E ? logits[lane] : 0.f;
+        const float own = l != l ? -__builtin_inff() : l, other = le != le ? -__builtin_inff() : le;
+        return __popcll(__ballot(lane < g.E && (own > other || (own == other && lane < e))));
+    }
+    const uint64_t key = order_key(le, e);
+    int n = 0;
+    for (int i = lane; i < (g.E + 63) / 64 * 64; i += 64) n += __popcll(__ballot(i < g.E && order_key(logits[min(i, g.E - 1)], i) > key));
+    return n;
+}
+
+// Choice j of a token, by one wavefront
+__device__ __forceinline__ int expert_of(const MoeArgs& g, const float* logits, int j) {
+    const int lane = threadIdx.x & 63;
+    if (g.E <= 64) {
+        const float l = lane < g.E ? logits[lane] : 0.f;
+        const float own = l != l ? -__builtin_inff() : l;
+        uint64_t free = g.E == 64 ? ~(uint64_t)0 : ((uint64_t)1 << g.E) - 1;
+        for (;;) {
+            const float most = max_of_wave(free >> lane & 1 ? own : -__builtin_inff());
+            const int first = __ffsll((unsigned long long)(__ballot(own == most) & free)) - 1;
+            if (j-- == 0) return __builtin_amdgcn_readfirstlane(first);
+            free &= ~((uint64_t)1 << first);
+        }
+    }
+    uint64_t last = ~(uint64_t)0;
+    for (; j >= 0; --j) {
+        uint64_t best = 0;
+        for (int e = lane; e < g.E; e += 64) {
+            const uint64_t key = order_key(logits[e], e);
+            if (key < last && key > best) best = key;
+        }
+        last = wave_max(best);
+    }
+    return __builtin_amdgcn_readfirstlane((int)index_of_key(last));
+}
+
+// blockIdx: token, 16 experts.  A wavefront has four of them, and the first workgroup of a token its virtual rows.
+template <typename XT>
+__global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs g) {
+    constexpr int P = XT::kParts, EB = 4;
+    const int t = blockIdx.x, e = blockIdx.y * 16 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * EB;
+    const typename XT::type* x = static_cast<const typename XT::type*>(g.x) + t * g.ldx;
+    if (e < g.E) router_rows<XT, EB>(g, x, e, g.logits + t * g.E);
+    if (blockIdx.y) return;
+    const int64_t columns = q4_padded(g.D), dp = row_pitch(g.D);
+    for (int64_t k = 8 * threadIdx.x; k < columns; k += 8 * 256) {
+        uint4 p[P];
+        pieces8<XT>(x, k, g.D, p);
+#pragma unroll
+        for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(g.xp + ((int64_t)t * P + i) * dp + k) = p[i];
+    }
+}
+
+// `rows` rows of `pieces` 16-byte pieces to LDS, `have` of which there are; from(row): where one is
+template <typename From>
+__device__ __forceinline__ void rows_to_lds(uint16_t* to, int to_pitch, From&& from, int rows, int pieces, uint32_t magic, int have) {
     const int all = rows * pieces, stride = blockDim.x;
     const auto load = [&](int j, int& at) {      // (what is not there is read as what is, and not stored)
         const int row = (int)div_magic_any(min(j, all - 1), pieces, magic), k = min(j, all - 1) - row * pieces;
         at = j < all && k < have ? row * to_pitch + 8 * k : -1;
-        return *reinterpret_cast<const uint4*>(from + row * from_pitch + 8 * min(k, have - 1));
+        return *reinterpret_cast<const uint4*>(from(row) + 8 * min(k, have - 1));
     };
     for (int j = threadIdx.x; j < all; j += 4 * stride) {      // four on their way together
         int a0, a1, a2, a3;
@@ -169,24 +219,62 @@ __device__ __forceinline__ void rows_to_lds(uint16_t* to, int to_pitch, const ui
     }
 }
 
-// the pairs at or behind `first` that chose expert e, in order, by one wavefront; their number
-__device__ __forceinline__ int pairs_of(const int32_t* ids, int pairs, int first, int e, int32_t* list) {
-    const int lane = threadIdx.x & 63;
-    int n = 0;
-    for (int b = first & ~63; b < pairs; b += 64) {
-        const int p = b + lane;
-        const bool hit = p >= first && p < pairs && ids[p] == e;
-        const uint64_t m = __ballot(hit);
-        if (hit) list[n + lanes_below(m)] = p;
-        n += __popcll(m);
+// All threads of a workgroup: every token's choices and what follows from them, written for the other kernels and the caller.
+// LDS: for every expert the tokens that chose it, as bits, [E]; its place in `order`, [E]; [pairs] ids, [pairs] weights.
+__device__ __forceinline__ void route(const MoeArgs& g, const float* logits, uint8_t* lds) {
+    static_assert(kTokens == 64);
+    unsigned long long* chose = reinterpret_cast<unsigned long long*>(lds);
+    int32_t* place = reinterpret_cast<int32_t*>(chose + g.E);
+    int32_t* ids = place + g.E;
+    float* weights = reinterpret_cast<float*>(ids + g.pairs);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    for (int t = wave; t < g.T; t += waves) choose(g, logits + t * g.E, ids + t * g.top_k, weights + t * g.top_k);
+    for (int i = threadIdx.x; i < g.E; i += blockDim.x) chose[i] = 0;
+    if (g.split > 1)
+        for (int i = threadIdx.x; i < (g.D + 15) / 16; i += blockDim.x) g.done[i] = 0;
+    __syncthreads();
+    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) {
+        g.ids[p] = ids[p];
+        g.weights[p] = weights[p];
+        atomicOr(chose + ids[p], 1ull << (p / g.top_k));
     }
-    return n;
+    __syncthreads();
+    const auto earlier = [&](int p, uint64_t m) { return __popcll(m & ((1ull << (p / g.top_k)) - 1)); };
+    if (wave == 0) {      // experts in the order of their first pairs
+        int n = 0, places = 0;
+        for (int b = 0; b < g.pairs; b += 64) {
+            const int p = b + lane, e = ids[min(p, g.pairs - 1)];
+            const uint64_t of = chose[e];
+            const bool leads = p < g.pairs && earlier(p, of) == 0;
+            const int count = leads ? __popcll(of) : 0, before = group_prefix_i<64>(count, lane);
+            const uint64_t m = __ballot(leads);
+            if (leads) {
+                g.groups[1 + n + lanes_below(m)] = int4{e, places + before, count, 0};
+                place[e] = places + before;
+            }
+            n += __popcll(m);
+            places += __builtin_amdgcn_readlane(before + count, 63);
+        }
+        if (lane == 0) g.groups[0] = int4{n, 0, 0, 0};
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) g.order[place[ids[p]] + earlier(p, chose[ids[p]])] = p;
+}
+
+__host__ __device__ constexpr int route_bytes(int pairs, int E) { return (pairs * 8 + E * 12 + 15) / 16 * 16; }
+
+// One workgroup: the choices, where there are many workgroups of `up` that would each have to find its expert
+__global__ __launch_bounds__(1024) void moe_route_kernel(MoeArgs g) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    route(g, g.logits, lds);
 }
 
 // LDS of `down` before h.  (All LDS here is dynamic: the kernels' limits are raised to all that a compute unit has.)
-__host__ __device__ constexpr int down_small(int T, int pairs) { return (kDownWaves * T * 68 + pairs * 12 + 4 + 15) / 16 * 16; }
+__host__ __device__ constexpr int down_small(int T, int pairs) { return (kDownWaves * T * 64 + pairs * 24 + 4 + 15) / 16 * 16; }
 // LDS of `up` before its sums
-__host__ __device__ constexpr int up_small(int T, int pairs, int E) { return (pairs * 8 + T * 4 + 4 + E * 4 + 15) / 16 * 16; }
+__host__ __device__ constexpr int up_small(int T, int pairs, int E, bool alone) {
+    return route_bytes(pairs, E) + (T * 4 + (alone ? T * E * 4 : 0) + 15) / 16 * 16;
+}
 
 // 16 * tiles hidden units of a chosen expert.  Half of the wavefronts have the gate rows, half the up rows; each half shares
 // D, and a wavefront walks its columns of one tile after the other, the next one's codes on their way.  IN_LDS: the tokens' x
@@ -195,21 +283,20 @@ template <typename XT, int NT, int GL, bool IN_LDS, bool ALONE>
 __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
     constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S, HP = Hidden<XT>::kParts, U = IN_LDS ? 4 : 2;
     extern __shared__ __align__(16) uint8_t lds[];
-    int32_t* ids = reinterpret_cast<int32_t*>(lds);                                         // [pairs]
-    float* weights = reinterpret_cast<float*>(ids + g.pairs);                               // [pairs]
-    int32_t* list = reinterpret_cast<int32_t*>(weights + g.pairs);                          // [T], then their number
-    int32_t* first_of = list + g.T + 1;                                                     // [E]
-    float* sums = reinterpret_cast<float*>(lds + up_small(g.T, g.pairs, g.E));      // [way][gate, up][tile][rows][16]
+    int32_t* list = reinterpret_cast<int32_t*>(lds + route_bytes(g.pairs, g.E));                   // [T]
+    float* sums = reinterpret_cast<float*>(lds + up_small(g.T, g.pairs, g.E, ALONE));      // [way][gate, up][tile][rows][16]
     uint16_t* xs = reinterpret_cast<uint16_t*>(sums + 2 * g.ways * g.tiles * g.rows * 16);         // [rows * parts][D padded + 8]
     const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int pair = blockIdx.y, f0 = 16 * g.tiles * blockIdx.x, half = wave & 1, way = wave >> 1;
+    const int f0 = 16 * g.tiles * blockIdx.x, half = wave & 1, way = wave >> 1;
     const int64_t fp = row_pitch(g.F), dp = row_pitch(g.D);
     const int chunks = (int)(q4_padded(g.D) / kQ4Chunk);
     const int xp = chunks * kQ4Chunk + 8;
+    const float* logits = g.logits;
     if constexpr (ALONE) {
-        float* logits = sums;      // [T][E], before the sums
+        float* made = reinterpret_cast<float*>(list + g.T);      // [T][E]
+        logits = made;
         for (int i = wave; i < g.T * g.E; i += 2 * g.ways)
-            router_rows<XT, 1>(g, static_cast<const typename XT::type*>(g.x) + i / g.E * g.ldx, i % g.E, logits + i / g.E * g.E);
+            router_rows<XT, 1>(g, static_cast<const typename XT::type*>(g.x) + i / g.E * g.ldx, i % g.E, made + i / g.E * g.E);
         for (int t = 0; t < g.T; ++t)
             for (int j = threadIdx.x; j < chunks * (kQ4Chunk / 8); j += blockDim.x) {
                 uint4 p[P];
@@ -218,14 +305,29 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
                 for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(xs + (t * P + i) * xp + 8 * j) = p[i];
             }
         __syncthreads();
-        for (int t = wave; t < g.T; t += 2 * g.ways) choose(g, logits + t * g.E, ids + t * g.top_k, weights + t * g.top_k);
-    } else {
-        for (int t = wave; t < g.T; t += 2 * g.ways) choose(g, g.logits + t * g.E, ids + t * g.top_k, weights + t * g.top_k);
     }
-    __syncthreads();
-    const int e = __builtin_amdgcn_readfirstlane(ids[pair]);
-    for (int b = 0; b < pair; b += 64)      // every wavefront by itself: the expert is an earlier pair's
-        if (__any(b + lane < pair && ids[min(b + lane, pair)] == e)) return;
+    // Every wavefront for itself (all write the same list): an expert, and the pairs that chose it
+    int e, tokens = 0;
+    if (!ALONE && g.routed) {
+        const int4 group = g.groups[1 + blockIdx.y];      // (behind the last one: of an earlier call or none, and not looked at)
+        if ((int)blockIdx.y >= g.groups[0].x) return;
+        e = __builtin_amdgcn_readfirstlane(group.x);
+        tokens = __builtin_amdgcn_readfirstlane(group.z);
+        for (int i = lane; i < tokens; i += 64) list[i] = g.order[group.y + i];
+    } else {
+        // that of pair blockIdx.y; if one of the pairs comes before it, its workgroups have the expert
+        const int pair = blockIdx.y, token = pair / g.top_k;
+        e = expert_of(g, logits + token * g.E, pair - token * g.top_k);
+#pragma unroll 4
+        for (int t = 0; t < g.T; ++t) {
+            const int before = experts_before(g, logits + t * g.E, e, logits[t * g.E + e]);
+            if (before >= g.top_k) continue;
+            if (t < token) return;
+            if (lane == 0) list[tokens] = t * g.top_k + before;
+            ++tokens;
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int64_t pitch = q4_row_bytes(g.D), groups = (g.D + (32 << GL) - 1) >> (5 + GL);
     const int64_t first = ((int64_t)e * 2 + half) * g.F;      // of the expert's gate or up rows
     Q4Walk<XT::kHalf, NT, 1, GL, U> walk;
@@ -234,23 +336,25 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
         walk.load(way * U);
     };
     start(0);
-    // x of all tokens while the first codes are on their way
-    if constexpr (IN_LDS && !ALONE) rows_to_lds(xs, xp, g.xp, dp, g.T * P, chunks * (kQ4Chunk / 8), g.magic_x, chunks * (kQ4Chunk / 8));
-    if (wave == 0) {
-        const int n = pairs_of(ids, g.pairs, pair, e, list);
-        if (lane == 0) list[g.T] = n;
-    }
-    __syncthreads();
-    const int tokens = list[g.T];
     constexpr int V = 4 / S;
     const int out = g.tiles * g.rows * 16;      // sums of a wavefront
-    for (int n0 = 0; n0 < tokens; n0 += NT * TPT) {
-        const int here = min(tokens - n0, NT * TPT);
+    for (int n0 = 0; n0 < tokens; n0 += g.rows) {
+        const int here = min(tokens - n0, g.rows);
+        if constexpr (IN_LDS && !ALONE) {      // x of the tokens while the first codes are on their way
+            const auto from = [&](int row) {
+                const int n = row / P;
+                return g.xp + ((int64_t)(list[n0 + n] / g.top_k) * P + (row - n * P)) * dp;
+            };
+            rows_to_lds(xs, xp, from, here * P, chunks * (kQ4Chunk / 8), g.magic_x, chunks * (kQ4Chunk / 8));
+            __syncthreads();
+        }
         std::conditional_t<IN_LDS, LdsRowsOfX<NT>, RowsOfX<NT, U, false>> x;
         if constexpr (IN_LDS) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)      // rows without a token repeat the last one
-                x.at[t] = xs + (list[n0 + min(t * TPT + r / S, here - 1)] / g.top_k * P + min(r % S, P - 1)) * xp + 8 * kb;
+            for (int t = 0; t < NT; ++t) {      // rows without a token repeat the last one
+                const int n = min(t * TPT + r / S, here - 1);
+                x.at[t] = xs + ((ALONE ? list[n0 + n] / g.top_k : n) * P + min(r % S, P - 1)) * xp + 8 * kb;
+            }
         } else {
             x.kb = kb;
             x.columns = chunks * kQ4Chunk;
@@ -311,28 +415,8 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
         }
         __syncthreads();
     }
-    if (blockIdx.x || pair) return;
-    // the first workgroup says what was chosen, and for `down` the first pair of every chosen expert, and their number
-    for (int i = threadIdx.x; i < g.E; i += blockDim.x) first_of[i] = g.pairs;
-    if (g.split > 1)
-        for (int i = threadIdx.x; i < (g.D + 15) / 16; i += blockDim.x) g.done[i] = 0;
-    __syncthreads();
-    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) {
-        g.ids[p] = ids[p];
-        g.weights[p] = weights[p];
-        atomicMin(first_of + ids[p], p);
-    }
-    __syncthreads();
-    if (wave) return;
-    int n = 0;
-    for (int b = 0; b < g.pairs; b += 64) {
-        const int p = b + lane;
-        const bool leads = p < g.pairs && first_of[ids[min(p, g.pairs - 1)]] == p;
-        const uint64_t m = __ballot(leads);
-        if (leads) g.leaders[1 + n + lanes_below(m)] = p;
-        n += __popcll(m);
-    }
-    if (lane == 0) g.leaders[0] = n;
+    if (blockIdx.x || blockIdx.y || (!ALONE && g.routed)) return;
+    route(g, logits, lds);      // the first workgroup says what was chosen
 }
 
 // Workgroup z of a tile has a part of F, two chunks at least; a wavefront's work is one step of one chosen expert after the
@@ -343,11 +427,10 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
     constexpr int P = Hidden<XT>::kParts, S = Hidden<XT>::kSlots, TPT = 16 / S, V = 4 / S, U = 2;
     extern __shared__ __align__(16) uint8_t lds[];
     float* sums = reinterpret_cast<float*>(lds);                                     // [wave][T][16]
-    int32_t* ids = reinterpret_cast<int32_t*>(sums + kDownWaves * g.T * 16);         // [pairs]
-    float* weights = reinterpret_cast<float*>(ids + g.pairs);                        // [pairs]
-    int32_t* leaders = reinterpret_cast<int32_t*>(weights + g.pairs);                // [pairs]
-    int32_t* lists = leaders + g.pairs;                                              // [wave][T]
-    int32_t* found = lists + kDownWaves * g.T;
+    int4* groups = reinterpret_cast<int4*>(sums + kDownWaves * g.T * 16);            // [pairs at most]
+    int32_t* order = reinterpret_cast<int32_t*>(groups + g.pairs);                   // [pairs]
+    float* weights = reinterpret_cast<float*>(order + g.pairs);                      // [pairs], in that order
+    int32_t* found = reinterpret_cast<int32_t*>(weights + g.pairs);
     uint16_t* xs = reinterpret_cast<uint16_t*>(lds + down_small(g.T, g.pairs));      // [pairs * parts][columns + 8]
     const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int d0 = 16 * blockIdx.x;
@@ -355,37 +438,33 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
     const int chunks = (int)(q4_padded(g.F) / kQ4Chunk), first_chunk = blockIdx.y * g.part_chunks;
     const int end = min(chunks, first_chunk + g.part_chunks), steps = (end - first_chunk + U - 1) / U;
     const int xp = g.part_chunks * kQ4Chunk + 8;
-    if constexpr (IN_LDS)
-        rows_to_lds(xs, xp, g.hp + first_chunk * kQ4Chunk, fp, g.pairs * P, g.part_chunks * (kQ4Chunk / 8), g.magic_h,
-                    (end - first_chunk) * (kQ4Chunk / 8));
-    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) {
-        ids[p] = g.ids[p];
-        weights[p] = g.weights[p];
-        leaders[p] = g.leaders[1 + p];      // (behind the last one: not looked at)
-    }
-    const int experts = g.leaders[0];
-    for (int i = threadIdx.x; i < kDownWaves * g.T * 16; i += blockDim.x) sums[i] = 0.f;
-    __syncthreads();
-    const int items = experts * steps;
-    const int64_t pitch = q4_row_bytes(g.F), groups = (g.F + (32 << GL) - 1) >> (5 + GL);
+    const int experts = __builtin_amdgcn_readfirstlane(g.groups[0].x), items = experts * steps;
+    const int64_t pitch = q4_row_bytes(g.F), row_groups = (g.F + (32 << GL) - 1) >> (5 + GL);
     float* mine = sums + wave * g.T * 16;
-    int32_t* list = lists + wave * g.T;
     Q4Walk<false, 1, 1, GL, U> walk;
-    int next = -1, listed = -1, tokens = 0;      // pairs that stand for the expert being loaded, and that of the list
-    const auto load = [&](int item) {
-        next = __builtin_amdgcn_readfirstlane(leaders[item / steps]);
-        const int64_t e = __builtin_amdgcn_readfirstlane(ids[next]);
-        walk.tile(0, g.w2 + e * g.D * pitch, g.s2 + e * g.D * groups, d0, g.D, g.F, lane);
+    const auto load = [&](int item, int4 group) {
+        const int64_t e = __builtin_amdgcn_readfirstlane(group.x);
+        walk.tile(0, g.w2 + e * g.D * pitch, g.s2 + e * g.D * row_groups, d0, g.D, g.F, lane);
         walk.load(first_chunk + item % steps * U);
     };
-    if (wave < items) load(wave);
+    if (wave < items) load(wave, g.groups[1 + wave / steps]);
+    if constexpr (IN_LDS)
+        rows_to_lds(xs, xp, [&](int row) { return g.hp + first_chunk * kQ4Chunk + row * fp; }, g.pairs * P, g.part_chunks * (kQ4Chunk / 8),
+                    g.magic_h, (end - first_chunk) * (kQ4Chunk / 8));
+    for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) {
+        const int pair = g.order[p];
+        order[p] = pair;
+        weights[p] = g.weights[pair];
+        if (p < experts) groups[p] = g.groups[1 + p];
+    }
+    for (int i = threadIdx.x; i < kDownWaves * g.T * 16; i += blockDim.x) sums[i] = 0.f;
+    __syncthreads();
     for (int item = wave; item < items; item += kDownWaves) {
         const int c = first_chunk + item % steps * U;
-        if (next != listed) {
-            listed = next;
-            tokens = pairs_of(ids, g.pairs, listed, ids[listed], list);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the list is written by some lanes and read by others
-        }
+        const int4 group = groups[item / steps];
+        const int32_t* list = order + group.y;
+        const float* share = weights + group.y;
+        const int tokens = __builtin_amdgcn_readfirstlane(group.z);
         walk.take();
         uint32_t sc[1][decltype(walk)::kWords][4];
         walk.spread(sc);
@@ -402,19 +481,18 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) x.fetch(c, u);
-            if (n0 + TPT >= tokens && item + kDownWaves < items) load(item + kDownWaves);
+            if (n0 + TPT >= tokens && item + kDownWaves < items) load(item + kDownWaves, groups[(item + kDownWaves) / steps]);
             f32x4 acc[1][1] = {};
             walk.template eat<0, U>(c, end, x, sc, acc);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int n = kb * V + v;
                 if (n >= here) continue;
-                const int pair = list[n0 + n];
                 float sum;
                 if constexpr (S == 4) sum = acc[0][0][0] + (acc[0][0][1] + acc[0][0][2]);
                 else sum = acc[0][0][2 * v] + acc[0][0][2 * v + 1];
-                float* to = mine + pair / g.top_k * 16 + r;
-                *to = fmaf(weights[pair], sum, *to);
+                float* to = mine + list[n0 + n] / g.top_k * 16 + r;
+                *to = fmaf(share[n0 + n], sum, *to);
             }
         }
     }
@@ -445,29 +523,67 @@ int launch_up_rows(const MoeArgs& g, size_t lds, hipStream_t st) {
         const int rc = ensure_lds_limit(Reg::reg, st);
         if (rc != BS_OK) return rc;
     }
-    const dim3 grid((unsigned)((q4_padded(g.F) + 16 * g.tiles - 1) / (16 * g.tiles)), (unsigned)g.pairs);
+    const dim3 grid((unsigned)((q4_padded(g.F) + 16 * g.tiles - 1) / (16 * g.tiles)), (unsigned)(g.routed && g.E < g.pairs ? g.E : g.pairs));
     hipLaunchKernelGGL((moe_up_kernel<XT, NT, GL, IN_LDS, ALONE>), grid, dim3(128 * g.ways), lds, st, g);
     return hip_status(hipGetLastError());
+}
+
+// Tiles of 16 hidden units for a workgroup of `up`, two of which share a compute unit.  What the busiest one does: its bytes at
+// the rate of reads, 4 us to begin and end each round of 512 workgroups, 3 where it has one only.  64 experts of 2048 x 1024, 32
+// of them chosen: 23.3 / 20.2 / 17.6 / 20.1 / 17.2 us with 1 / 2 / 4 / 5 / 8; 8 of 944 x 4094: 31 / 20.6 / 14.9 / 17 / 18.8.
+int tiles_for(double experts, int64_t tiles, double bytes, int lds) {
+    int best = 1;
+    double least = 0;
+    for (int t = 1; t <= 16 && (t == 1 || t * lds <= 32 * 1024); ++t) {
+        const double wgs = experts * ((tiles + t - 1) / t);
+        const double cost = std::ceil(wgs / 256) * t * bytes / 21.5e3 + 4 * std::ceil(wgs / 512) + (wgs <= 256 ? 3 : 0);
+        if (t == 1 || cost < least) { best = t; least = cost; }
+    }
+    return best;
 }
 
 template <typename XT, int GL>
 int launch_up(MoeArgs g, hipStream_t st) {
     constexpr int TPT = 16 / XT::kSlots;
-    // four tiles a workgroup where that still leaves two workgroups for a compute unit
-    g.tiles = g.pairs * (q4_padded(g.F) / 16) >= 2048 ? 4 : 1;
-    g.rows = g.T < TPT ? g.T : g.T < 2 * TPT ? g.T : 2 * TPT;
-    const int small = up_small(g.T, g.pairs, g.E), sums = 2 * g.ways * g.tiles * g.rows * 64;
-    const size_t lds_x = (size_t)g.rows * XT::kParts * (q4_padded(g.D) + 8) * 2;
+    const size_t row = (size_t)XT::kParts * (q4_padded(g.D) + 8) * 2;      // of x in LDS
+    const double experts = g.E * (1 - std::pow(1 - (double)g.top_k / g.E, g.T));
+    g.tiles = tiles_for(experts, q4_padded(g.F) / 16, 32.0 * (q4_row_bytes(g.D) + 2 * q4_groups(g.D, 32 << GL)), 2 * g.ways * std::min(g.T, TPT) * 64);
+    const auto sizes = [&](int rows, bool alone, size_t& small, size_t& sums) {
+        g.rows = g.T < rows ? g.T : rows;
+        small = up_small(g.T, g.pairs, g.E, alone);
+        sums = (size_t)2 * g.ways * g.tiles * g.rows * 64;
+    };
+    size_t small, sums;
+    sizes(TPT, true, small, sums);
     // The logits by every workgroup itself where they are few (1 token, 8 experts, 1500 columns: 14.7 us in two kernels against
     // 18 in three); 64 experts of 2048 columns would have each read 256 KB.
-    if (g.T <= TPT && lds_x <= kLdsOfX && (int64_t)g.T * g.E * g.D <= 32768 && g.T * g.E * 4 <= sums)
-        return launch_up_rows<XT, GL, 1, true, true>(g, small + sums + lds_x, st);
+    if (g.T <= TPT && g.T * row <= 40 * 1024 && g.T * g.E <= 4 * g.ways && (int64_t)g.T * g.E * g.D <= 32768)
+        return launch_up_rows<XT, GL, 1, true, true>(g, small + sums + g.T * row, st);
+    g.routed = g.T >= 4;
     hipLaunchKernelGGL(moe_logits_kernel<XT>, dim3(g.T, (g.E + 15) / 16), dim3(256), 0, st, g);
-    const int rc = hip_status(hipGetLastError());
+    int rc = hip_status(hipGetLastError());
     if (rc != BS_OK) return rc;
-    if (g.T > TPT) return launch_up_rows<XT, GL, 2, false, false>(g, small + sums, st);
-    return lds_x <= kLdsOfX ? launch_up_rows<XT, GL, 1, true, false>(g, small + sums + lds_x, st)
-                            : launch_up_rows<XT, GL, 1, false, false>(g, small + sums, st);
+    if (g.routed) {
+        const int lds = route_bytes(g.pairs, g.E);
+        hipLaunchKernelGGL(moe_route_kernel, dim3(1), dim3(g.T < 4 ? 256 : g.T < 16 ? 64 * g.T : 1024), lds, st, g);
+        rc = hip_status(hipGetLastError());
+        if (rc != BS_OK) return rc;
+    }
+    // x in LDS where most experts' tokens fit there at once, or in three passes over the expert's codes: 12 tokens of 2322 x 2716 in
+    // fp32, 7 of 8 experts each, 45 us in three passes, 75 with x from memory in two
+    for (const size_t room : {kLdsOfX, 2 * kLdsOfX}) {
+        const int fit = (int)(room / row < TPT ? room / row : TPT);
+        const int pairs = room == kLdsOfX ? 2 * g.pairs : g.pairs / 3;
+        if (fit < 1 || (fit < g.T && pairs > g.E * fit)) continue;
+        sizes(fit, false, small, sums);
+        return launch_up_rows<XT, GL, 1, true, false>(g, small + sums + g.rows * row, st);
+    }
+    if (g.T > TPT) {
+        sizes(2 * TPT, false, small, sums);
+        return launch_up_rows<XT, GL, 2, false, false>(g, small + sums, st);
+    }
+    sizes(TPT, false, small, sums);
+    return launch_up_rows<XT, GL, 1, false, false>(g, small + sums, st);
 }
 
 template <typename XT, int GL, bool IN_LDS>
@@ -501,7 +617,7 @@ int launch_group(const MoeArgs& g, int group, hipStream_t st) {
 
 // the workspace: x's rows, h's rows, logits, sums of down's workgroups, their counts
 struct Space {
-    size_t h, logits, leaders, parts, done, all;
+    size_t h, logits, groups, order, parts, done, all;
     int split, part_chunks;
 };
 
@@ -515,7 +631,8 @@ Space space_for(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
     s.split = 1;
     s.part_chunks = (int)chunks;
     while (s.split < 16 && s.part_chunks > 2) {
-        const bool fits = pairs * parts * (s.part_chunks * kQ4Chunk + 8) * 2 <= (int64_t)kLdsOfH;
+        const auto room = [&](int64_t n) { return pairs * parts * (n * kQ4Chunk + 8) * 2; };
+        const bool fits = room(s.part_chunks) <= (int64_t)kLdsOfH || room(2) > (int64_t)kLdsOfH;      // or no split would make it fit
         const int64_t steps = (s.part_chunks + 1) / 2 * experts;
         if (fits && (tiles * s.split >= 512 || steps < 4 * kDownWaves)) break;
         s.split *= 2;
@@ -525,8 +642,9 @@ Space space_for(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
     const auto up16 = [](size_t n) { return (n + 15) / 16 * 16; };
     s.h = (size_t)T * (dtype == BS_F32 ? 3 : 1) * row_pitch(D) * 2;
     s.logits = s.h + (size_t)pairs * parts * row_pitch(F) * 2;
-    s.leaders = s.logits + up16((size_t)T * E * 4);
-    s.parts = s.leaders + up16((size_t)(pairs + 1) * 4);
+    s.groups = s.logits + up16((size_t)T * E * 4);
+    s.order = s.groups + (size_t)(pairs + 1) * 16;
+    s.parts = s.order + up16((size_t)pairs * 4);
     s.done = s.parts + (s.split > 1 ? (size_t)tiles * s.split * T * 64 : 0);
     s.all = s.done + (s.split > 1 ? (size_t)tiles * 4 : 0);
     return s;
@@ -560,7 +678,8 @@ int launch_tokens(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, c
     g.done = reinterpret_cast<uint32_t*>(base + s.done);
     g.split = s.split;
     g.part_chunks = s.part_chunks;
-    g.leaders = reinterpret_cast<int32_t*>(base + s.leaders);
+    g.groups = reinterpret_cast<int4*>(base + s.groups);
+    g.order = reinterpret_cast<int32_t*>(base + s.order);
     g.magic_x = magic_u32((uint32_t)(q4_padded(D) / 8));
     g.magic_h = magic_u32((uint32_t)(s.part_chunks * (kQ4Chunk / 8)));
     const int64_t steps = (q4_padded(D) / kQ4Chunk + 1) / 2;
