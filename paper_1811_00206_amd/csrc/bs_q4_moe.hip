@@ -270,7 +270,7 @@ __global__ __launch_bounds__(1024) void moe_route_kernel(MoeArgs g) {
 }
 
 // LDS of `down` before h.  (All LDS here is dynamic: the kernels' limits are raised to all that a compute unit has.)
-__host__ __device__ constexpr int down_small(int T, int pairs) { return (kDownWaves * T * 64 + pairs * 24 + 4 + 15) / 16 * 16; }
+__host__ __device__ constexpr int down_small(int T, int pairs) { return (kDownWaves * T * 64 + pairs * 28 + 4 + 15) / 16 * 16; }
 // LDS of `up` before its sums
 __host__ __device__ constexpr int up_small(int T, int pairs, int E, bool alone) {
     return route_bytes(pairs, E) + (T * 4 + (alone ? T * E * 4 : 0) + 15) / 16 * 16;
@@ -429,7 +429,8 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
     float* sums = reinterpret_cast<float*>(lds);                                     // [wave][T][16]
     int4* groups = reinterpret_cast<int4*>(sums + kDownWaves * g.T * 16);            // [pairs at most]
     int32_t* order = reinterpret_cast<int32_t*>(groups + g.pairs);                   // [pairs]
-    float* weights = reinterpret_cast<float*>(order + g.pairs);                      // [pairs], in that order
+    int32_t* places = order + g.pairs;                                               // [pairs], in that order: of the token's sums
+    float* weights = reinterpret_cast<float*>(places + g.pairs);                     // [pairs], in that order
     int32_t* found = reinterpret_cast<int32_t*>(weights + g.pairs);
     uint16_t* xs = reinterpret_cast<uint16_t*>(lds + down_small(g.T, g.pairs));      // [pairs * parts][columns + 8]
     const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -442,28 +443,32 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
     const int64_t pitch = q4_row_bytes(g.F), row_groups = (g.F + (32 << GL) - 1) >> (5 + GL);
     float* mine = sums + wave * g.T * 16;
     Q4Walk<false, 1, 1, GL, U> walk;
-    const auto load = [&](int item, int4 group) {
+    const auto load = [&](int step, int4 group) {
         const int64_t e = __builtin_amdgcn_readfirstlane(group.x);
         walk.tile(0, g.w2 + e * g.D * pitch, g.s2 + e * g.D * row_groups, d0, g.D, g.F, lane);
-        walk.load(first_chunk + item % steps * U);
+        walk.load(first_chunk + step * U);
     };
-    if (wave < items) load(wave, g.groups[1 + wave / steps]);
+    // (the next item of a wavefront is found by counting: divisions are 25 instructions each)
+    int expert = wave / steps, step = wave - expert * steps;
+    if (wave < items) load(step, g.groups[1 + expert]);
     if constexpr (IN_LDS)
         rows_to_lds(xs, xp, [&](int row) { return g.hp + first_chunk * kQ4Chunk + row * fp; }, g.pairs * P, g.part_chunks * (kQ4Chunk / 8),
                     g.magic_h, (end - first_chunk) * (kQ4Chunk / 8));
     for (int p = threadIdx.x; p < g.pairs; p += blockDim.x) {
         const int pair = g.order[p];
         order[p] = pair;
+        places[p] = pair / g.top_k * 16;
         weights[p] = g.weights[pair];
         if (p < experts) groups[p] = g.groups[1 + p];
     }
     for (int i = threadIdx.x; i < kDownWaves * g.T * 16; i += blockDim.x) sums[i] = 0.f;
     __syncthreads();
     for (int item = wave; item < items; item += kDownWaves) {
-        const int c = first_chunk + item % steps * U;
-        const int4 group = groups[item / steps];
-        const int32_t* list = order + group.y;
+        const int c = first_chunk + step * U;
+        const int4 group = groups[expert];
+        const int32_t *list = order + group.y, *place = places + group.y;
         const float* share = weights + group.y;
+        for (step += kDownWaves; step >= steps; step -= steps) ++expert;
         const int tokens = __builtin_amdgcn_readfirstlane(group.z);
         walk.take();
         uint32_t sc[1][decltype(walk)::kWords][4];
@@ -481,7 +486,7 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) x.fetch(c, u);
-            if (n0 + TPT >= tokens && item + kDownWaves < items) load(item + kDownWaves, groups[(item + kDownWaves) / steps]);
+            if (n0 + TPT >= tokens && item + kDownWaves < items) load(step, groups[expert]);
             f32x4 acc[1][1] = {};
             walk.template eat<0, U>(c, end, x, sc, acc);
 #pragma unroll
@@ -491,7 +496,7 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
                 float sum;
                 if constexpr (S == 4) sum = acc[0][0][0] + (acc[0][0][1] + acc[0][0][2]);
                 else sum = acc[0][0][2 * v] + acc[0][0][2 * v + 1];
-                float* to = mine + list[n0 + n] / g.top_k * 16 + r;
+                float* to = mine + place[n0 + n] + r;
                 *to = fmaf(share[n0 + n], sum, *to);
             }
         }

@@ -137,6 +137,27 @@ def test_graph_replays():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("T,D,F,E,top_k,group,dtype", [(9, 192, 1100, 60, 8, 32, "f32"), (70, 130, 96, 12, 4, 64, "f16")])
+def test_graph_replays_of_many_tokens(T, D, F, E, top_k, group, dtype):
+    """Choices in a kernel of their own, several workgroups for a tile of outputs, more than 64 tokens: counted anew on every replay."""
+    p = layer(T, D, F, E, group, dtype, 18)
+    bs.bs_init()
+    x, router = p["x"].cuda(), p["router"].cuda()
+    size = bs.bs_q4_moe_workspace_bytes(bs._TYPES[TYPES[dtype]], T, D, F, E, top_k, group)
+    workspace = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = bs.bs_q4_moe(x, router, p["c1"], p["s1"], p["c2"], p["s2"], group, top_k, workspace=workspace)
+    for seed in range(3):
+        p["x"] = (torch.randint(-8, 9, (T, D), generator=torch.Generator().manual_seed(seed)) / 8).to(TYPES[dtype])
+        x.copy_(p["x"])
+        graph.replay()
+        torch.cuda.synchronize()
+        check(out, definition(p, top_k, True), dtype)
+        for a, b in zip(out, call(p, top_k, True)):
+            assert torch.equal(a, b)
+
+
 def test_refusals():
     p = layer(2, 64, 32, 4, 32, "f32", 1)
     x, r = p["x"].cuda(), p["router"].cuda()
