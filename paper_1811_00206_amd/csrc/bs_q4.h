@@ -305,8 +305,7 @@ struct LdsRowsOfX {
 // columns of it (tile by tile, `chunks` chunks each)
 template <int NT, int FETCH>
 struct TilesOfX {
-    const uint16_t* at;      // the lane's piece of tile 0, chunk 0
-    int64_t tile;            // elements between tiles
+    const uint16_t* at[NT];      // the lane's piece of a tile's chunk 0
     int last;
     uint4 v[NT][FETCH][4];
     __device__ __forceinline__ void fetch(int c, int u) {
@@ -314,7 +313,7 @@ struct TilesOfX {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[t][u % FETCH][i] = *reinterpret_cast<const uint4*>(at + t * tile + (cc * 4 + i) * 512);
+            for (int i = 0; i < 4; ++i) v[t][u % FETCH][i] = *reinterpret_cast<const uint4*>(at[t] + (cc * 4 + i) * 512);
     }
     __device__ __forceinline__ uint4 operator()(int t, int, int u, int i) const { return v[t][u % FETCH][i]; }
 };

@@ -118,8 +118,11 @@ __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(
     constexpr int kFetch = NT <= 2 ? U : 1;
     if constexpr (TILED) {
         TilesOfX<NT, kFetch> x;
-        x.tile = (int64_t)chunks * 2048;
-        x.at = static_cast<const uint16_t*>(g.x) + blockIdx.y * NT * x.tile + 8 * lane;
+        // (tiles of 16 virtual rows that no vector is in were not made: the last one is read instead, for rows that nobody stores)
+        const int last = (int)((g.N + TPT - 1) / TPT) - 1;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            x.at[t] = static_cast<const uint16_t*>(g.x) + (int64_t)min((int)blockIdx.y * NT + t, last) * chunks * 2048 + 8 * lane;
         x.last = chunks - 1;
         walk.load(first + wave * U);
         walk.template rest<kFetch>(first + wave * U, g.ways, end, x, acc);

@@ -195,6 +195,19 @@ def test_gemv_on_another_stream_and_in_a_graph():
         assert torch.equal(out, eager)
 
 
+@pytest.mark.parametrize("dtype,N", [("f32", 17), ("f32", 24), ("f32", 41), ("f16", 33), ("bf16", 70), ("bf16", 65)])
+def test_gemv_whose_last_tiles_have_no_vector(dtype, N):
+    """Groups of four tiles, the last of which are empty, in a workspace that ends where it says it does."""
+    M, K, group = 70, 1300, 32
+    codes, scales, W = packed(M, K, group, N)
+    x = torch.randn((N, K), generator=torch.Generator().manual_seed(N)).to(TYPES[dtype])
+    need = bs.bs_q4_gemv_workspace_bytes(bs._TYPES[TYPES[dtype]], M, K, group, N)
+    room = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    y = bs.bs_q4_gemv(codes, scales, group, x.cuda(), workspace=room[:need])
+    check_product(y, W, x)
+    assert bool((room[need:] == 255).all())
+
+
 def test_gemv_whose_workgroups_share_k_in_a_graph():
     """Few rows, many columns, several vectors: sums are joined, and counted anew on every replay."""
     M, K, N, group = 40, 12000, 9, 64
