@@ -534,14 +534,19 @@ int launch_up_rows(const MoeArgs& g, size_t lds, hipStream_t st) {
 }
 
 // Tiles of 16 hidden units for a workgroup of `up`, two of which share a compute unit.  What the busiest one does: its bytes at
-// the rate of reads, 4 us to begin and end each round of 512 workgroups, 3 where it has one only.  64 experts of 2048 x 1024, 32
-// of them chosen: 23.3 / 20.2 / 17.6 / 20.1 / 17.2 us with 1 / 2 / 4 / 5 / 8; 8 of 944 x 4094: 31 / 20.6 / 14.9 / 17 / 18.8.
-int tiles_for(double experts, int64_t tiles, double bytes, int lds) {
+// the rate of reads, 4 us to begin and end each round of 512 workgroups, 3 where it has one only.  How many experts several tokens
+// choose is not known here: `experts`, their expected number, or, at a weight of 0.3, a tenth more (the same launch takes 28.7 us with
+// 46 chosen experts and 42.5 with 47, where those need a second round).  64 experts of 2048 x 1024, 32 of them chosen: 23.3 / 20.2 /
+// 17.6 / 20.1 / 17.2 us with 1 / 2 / 4 / 5 / 8; 8 of 944 x 4094: 31 / 20.6 / 14.9 / 17 / 18.8.
+int tiles_for(double experts, bool known, int64_t tiles, double bytes, int lds) {
     int best = 1;
     double least = 0;
     for (int t = 1; t <= 16 && (t == 1 || t * lds <= 32 * 1024); ++t) {
-        const double wgs = experts * ((tiles + t - 1) / t);
-        const double cost = std::ceil(wgs / 256) * t * bytes / 21.5e3 + 4 * std::ceil(wgs / 512) + (wgs <= 256 ? 3 : 0);
+        const auto time = [&](double chosen) {
+            const double wgs = chosen * ((tiles + t - 1) / t);
+            return std::ceil(wgs / 256) * t * bytes / 21.5e3 + 4 * std::ceil(wgs / 512) + (wgs <= 256 ? 3 : 0);
+        };
+        const double cost = known ? time(experts) : 0.7 * time(experts) + 0.3 * time(1.1 * experts);
         if (t == 1 || cost < least) { best = t; least = cost; }
     }
     return best;
@@ -552,7 +557,7 @@ int launch_up(MoeArgs g, hipStream_t st) {
     constexpr int TPT = 16 / XT::kSlots;
     const size_t row = (size_t)XT::kParts * (q4_padded(g.D) + 8) * 2;      // of x in LDS
     const double experts = g.E * (1 - std::pow(1 - (double)g.top_k / g.E, g.T));
-    g.tiles = tiles_for(experts, q4_padded(g.F) / 16, 32.0 * (q4_row_bytes(g.D) + 2 * q4_groups(g.D, 32 << GL)), 2 * g.ways * std::min(g.T, TPT) * 64);
+    g.tiles = tiles_for(experts, g.T == 1, q4_padded(g.F) / 16, 32.0 * (q4_row_bytes(g.D) + 2 * q4_groups(g.D, 32 << GL)), 2 * g.ways * std::min(g.T, TPT) * 64);
     const auto sizes = [&](int rows, bool alone, size_t& small, size_t& sums) {
         g.rows = g.T < rows ? g.T : rows;
         small = up_small(g.T, g.pairs, g.E, alone);
