@@ -17,8 +17,9 @@
 // bfloat16 parts for 16-bit activations (16 leading bits: their rounding is not seen behind the output's) and in three (all 24
 // bits) for fp32.
 //
-// Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 42 us (logits 6.4, route 4.7, up 18 to 21, down 15; 18.4
-// at the rate of a copy).  16 tokens, 8 each: up 31, down 30.  One token of 1500 x 1500 in fp32, 2 of 8: up 10.3, down 5.6.
+// Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 38 to 42 us (logits 6.5, route 4.8, up 18 to 22 as 32 or
+// more experts are chosen, down 14.6; 18.4 at the rate of reads).  16 tokens, 8 each: up 31, down 30.  One token of 1500 x 1500 in
+// fp32, 2 of 8: 14.9 us, up 10, down 5.5.
 #include "bs_q4.h"
 
 #include <algorithm>
