@@ -254,11 +254,6 @@ struct Q4Walk {
             }
         }
     }
-    template <int FETCH, typename X>
-    __device__ __forceinline__ void walk(int first, int stride, int end, X& x, f32x4 (&acc)[R][NT]) {
-        load(first * U);
-        rest<FETCH>(first * U, stride, end, x, acc);
-    }
 };
 
 __device__ __forceinline__ uint4 bits8(const uint16_t* row, int64_t k, int64_t K);

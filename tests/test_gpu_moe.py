@@ -83,6 +83,19 @@ def test_layer(T, D, F, E, top_k, group, renormalise, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,D,F,E,top_k,renormalise", [(1, 300, 70, 300, 5, False), (2, 128, 90, 65, 6, True), (3, 64, 64, 1024, 32, True),
+                                                       (3, 700, 40, 64, 8, False), (4, 64, 33, 1000, 32, True), (2, 4096, 48, 16, 2, True)])
+def test_few_tokens_of_many_experts(T, D, F, E, top_k, renormalise, dtype):
+    """Choices with and without a kernel of their own, of more experts than a wavefront has lanes; equal logits among them."""
+    p = layer(T, D, F, E, 32, dtype, T + D + E)
+    p["router"][1::3] = p["router"][0]
+    got = call(p, top_k, renormalise)
+    check(got, definition(p, top_k, renormalise), dtype)
+    for a, b in zip(got, call(p, top_k, renormalise)):
+        assert torch.equal(a, b), "another call, other bits"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_all_tokens_of_one_expert_and_ties(dtype):
     """Every token wants the same experts, whose logits are equal: the lower numbers win."""
     p = layer(20, 64, 96, 7, 32, dtype, 3)
