@@ -1,6 +1,6 @@
 // A mixture-of-experts layer on 4-bit expert matrices for a few tokens (bs.h: bs_q4_moe), 64 at a time, in two to four kernels:
 //
-//   logits  a wavefront per token and four experts: router logits; and the token's activations as virtual rows (bs_q4.h),
+//   logits  a wavefront per token and expert: router logits; and the token's activations as virtual rows (bs_q4.h),
 //           padded with zeros, for `up` to read in whole pieces
 //   route   one workgroup: every token's top_k experts and their weights, and the pairs (token, choice) expert by expert
 //   up      some tiles of 16 hidden units of a chosen expert: gate and up rows against all tokens that chose it,
@@ -17,7 +17,7 @@
 // bfloat16 parts for 16-bit activations (16 leading bits: their rounding is not seen behind the output's) and in three (all 24
 // bits) for fp32.
 //
-// Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 38 to 42 us (logits 6.5, route 4.8, up 18 to 22 as 32 or
+// Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 38 to 42 us (logits 4.8, route 4.8, up 18 to 22 as 32 or
 // more experts are chosen, down 14.6; 18.4 at the rate of reads).  16 tokens, 8 each: up 31, down 30.  One token of 1500 x 1500 in
 // fp32, 2 of 8: 14.9 us, up 10, down 5.5.
 #include "bs_q4.h"
@@ -64,31 +64,22 @@ struct MoeArgs {
     int ways, tiles, rows;       // rows: tokens whose sums a wavefront of `up` keeps
 };
 
-// one wavefront: EB router rows (those that there are) times a token's activations
-template <typename XT, int EB>
-__device__ __forceinline__ void router_rows(const MoeArgs& g, const typename XT::type* x, int e, float* logits) {
-    using T = typename XT::type;
+// one wavefront: a router row times a token's activations
+template <typename XT>
+__device__ __forceinline__ void router_row(const MoeArgs& g, const typename XT::type* x, int e, float* logit) {
     const int lane = threadIdx.x & 63;
-    float sum[EB] = {};
-    const T* row[EB];
-#pragma unroll
-    for (int i = 0; i < EB; ++i) row[i] = static_cast<const T*>(g.router) + (int64_t)min(e + i, g.E - 1) * g.D;
+    const typename XT::type* row = static_cast<const typename XT::type*>(g.router) + (int64_t)e * g.D;
+    float sum = 0.f;
 #pragma unroll 4
     for (int k0 = 0; k0 < g.D; k0 += 512) {
-        float a[8], w[EB][8];
+        float a[8], w[8];
         load8<XT>(x, k0 + 8 * lane, g.D, a);
+        load8<XT>(row, k0 + 8 * lane, g.D, w);
 #pragma unroll
-        for (int i = 0; i < EB; ++i) load8<XT>(row[i], k0 + 8 * lane, g.D, w[i]);
-#pragma unroll
-        for (int i = 0; i < EB; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum[i] = fmaf(a[j], w[i][j], sum[i]);
+        for (int j = 0; j < 8; ++j) sum = fmaf(a[j], w[j], sum);
     }
-#pragma unroll
-    for (int i = 0; i < EB; ++i) {
-        const float s = sum_of_wave(sum[i]);
-        if (lane == 0 && e + i < g.E) logits[e + i] = s;
-    }
+    sum = sum_of_wave(sum);
+    if (lane == 0) *logit = sum;
 }
 
 // One wavefront: a token's top_k experts and their weights.  Up to 64 experts are a lane's each: the largest logit of the free
@@ -184,13 +175,15 @@ __device__ __forceinline__ int expert_of(const MoeArgs& g, const float* logits, 
     return __builtin_amdgcn_readfirstlane((int)index_of_key(last));
 }
 
-// blockIdx: token, 16 experts.  A wavefront has four of them, and the first workgroup of a token its virtual rows.
+// blockIdx: token, four experts, a wavefront's each; and the first workgroup of a token has its virtual rows.  (Four experts a
+// wavefront read less of x and are slower: 7 tokens, 64 experts of 2048 columns 6.6 us instead of 4.8, 64 tokens of 1024 experts of
+// 512 19.4 instead of 16.)
 template <typename XT>
 __global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs g) {
-    constexpr int P = XT::kParts, EB = 4;
-    const int t = blockIdx.x, e = blockIdx.y * 16 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * EB;
+    constexpr int P = XT::kParts;
+    const int t = blockIdx.x, e = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const typename XT::type* x = static_cast<const typename XT::type*>(g.x) + t * g.ldx;
-    if (e < g.E) router_rows<XT, EB>(g, x, e, g.logits + t * g.E);
+    if (e < g.E) router_row<XT>(g, x, e, g.logits + t * g.E + e);
     if (blockIdx.y) return;
     const int64_t columns = q4_padded(g.D), dp = row_pitch(g.D);
     for (int64_t k = 8 * threadIdx.x; k < columns; k += 8 * 256) {
@@ -297,7 +290,7 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
         float* made = reinterpret_cast<float*>(list + g.T);      // [T][E]
         logits = made;
         for (int i = wave; i < g.T * g.E; i += 2 * g.ways)
-            router_rows<XT, 1>(g, static_cast<const typename XT::type*>(g.x) + i / g.E * g.ldx, i % g.E, made + i / g.E * g.E);
+            router_row<XT>(g, static_cast<const typename XT::type*>(g.x) + i / g.E * g.ldx, i % g.E, made + i);
         for (int t = 0; t < g.T; ++t)
             for (int j = threadIdx.x; j < chunks * (kQ4Chunk / 8); j += blockDim.x) {
                 uint4 p[P];
@@ -566,12 +559,12 @@ int launch_up(MoeArgs g, hipStream_t st) {
     };
     size_t small, sums;
     sizes(TPT, true, small, sums);
-    // The logits by every workgroup itself where they are few (1 token, 8 experts, 1500 columns: 14.7 us in two kernels against
-    // 18 in three); 64 experts of 2048 columns would have each read 256 KB.
+    // The logits by every workgroup itself where they are few (1 token, 8 experts, 1500 columns: 15.0 us in two kernels against
+    // 17.4 in three); 64 experts of 2048 columns would have each read 256 KB.
     if (g.T <= TPT && g.T * row <= 40 * 1024 && g.T * g.E <= 4 * g.ways && (int64_t)g.T * g.E * g.D <= 32768)
         return launch_up_rows<XT, GL, 1, true, true>(g, small + sums + g.T * row, st);
     g.routed = g.T >= 4;
-    hipLaunchKernelGGL(moe_logits_kernel<XT>, dim3(g.T, (g.E + 15) / 16), dim3(256), 0, st, g);
+    hipLaunchKernelGGL(moe_logits_kernel<XT>, dim3(g.T, (g.E + 3) / 4), dim3(256), 0, st, g);
     int rc = hip_status(hipGetLastError());
     if (rc != BS_OK) return rc;
     if (g.routed) {
