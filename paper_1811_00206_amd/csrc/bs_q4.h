@@ -313,6 +313,22 @@ struct TilesOfX {
     __device__ __forceinline__ uint4 operator()(int t, int, int u, int i) const { return v[t][u % FETCH][i]; }
 };
 
+// 8 elements of a row that were loaded from column `from` = min(k, K - 8), as those from column k on, zero behind K
+__device__ __forceinline__ uint4 moved8(uint4 v, int64_t k, int64_t from, int64_t K) {
+    if (k == from) return v;
+    return k < K ? __builtin_bit_cast(uint4, __builtin_bit_cast(unsigned __int128, v) >> (16 * (int)(k - from))) : uint4{0, 0, 0, 0};
+}
+__device__ __forceinline__ void moved8(float (&v)[8], int64_t k, int64_t from) {
+    if (k == from) return;
+    const int by = (int)min(k - from, (int64_t)8);      // 3 bits of the distance, one after the other; 8: nothing is left
+#pragma unroll
+    for (int step = 4; step; step /= 2)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = by & step ? (i + step < 8 ? v[i + step] : 0.f) : v[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = by & 8 ? 0.f : v[i];
+}
+
 // 8 elements of a row from column k on, zero behind K; the row may start anywhere.  A piece that is not whole is the row's
 // last 8 elements, moved: no lane loads element by element, which would be eight trips to memory one after the other.
 __device__ __forceinline__ uint4 bits8(const uint16_t* row, int64_t k, int64_t K) {
@@ -320,7 +336,7 @@ __device__ __forceinline__ uint4 bits8(const uint16_t* row, int64_t k, int64_t K
     if (K >= 8) {
         const int64_t from = min(k, K - 8);
         __builtin_memcpy(&v, row + from, 16);
-        if (k != from) v = k < K ? __builtin_bit_cast(uint4, __builtin_bit_cast(unsigned __int128, v) >> (16 * (int)(k - from))) : uint4{0, 0, 0, 0};
+        v = moved8(v, k, from, K);
     } else {
         uint32_t h[8];
 #pragma unroll
@@ -339,15 +355,7 @@ __device__ __forceinline__ void load8(const typename XT::type* row, int64_t k, i
     } else if (K >= 8) {
         const int64_t from = min(k, K - 8);
         __builtin_memcpy(v, row + from, 32);
-        if (k != from) {
-            const int by = (int)min(k - from, (int64_t)8);      // 3 bits of the distance, one after the other; 8: nothing is left
-#pragma unroll
-            for (int step = 4; step; step /= 2)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = by & step ? (i + step < 8 ? v[i + step] : 0.f) : v[i];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = by & 8 ? 0.f : v[i];
-        }
+        moved8(v, k, from);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : 0.f;

@@ -4,8 +4,9 @@
 // (step i of U chunks goes to wavefront i % ways), so that a few thousand rows already fill the chip, and add their sums in
 // LDS in the order of the wavefronts: the same bits from every call.
 //
-// x comes to the matrix unit in two ways.  A few virtual rows (4: one fp32 vector, four in 16 bits) a workgroup brings to LDS
-// itself, in slabs of K, split into parts there; `tiles` groups of 16 rows share them.  More are read from memory by every
+// x comes to the matrix unit in three ways.  A few virtual rows (4: one fp32 vector, four in 16 bits) are brought to LDS and split
+// into parts there: by a workgroup, in slabs of K, where `tiles` groups of 16 rows share them, or by every wavefront for its own
+// columns, a step ahead, where a workgroup has one group of rows.  More are read from memory by every
 // wavefront, 64 bytes of 16 rows at a time, which the caches hold: rows of 16-bit vectors as they are, or tiles of parts that a
 // first kernel puts into the workspace.
 #include "bs_q4.h"
@@ -100,6 +101,98 @@ __global__ __launch_bounds__(1024) void q4_gemv_kernel(GemvArgs g) {
     }
 }
 
+// x of a wavefront's step, 128 * U columns of a few virtual rows, in LDS of its own: asked for a step ahead, split and put there
+// when the step begins.  K >= 8.
+template <typename XT, int U>
+struct OwnX {
+    using T = typename XT::type;
+    static constexpr int P = XT::kParts, kMost = P == 3 ? 1 : kStagedRows, kPitch = U * kQ4Chunk + 8;
+    const T* x;
+    int64_t K, ldx;
+    int tokens, lane;
+    uint16_t* own;            // [tokens * P][kPitch]
+    const uint16_t* mine;     // the lane's row, from its column 8 * kb on
+    uint4 raw[kMost][sizeof(T) / 2];
+    __device__ __forceinline__ int64_t column(int c) const { return (int64_t)c * kQ4Chunk + 8 * (U == 4 ? lane : lane & 31); }
+    __device__ __forceinline__ void fetch(int c) {
+        const int64_t from = min(column(c), K - 8);
+#pragma unroll
+        for (int n = 0; n < kMost; ++n)
+            if (n < tokens) __builtin_memcpy(raw[n], x + n * ldx + from, sizeof(raw[n]));
+    }
+    __device__ __forceinline__ void put(int c) {
+        const int64_t k = column(c), from = min(k, K - 8);
+#pragma unroll
+        for (int n = 0; n < kMost; ++n) {
+            if (n >= tokens) break;
+            uint4 p[P];
+            if constexpr (P == 3) {
+                float v[8];
+                __builtin_memcpy(v, raw[n], 32);
+                moved8(v, k, from);
+                split8(v, p);
+            } else {
+                p[0] = moved8(raw[n][0], k, from, K);
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(own + (n * P + i) * kPitch + (k - (int64_t)c * kQ4Chunk)) = p[i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // some lanes write what others read
+    }
+    __device__ __forceinline__ uint4 operator()(int, int, int u, int i) const {
+        return *reinterpret_cast<const uint4*>(mine + u * kQ4Chunk + 32 * i);
+    }
+};
+
+// The same for few rows: a workgroup has one tile, so no two wavefronts want the same columns of x, and each brings its own.
+template <typename XT, int GL, int U>
+__global__ __launch_bounds__(1024) void q4_gemv_own_kernel(GemvArgs g) {
+    using T = typename XT::type;
+    constexpr int P = XT::kParts, S = XT::kSlots, kOut = 256 / S;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, kb = lane >> 4, r = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row0 = (int64_t)blockIdx.x * 16;
+    const int chunks = (int)((g.K + kQ4Chunk - 1) / kQ4Chunk), tokens = (int)g.N;
+    Q4Walk<XT::kHalf, 1, 1, GL, U> walk;
+    walk.tile(0, g.codes, g.scales, row0, g.M, g.K, lane);
+    OwnX<XT, U> x;
+    x.x = static_cast<const T*>(g.x);
+    x.K = g.K;
+    x.ldx = g.ldx;
+    x.tokens = tokens;
+    x.lane = lane;
+    x.own = reinterpret_cast<uint16_t*>(lds) + wave * tokens * P * x.kPitch;
+    x.mine = x.own + (min(r / S, tokens - 1) * P + min(r % S, P - 1)) * x.kPitch + 8 * kb;
+    f32x4 acc[1][1] = {};
+    int c = wave * U;
+    walk.load(c);
+    x.fetch(c);
+    while (c < chunks) {
+        const int now = c;
+        walk.take();
+        x.put(now);
+        c += g.ways * U;
+        if (c < chunks) {
+            walk.load(c);
+            x.fetch(c);
+        }
+        uint32_t sc[1][decltype(walk)::kWords][4];
+        walk.spread(sc);
+        walk.template eat<0, U>(now, chunks, x, sc, acc);
+    }
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(lds);
+    put_sums<S>(sums, wave, lane, acc);
+    __syncthreads();
+    for (int o = threadIdx.x; o < kOut; o += blockDim.x) {
+        const int64_t row = row0 + o % 16;
+        if (o / 16 >= tokens || row >= g.M) continue;
+        float sum = sums[o];
+        for (int w = 1; w < g.ways; ++w) sum += sums[w * kOut + o];
+        static_cast<T*>(g.y)[o / 16 * g.ldy + row] = XT::store(sum);
+    }
+}
+
 template <typename XT, int NT, int R, int GL, bool TILED>
 __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(GemvArgs g) {
     using T = typename XT::type;
@@ -188,7 +281,7 @@ __global__ __launch_bounds__(256) void q4_tiles_kernel(const void* x, int64_t K,
 }
 
 struct Plan {
-    bool staged;
+    bool staged, own;
     bool tiled;
     int nt, r, u, ways, tiles, slab, split, part_chunks;
     int64_t counts;
@@ -203,14 +296,24 @@ Plan plan_for(int dtype, int64_t M, int64_t K, int64_t N) {
     if (p.staged) {
         // Wavefronts that share K: as many as give the chip 2048 (eight for a compute unit), or what K has steps for.  Where
         // two are enough, four groups share x.  16384 x 8192: 14.9 us with 2 x 4, 16.6 with 2 x 1, 15.4 with 4 x 1, 17.2 with
-        // 8 x 1; 10000 x 1500: 6.1 / 6.1 / 5.6 / 6.0; 4096 x 25088: 37 / 40 / 22 / 15.
+        // 8 x 1.
         const int64_t steps = (chunks + 1) / 2;
         p.ways = 1;
         while (p.ways < 16 && tiles * p.ways < 2048 && p.ways < steps) p.ways *= 2;
-        p.tiles = p.ways <= 2 ? 4 : 1;
+        p.tiles = 4;
         // four chunks a step where every wavefront has many: 16384 x 8192 14.1 us against 14.9
         p.u = chunks >= 16 * p.ways ? 4 : 2;
         const int rows = (int)N * parts;
+        // A workgroup of one tile has nobody to share x with: 4096 x 25088 for an fp32 vector 17 us with all of x in LDS first, 13.2
+        // with x step by step; for four binary16 ones 24 and 14.7; 2000 x 1000 3.9 and 3.5.  Steps of four chunks where a wavefront has
+        // more than three: 1269 x 13037 7.7 us instead of 8.1, 2000 x 1000 4.1 instead of 3.5.
+        p.own = p.ways > 2;
+        if (p.own) {
+            p.u = chunks > 3 * p.ways ? 4 : 2;
+            const size_t xs = (size_t)p.ways * rows * (p.u * kQ4Chunk + 8) * 2, sums = (size_t)p.ways * tpt * 16 * 4;
+            p.lds = xs > sums ? xs : sums;
+            return p;
+        }
         const int64_t whole = p.u * kQ4Chunk, most = (int64_t)kSlabBytes / (rows * 2) / whole * whole, all = (K + whole - 1) / whole * whole;
         p.slab = (int)(all < most ? all : most);
         const size_t xs = (size_t)rows * (p.slab + 8) * 2, sums = (size_t)p.ways * p.tiles * tpt * 16 * 4;
@@ -256,6 +359,15 @@ int launch_staged(const GemvArgs& g, const Plan& p, hipStream_t st) {
     if (p.lds > kLdsWithoutLimit) {
         const int rc = ensure_lds_limit(Reg::reg, st);
         if (rc != BS_OK) return rc;
+    }
+    if (p.own) {
+        using Own = LdsKernelOf<q4_gemv_own_kernel<XT, GL, U>>;
+        if (p.lds > kLdsWithoutLimit) {
+            const int rc = ensure_lds_limit(Own::reg, st);
+            if (rc != BS_OK) return rc;
+        }
+        hipLaunchKernelGGL((q4_gemv_own_kernel<XT, GL, U>), dim3((unsigned)((g.M + 15) / 16)), dim3(64 * p.ways), p.lds, st, g);
+        return hip_status(hipGetLastError());
     }
     const dim3 grid((unsigned)((g.M + 16 * p.tiles - 1) / (16 * p.tiles)));
     hipLaunchKernelGGL((q4_gemv_kernel<XT, GL, U>), grid, dim3(64 * p.ways * p.tiles), p.lds, st, g);
