@@ -13,9 +13,9 @@
 // the beginning and end of the workgroups of `up` and `down`.  For up to three tokens every workgroup of `up` finds its expert by
 // itself, without `route` (which is 3 to 5 us; 7 tokens, 64 experts of 2048 x 1024, 6 each: 41.9 us with it, 47.6 without;
 // 2 tokens, 32 experts of 1004 x 415, 8 each: kernels of 26.9 with it, 22.4 without), and where the logits are few they are made
-// there too.  The order of all sums is fixed: a result has the same bits from every call.  Hidden values pass to `down` in two
-// bfloat16 parts for 16-bit activations (16 leading bits: their rounding is not seen behind the output's) and in three (all 24
-// bits) for fp32.
+// there too.  The order of all sums is fixed: a result has the same bits from every call.  Hidden values pass to `down` in three
+// bfloat16 parts, all 24 bits, for 16-bit activations too: in two parts, 16 bits, their rounding was seen where the sum over F
+// cancels.
 //
 // Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 38 to 42 us (logits 4.8, route 4.8, up 18 to 22 as 32 or
 // more experts are chosen, down 14.6; 18.4 at the rate of reads).  16 tokens, 8 each: up 31, down 30.  One token of 1500 x 1500 in
@@ -30,17 +30,16 @@ namespace bs {
 namespace {
 
 constexpr int kDownWaves = 8;
-constexpr size_t kLdsOfX = 32 * 1024, kLdsOfH = 64 * 1024;      // x (twice that, if need be) and h are brought to LDS where they take no more
+// x (twice that, if need be) and h are brought to LDS where they take no more: h of 44 pairs and 256 columns, of which a compute unit holds
+// two workgroups (7 tokens, 6 experts each: 43.9 us a call, 48.9 with h from memory)
+constexpr size_t kLdsOfX = 32 * 1024, kLdsOfH = 68 * 1024;
 constexpr int kTokens = 64;      // that pass together; more pass 64 by 64
 
 // Elements between virtual rows in the workspace: whole chunks and a cache line, so that rows a power of two long do not
 // meet in the same sets of the caches.
 __host__ __device__ constexpr int64_t row_pitch(int64_t columns) { return q4_padded(columns) + 64; }
 
-template <typename XT>
-struct Hidden {      // virtual rows of h
-    static constexpr int kParts = XT::kParts == 3 ? 3 : 2, kSlots = XT::kParts == 3 ? 4 : 2;
-};
+constexpr int kHiddenParts = 3, kHiddenSlots = 4;      // virtual rows of h, and those set aside for a token, as for fp32 activations
 
 struct MoeArgs {
     const void *x, *router;
@@ -275,7 +274,7 @@ __host__ __device__ constexpr int up_small(int T, int pairs, int E, bool alone) 
 // is brought to LDS, else read from memory.  ALONE: without the kernel of the logits, they are made here, by every workgroup.
 template <typename XT, int NT, int GL, bool IN_LDS, bool ALONE>
 __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
-    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S, HP = Hidden<XT>::kParts, U = IN_LDS ? 4 : 2;
+    constexpr int P = XT::kParts, S = XT::kSlots, TPT = 16 / S, HP = kHiddenParts, U = IN_LDS ? 4 : 2;
     extern __shared__ __align__(16) uint8_t lds[];
     int32_t* list = reinterpret_cast<int32_t*>(lds + route_bytes(g.pairs, g.E));                   // [T]
     float* sums = reinterpret_cast<float*>(lds + up_small(g.T, g.pairs, g.E, ALONE));      // [way][gate, up][tile][rows][16]
@@ -397,12 +396,8 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
                 for (int w = 1; w < g.ways; ++w) { gate += from[2 * w * out]; up += from[(2 * w + 1) * out]; }
                 h = gate / (1.f + expf(-gate)) * up;
             }
-            uint32_t part[3];
+            uint32_t part[HP];
             split3(h, part[0], part[1], part[2]);
-            if constexpr (HP == 2) {      // the second part rounded
-                const float rest = __builtin_bit_cast(float, part[1]) + __builtin_bit_cast(float, part[2]);
-                part[1] = (uint32_t)BF16::store(rest) << 16;
-            }
             uint16_t* to = g.hp + (int64_t)list[n0 + n] * HP * fp + f;
 #pragma unroll
             for (int i = 0; i < HP; ++i) to[i * fp] = (uint16_t)(part[i] >> 16);
@@ -418,7 +413,7 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
 // IN_LDS: the part's h of all pairs is brought to LDS, else read from memory.
 template <typename XT, int GL, bool IN_LDS>
 __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
-    constexpr int P = Hidden<XT>::kParts, S = Hidden<XT>::kSlots, TPT = 16 / S, V = 4 / S, U = 2;
+    constexpr int P = kHiddenParts, S = kHiddenSlots, TPT = 16 / S, U = 2;
     extern __shared__ __align__(16) uint8_t lds[];
     float* sums = reinterpret_cast<float*>(lds);                                     // [wave][T][16]
     int4* groups = reinterpret_cast<int4*>(sums + kDownWaves * g.T * 16);            // [pairs at most]
@@ -483,15 +478,10 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
             if (n0 + TPT >= tokens && item + kDownWaves < items) load(step, groups[expert]);
             f32x4 acc[1][1] = {};
             walk.template eat<0, U>(c, end, x, sc, acc);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int n = kb * V + v;
-                if (n >= here) continue;
-                float sum;
-                if constexpr (S == 4) sum = acc[0][0][0] + (acc[0][0][1] + acc[0][0][2]);
-                else sum = acc[0][0][2 * v] + acc[0][0][2 * v + 1];
-                float* to = mine + place[n0 + n] + r;
-                *to = fmaf(share[n0 + n], sum, *to);
+            if (kb < here) {      // a lane's four rows are the parts of token kb
+                const float sum = acc[0][0][0] + (acc[0][0][1] + acc[0][0][2]);
+                float* to = mine + place[n0 + kb] + r;
+                *to = fmaf(share[n0 + kb], sum, *to);
             }
         }
     }
@@ -606,7 +596,7 @@ template <typename XT, int GL>
 int launch(const MoeArgs& g, hipStream_t st) {
     const int rc = launch_up<XT, GL>(g, st);
     if (rc != BS_OK) return rc;
-    const size_t small = down_small(g.T, g.pairs), h = (size_t)g.pairs * Hidden<XT>::kParts * (g.part_chunks * kQ4Chunk + 8) * 2;
+    const size_t small = down_small(g.T, g.pairs), h = (size_t)g.pairs * kHiddenParts * (g.part_chunks * kQ4Chunk + 8) * 2;
     return h <= kLdsOfH ? launch_down<XT, GL, true>(g, small + h, st) : launch_down<XT, GL, false>(g, small, st);
 }
 
@@ -631,11 +621,10 @@ Space space_for(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
     // (more where their wavefronts have four steps each).  7 tokens of 2048 x 1024, 64 experts, 6 of them each: `down` 14.8 us with
     // four workgroups a tile, 34 with one.
     const int64_t tiles = (D + 15) / 16, chunks = q4_padded(F) / kQ4Chunk, pairs = T * top_k, experts = pairs < E ? pairs : E;
-    const int parts = dtype == BS_F32 ? 3 : 2;
     s.split = 1;
     s.part_chunks = (int)chunks;
     while (s.split < 16 && s.part_chunks > 2) {
-        const auto room = [&](int64_t n) { return pairs * parts * (n * kQ4Chunk + 8) * 2; };
+        const auto room = [&](int64_t n) { return pairs * kHiddenParts * (n * kQ4Chunk + 8) * 2; };
         const bool fits = room(s.part_chunks) <= (int64_t)kLdsOfH || room(2) > (int64_t)kLdsOfH;      // or no split would make it fit
         const int64_t steps = (s.part_chunks + 1) / 2 * experts;
         if (fits && (tiles * s.split >= 512 || steps < 4 * kDownWaves)) break;
@@ -645,7 +634,7 @@ Space space_for(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k) {
     s.split = (int)((chunks + s.part_chunks - 1) / s.part_chunks);
     const auto up16 = [](size_t n) { return (n + 15) / 16 * 16; };
     s.h = (size_t)T * (dtype == BS_F32 ? 3 : 1) * row_pitch(D) * 2;
-    s.logits = s.h + (size_t)pairs * parts * row_pitch(F) * 2;
+    s.logits = s.h + (size_t)pairs * kHiddenParts * row_pitch(F) * 2;
     s.groups = s.logits + up16((size_t)T * E * 4);
     s.order = s.groups + (size_t)(pairs + 1) * 16;
     s.parts = s.order + up16((size_t)pairs * 4);
