@@ -574,28 +574,38 @@ struct BackArgs {
     int slices;
 };
 
-// log p = (x - m) - log_s for all of a row, by all threads
+// log p = (x - m) - log_s for all of a row, by all threads.  These sums are of 2^((x - m) L), differences first, and go with another m by a
+// difference too: raise() and join() are for sums made with m L rounded by itself, whose rounding is theirs as well.
 struct Shift {
     float m, log_s;
 };
+__device__ __forceinline__ float moved_sum(float s, float from, float to) {
+    return from == to ? s : s * exp2_hw(at_least((from - to) * kLog2e, -200.f));
+}
 template <typename XT>
 __device__ __forceinline__ Shift shift_of(const typename XT::type* row, int64_t V) {
-    __shared__ Stats stats[kWaves];
-    Stats st{-__builtin_inff(), 0.f, 0.f};
+    __shared__ float largest[kWaves], sums[kWaves];
+    float m = -__builtin_inff(), s = 0.f;
     for (int64_t k = threadIdx.x; k < V; k += kThreads) {
         const float x = XT::load(row[k]);
-        if (x > st.m) {
-            st.s *= exp2_hw(at_least((st.m - x) * kLog2e, -200.f));
-            st.m = x;
+        if (x > m) {
+            s = moved_sum(s, m, x);
+            m = x;
         }
-        if (x != -__builtin_inff()) st.s += exp2_hw(at_least((x - st.m) * kLog2e, -200.f));
+        if (x != -__builtin_inff()) s += exp2_hw(at_least((x - m) * kLog2e, -200.f));
     }
-    st = join_wave(st);
-    if ((threadIdx.x & 63) == 0) stats[threadIdx.x >> 6] = st;
+    const float most = max_of_wave(m);
+    s = sum_of_wave(moved_sum(s, m, most));
+    if ((threadIdx.x & 63) == 0) {
+        largest[threadIdx.x >> 6] = most;
+        sums[threadIdx.x >> 6] = s;
+    }
     __syncthreads();
-    st = stats[0];
-    for (int w = 1; w < kWaves; ++w) st = join(st, stats[w]);
-    return {st.m, logf(st.s)};
+    m = largest[0];
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, largest[w]);
+    s = 0.f;
+    for (int w = 0; w < kWaves; ++w) s += moved_sum(sums[w], largest[w], m);
+    return {m, logf(s)};
 }
 
 // d = p * -(g_lp + g_H (log p + H)), and g_lp at the target.  A large lse (4096 is 2^12) has lost what a difference of logits

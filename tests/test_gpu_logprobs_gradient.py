@@ -1,0 +1,58 @@
+"""The gradient of log probabilities and entropies for rows that lie far from 0, against the softmax in 64 bits of the logits as they are.
+
+Bounds: the log of a row's sum is off by 1e-5 at most (fp32 roundings of a few hundred additions, of 2^u, and of lse itself), an
+entropy by 1e-5 (2 + H); both are factors or terms of p, and the result has its own rounding."""
+import pytest
+import torch
+
+from paper_1811_00206_amd import binding as bs
+from test_gpu_logprobs import ROUNDING, TYPES
+
+pytestmark = pytest.mark.gpu
+
+
+def check(x, targets, seed):
+    T, V = x.shape
+    g = torch.Generator().manual_seed(seed)
+    gl, gh = torch.randn(T, generator=g), torch.randn(T, generator=g)
+    _, entropy, lse, _, _ = bs.bs_logprobs(x, targets)
+    logp = torch.log_softmax(x.double(), -1).cpu()
+    p = logp.exp()
+    H = torch.special.entr(p).sum(-1, keepdim=True)
+    t = targets.cpu()
+    a = torch.where(t < 0, torch.zeros(T), gl).double().unsqueeze(-1)
+    smallest = 2.0**-25 if x.dtype == torch.float16 else 2.0**-126
+    for gh in (torch.zeros(T), gh):
+        b = gh.double().unsqueeze(-1)
+        got = bs.bs_logprobs_backward(x, targets, lse, entropy, gl.cuda(), gh.cuda())
+        room = x.clone()
+        assert torch.equal(bs.bs_logprobs_backward(room, targets, lse, entropy, gl.cuda(), gh.cuda(), out=room), got)
+        got = got.cpu().double()
+        want = -p * a - b * torch.where(p > 0, p * (logp + H), torch.zeros_like(p))
+        row = t >= 0
+        want[row.nonzero().squeeze(-1), t[row]] += a[row, 0]
+        allowed = p * 1e-5 * (a.abs() + b.abs() * (2 + 2 * H + torch.where(p > 0, logp.abs(), torch.zeros_like(p))))
+        allowed = allowed + ROUNDING[x.dtype] * want.abs() * 1.001 + 2.0**-23 * a.abs() + smallest
+        off = (got - want).abs()
+        assert bool((off <= allowed).all()), (off / allowed).amax(-1).tolist()
+        if x.dtype == torch.float32 and not bool(gh.any()):
+            # p adds up to 1: nothing is left of a row but those errors
+            left = got.sum(-1).abs()
+            assert bool((left <= 1.1e-5 * a.abs().squeeze(-1) + 1e-30).all()), left.tolist()
+
+
+FAR = {"f32": (0.0, 5e3, -1e4, -65504.0, 1e5, -1e5, 1e6, -1e6, 2.0**20 - 3, -(2.0**20), 2e6), "f16": (0.0, 5e3, -3e4, 6e4), "bf16": (0.0, -1e4, 1e5, 1e6)}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [3, 200, 1000, 5003, 40000])
+def test_rows_far_from_zero(V, dtype):
+    """Every lane has another largest logit: steps of the type's own size there, or a spread of 3."""
+    rows = []
+    for i, at in enumerate(FAR[dtype]):
+        x = torch.randn(V, generator=torch.Generator().manual_seed(V + i)).double()
+        step = torch.finfo(TYPES[dtype]).eps * abs(at)
+        rows.append((at + x * max(3.0, 2 * step)).clamp(-65504, 65504) if dtype == "f16" else at + x * max(3.0, 2 * step))
+    x = torch.stack(rows).to(TYPES[dtype])
+    targets = torch.randint(-1, V, (len(rows),), generator=torch.Generator().manual_seed(V))
+    check(x.cuda(), targets.cuda(), V)
