@@ -413,7 +413,10 @@ int bs_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
  * lse, entropy  DEVICE in   as bs_logprobs gave them          g_logprob, g_entropy  DEVICE in  T fp32 each
  * grad          DEVICE out  T rows of V, same type as the logits, ldg >= V apart; may be the logits themselves
  * entropy and g_entropy may both be NULL: the log probability's gradient alone.  A row without a target has that of its
- * entropy alone, one with a target that is not below V NaN; a row in which nothing is left (lse <= -1e30: all words -inf, or all the lowest fp32 / bfloat16 number) 0.
+ * entropy alone, one with a target that is not below V NaN; a row in which nothing is left (lse <= -1e30: all words -inf, or all
+ * the lowest fp32 / bfloat16 number) 0.  lse's rounding is a factor of the row's p: 1e-5 at most, or a sixteenth of the rounding of
+ * a type of 16 bits; a row whose lse has lost more is summed up once more (|lse| > 256 in fp32, 1024 in binary16, 4096 in
+ * bfloat16), which takes two to fifteen times as long.
  */
 int bs_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets,
                          const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,

@@ -11,7 +11,8 @@ from test_gpu_logprobs import ROUNDING, TYPES
 pytestmark = pytest.mark.gpu
 
 
-def check(x, targets, seed):
+def check(x, targets, seed, lost=0.0):
+    """`lost`: what a rounded lse may cost beside the type's rounding"""
     T, V = x.shape
     g = torch.Generator().manual_seed(seed)
     gl, gh = torch.randn(T, generator=g), torch.randn(T, generator=g)
@@ -31,7 +32,7 @@ def check(x, targets, seed):
         want = -p * a - b * torch.where(p > 0, p * (logp + H), torch.zeros_like(p))
         row = t >= 0
         want[row.nonzero().squeeze(-1), t[row]] += a[row, 0]
-        allowed = p * 1e-5 * (a.abs() + b.abs() * (2 + 2 * H + torch.where(p > 0, logp.abs(), torch.zeros_like(p))))
+        allowed = p * (1e-5 + lost) * (a.abs() + b.abs() * (2 + 2 * H + torch.where(p > 0, logp.abs(), torch.zeros_like(p))))
         allowed = allowed + ROUNDING[x.dtype] * want.abs() * 1.001 + 2.0**-23 * a.abs() + smallest
         off = (got - want).abs()
         assert bool((off <= allowed).all()), (off / allowed).amax(-1).tolist()
@@ -56,3 +57,13 @@ def test_rows_far_from_zero(V, dtype):
     x = torch.stack(rows).to(TYPES[dtype])
     targets = torch.randint(-1, V, (len(rows),), generator=torch.Generator().manual_seed(V))
     check(x.cuda(), targets.cuda(), V)
+
+
+@pytest.mark.parametrize("dtype,lost", [("f32", 0.0), ("f16", 2.0**-15), ("bf16", 2.0**-13)])
+@pytest.mark.parametrize("V", [200, 5003, 140000])
+def test_rows_as_far_as_lse_is_not_rounded_away(V, dtype, lost):
+    """Up to where lse's rounding reaches what the row's sums are off by (a sixteenth of the rounding of a type of 16 bits), and behind it."""
+    at = torch.tensor([20.0, -100.0, 240.0, -270.0, 500.0, -1100.0, 2500.0, 4000.0, -4095.0]).unsqueeze(-1)
+    x = torch.randn((9, V), generator=torch.Generator().manual_seed(V)) * 3 + at
+    targets = torch.randint(-1, V, (9,), generator=torch.Generator().manual_seed(V + 1))
+    check(x.to(TYPES[dtype]).cuda(), targets.cuda(), V, lost)
