@@ -371,7 +371,7 @@ int bs_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t 
 
 /*
  * A layer of E experts, of which every token uses top_k:
- *     l = R x;   the top_k largest l, the lower expert first among equals
+ *     l = R x;   the top_k largest l, the lower expert first among equals (an l that is NaN last, behind -inf)
  *     p = softmax of the chosen l (renormalise != 0), or softmax of all l at the chosen ones
  *     y = sum over the chosen e of p_e * W2_e (silu(G_e x) * (U_e x)),   silu(a) = a / (1 + exp(-a))
  * x        DEVICE in   T rows of D, ldx apart        y  DEVICE out  T rows of D, ldy apart

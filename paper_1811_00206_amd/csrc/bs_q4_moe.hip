@@ -81,21 +81,28 @@ __device__ __forceinline__ void router_row(const MoeArgs& g, const typename XT::
     if (lane == 0) *logit = sum;
 }
 
-// One wavefront: a token's top_k experts and their weights.  Up to 64 experts are a lane's each: the largest logit of the free
-// lanes, and of lanes that have it the first.  (A logit that is no number is the lowest there is.)
+// Of up to 64 experts, a lane's each, the next choice among the free ones, by one wavefront: the largest logit, and of lanes that have it
+// the first.  A logit that is no number comes last, behind -inf too: `own` is -inf there, and the lane is not in `numbers`.
+__device__ __forceinline__ int next_choice(float own, uint64_t numbers, uint64_t free, float& most) {
+    most = max_of_wave(free >> (threadIdx.x & 63) & 1 ? own : -__builtin_inff());
+    const uint64_t m = __ballot(own == most) & free, n = m & numbers;
+    return __ffsll((unsigned long long)(n ? n : m)) - 1;
+}
+
+// One wavefront: a token's top_k experts and their weights.
 __device__ __forceinline__ void choose(const MoeArgs& g, const float* logits, int32_t* ids, float* weights) {
     const int lane = threadIdx.x & 63;
     if (g.E <= 64) {
         float l = lane < g.E ? logits[lane] : 0.f;
         const bool nan = l != l;
         const float own = nan ? -__builtin_inff() : l;
+        const uint64_t numbers = __ballot(!nan);
         uint64_t free = g.E == 64 ? ~(uint64_t)0 : ((uint64_t)1 << g.E) - 1;
         int rank = -1;
         float top = 0.f;
         for (int j = 0; j < g.top_k; ++j) {
-            const float most = max_of_wave(free >> lane & 1 ? own : -__builtin_inff());
-            const uint64_t m = __ballot(own == most) & free;
-            const int first = __ffsll((unsigned long long)m) - 1;
+            float most;
+            const int first = next_choice(own, numbers, free, most);
             if (lane == first) rank = j;
             free &= ~((uint64_t)1 << first);
             if (j == 0) top = most;
@@ -139,8 +146,9 @@ __device__ __forceinline__ int experts_before(const MoeArgs& g, const float* log
     const int lane = threadIdx.x & 63;
     if (g.E <= 64) {
         const float l = lane < g.E ? logits[lane] : 0.f;
-        const float own = l != l ? -__builtin_inff() : l, other = le != le ? -__builtin_inff() : le;
-        return __popcll(__ballot(lane < g.E && (own > other || (own == other && lane < e))));
+        const bool nan = l != l, other_nan = le != le;
+        const float own = nan ? -__builtin_inff() : l, other = other_nan ? -__builtin_inff() : le;
+        return __popcll(__ballot(lane < g.E && (own > other || (own == other && (nan == other_nan ? lane < e : other_nan)))));
     }
     const uint64_t key = order_key(le, e);
     int n = 0;
@@ -154,10 +162,11 @@ __device__ __forceinline__ int expert_of(const MoeArgs& g, const float* logits, 
     if (g.E <= 64) {
         const float l = lane < g.E ? logits[lane] : 0.f;
         const float own = l != l ? -__builtin_inff() : l;
+        const uint64_t numbers = __ballot(l == l);
         uint64_t free = g.E == 64 ? ~(uint64_t)0 : ((uint64_t)1 << g.E) - 1;
         for (;;) {
-            const float most = max_of_wave(free >> lane & 1 ? own : -__builtin_inff());
-            const int first = __ffsll((unsigned long long)(__ballot(own == most) & free)) - 1;
+            float most;
+            const int first = next_choice(own, numbers, free, most);
             if (j-- == 0) return __builtin_amdgcn_readfirstlane(first);
             free &= ~((uint64_t)1 << first);
         }

@@ -1,9 +1,9 @@
-"""Expert layers where their numbers can go wrong: hidden values that cancel."""
+"""Expert layers where their numbers can go wrong: hidden values that cancel, router logits that are no number."""
 import pytest
 import torch
 
 from paper_1811_00206_amd import binding as bs
-from test_gpu_moe import call, layer, values_of
+from test_gpu_moe import BOUND, call, layer, values_of
 from test_gpu_q4 import TYPES
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +41,29 @@ def test_hidden_values_that_cancel(T, E, top_k, dtype):
     smallest = 2.0**-25 if dtype == "f16" else 0.0                    # binary16 has no smaller numbers
     off = y.cpu().double().abs().amax(-1)
     assert bool((off <= 10 * 2.0**-24 * size + smallest).all()), float((off / size.clamp(min=1e-30)).max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,E", [(1, 5), (1, 64), (3, 40), (2, 64), (2, 70), (6, 5), (9, 64), (7, 70)])
+def test_logits_that_are_no_number_come_last(T, E, dtype):
+    """Behind -inf too, whatever their index: who chooses as many experts as have numbers is not touched by the others."""
+    p = layer(T, 64, 40, E, 32, dtype, T + E)
+    p["x"] = p["x"].abs() + 0.125
+    p["router"] = torch.zeros((E, 64), dtype=TYPES[dtype])
+    p["router"][0, 3] = p["router"][3, 60] = float("nan")
+    p["router"][2, 7] = p["router"][4, 9] = -float("inf")
+    p["router"][5:8, 0] = -1.0
+    p["router"][8:, 63] = -float("inf")
+    finite = [1, *range(5, min(E, 8))]
+    impossible = [2, 4, *range(8, E)]
+    order = [*finite, *impossible, 0, 3]
+    for top_k in sorted({min(n, 32) for n in (1, 2, len(finite) + 1, E - 2, E - 1, E)}):
+        y, ids, weights = call(p, top_k, True)
+        assert ids.tolist() == [order[:top_k]] * T
+        if top_k <= E - 2:
+            want_y, _, want = call(p, min(top_k, len(finite)), True)
+            assert not bool(weights[:, len(finite):].any()) and torch.equal(weights[:, :len(finite)], want)
+            off = (y.double() - want_y.double()).norm(dim=-1)      # added up in another order
+            assert bool((off <= 2 * BOUND[dtype] * want_y.double().norm(dim=-1)).all())
+        else:
+            assert bool(torch.isnan(weights).all())
