@@ -1,9 +1,10 @@
-"""Expert layers where their numbers can go wrong: hidden values that cancel, router logits that are no number."""
+"""Expert layers where their numbers can go wrong: hidden values that cancel, router logits that are no number; and
+activations too long for LDS."""
 import pytest
 import torch
 
 from paper_1811_00206_amd import binding as bs
-from test_gpu_moe import BOUND, call, layer, values_of
+from test_gpu_moe import BOUND, call, check, definition, layer, values_of
 from test_gpu_q4 import TYPES
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +68,9 @@ def test_logits_that_are_no_number_come_last(T, E, dtype):
             assert bool((off <= 2 * BOUND[dtype] * want_y.double().norm(dim=-1)).all())
         else:
             assert bool(torch.isnan(weights).all())
+
+
+@pytest.mark.parametrize("T,D,F,E,top_k", [(1, 11000, 40, 3, 2), (3, 11000, 40, 3, 1), (4, 11003, 33, 5, 2), (9, 11000, 20, 2, 2)])
+def test_activations_too_long_to_be_brought_together(T, D, F, E, top_k):
+    p = layer(T, D, F, E, 64, "f32", T + D)
+    check(call(p, top_k, True), definition(p, top_k, True), "f32")
