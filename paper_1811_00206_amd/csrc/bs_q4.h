@@ -4,7 +4,8 @@
 // instruction per 32 columns.  Lane l = 16 * kb + r brings 8 columns, 32 * step + 8 * kb .. + 7, of matrix row r and of
 // virtual row r, and ends with the sums of matrix row r and virtual rows 4 * kb .. 4 * kb + 3.  E2M1 values are exact in
 // bfloat16 and binary16 (`v_cvt_scalef32_pk_*_fp4`: two values an instruction), products are exact in the matrix unit,
-// sums are fp32, and the group's scale is applied to the fp32 sum of the group: no weight is ever rounded.
+// sums are fp32, and the group's scale is applied to the fp32 sum of the group: no weight is ever rounded.  Sums of a walk are those of
+// W x over kQ4Unit.
 //
 // A 16-bit activation is one virtual row.  An fp32 activation is three (`split3`): its leading 8 bits, the next 8 and the
 // last 8, each exact in bfloat16, so that the product keeps all 24 bits at the cost of rows that a few tokens leave empty.
@@ -65,19 +66,27 @@ __device__ __forceinline__ void split3(float x, uint32_t& a, uint32_t& b, uint32
 // the upper halves of two words: the first in the low half
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 
+// A group's scale comes after its sum, which may therefore be larger than the result: up to 6 * 128 times an activation.  So bfloat16
+// values are multiplied by 2^-10 when they are made, for nothing, and a walk's sums by kQ4Unit where they become results: both are exact,
+// and nothing overflows but what a result overflows by.  (What it costs is at the other end: fp32 activations below 2^-99 lose bits, 2^-109
+// otherwise.)  Binary16 activations are too small to overflow fp32 sums.
 template <bool HALF>
-__device__ __forceinline__ uint4 q4_values(uint32_t w) {   // 8 codes as 8 binary16 / bfloat16 values
+constexpr float kQ4Unit = HALF ? 1.0f : 1024.0f;
+
+template <bool HALF>
+__device__ __forceinline__ uint4 q4_values(uint32_t w) {   // 8 codes as 8 binary16 / bfloat16 values, over kQ4Unit
     uint4 v;
+    constexpr float kOver = 1.0f / kQ4Unit<HALF>;
     if constexpr (HALF) {
-        v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0));
-        v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1));
-        v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2));
-        v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3));
+        v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, kOver, 0));
+        v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, kOver, 1));
+        v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, kOver, 2));
+        v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, kOver, 3));
     } else {
-        v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
-        v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
-        v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
-        v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+        v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kOver, 0));
+        v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kOver, 1));
+        v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kOver, 2));
+        v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kOver, 3));
     }
     return v;
 }

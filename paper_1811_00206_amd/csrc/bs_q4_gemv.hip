@@ -97,7 +97,7 @@ __global__ __launch_bounds__(1024) void q4_gemv_kernel(GemvArgs g) {
         const float* from = sums + i * g.ways * kOut + o % kOut;
         float sum = from[0];
         for (int w = 1; w < g.ways; ++w) sum += from[w * kOut];
-        static_cast<T*>(g.y)[n * g.ldy + row] = XT::store(sum);
+        static_cast<T*>(g.y)[n * g.ldy + row] = XT::store(sum * kQ4Unit<XT::kHalf>);
     }
 }
 
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(1024) void q4_gemv_own_kernel(GemvArgs g) {
         if (o / 16 >= tokens || row >= g.M) continue;
         float sum = sums[o];
         for (int w = 1; w < g.ways; ++w) sum += sums[w * kOut + o];
-        static_cast<T*>(g.y)[o / 16 * g.ldy + row] = XT::store(sum);
+        static_cast<T*>(g.y)[o / 16 * g.ldy + row] = XT::store(sum * kQ4Unit<XT::kHalf>);
     }
 }
 
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(NT * R == 1 ? 1024 : 512) void q4_gemv_many_kernel(
     constexpr int kOut = R * NT * TPT * 16;
     const auto store = [&](int o, float sum) {
         const int64_t row = row0 + o / (NT * TPT * 16) * 16 + o % 16;
-        static_cast<T*>(g.y)[(n0 + o / 16 % (NT * TPT)) * g.ldy + row] = XT::store(sum);
+        static_cast<T*>(g.y)[(n0 + o / 16 % (NT * TPT)) * g.ldy + row] = XT::store(sum * kQ4Unit<XT::kHalf>);
     };
     const auto wanted = [&](int o) { return o / 16 % (NT * TPT) < tokens && row0 + o / (NT * TPT * 16) * 16 + o % 16 < g.M; };
     const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;

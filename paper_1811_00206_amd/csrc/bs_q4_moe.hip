@@ -403,6 +403,8 @@ __global__ __launch_bounds__(512) void moe_up_kernel(MoeArgs g) {
                 const float* from = sums + (tile * g.rows + n) * 16 + o % 16;
                 float gate = from[0], up = from[out];
                 for (int w = 1; w < g.ways; ++w) { gate += from[2 * w * out]; up += from[(2 * w + 1) * out]; }
+                gate *= kQ4Unit<XT::kHalf>;
+                up *= kQ4Unit<XT::kHalf>;
                 h = gate / (1.f + expf(-gate)) * up;
             }
             uint32_t part[HP];
@@ -501,7 +503,7 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
         float sum = sums[o];
         for (int w = 1; w < kDownWaves; ++w) sum += sums[w * all + o];
         if (g.split == 1) {
-            if (d0 + o % 16 < g.D) static_cast<typename XT::type*>(g.y)[o / 16 * g.ldy + d0 + o % 16] = XT::store(sum);
+            if (d0 + o % 16 < g.D) static_cast<typename XT::type*>(g.y)[o / 16 * g.ldy + d0 + o % 16] = XT::store(sum * kQ4Unit<false>);
         } else {
             __hip_atomic_store(parts + blockIdx.y * all + o, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
@@ -510,7 +512,7 @@ __global__ __launch_bounds__(512) void moe_down_kernel(MoeArgs g) {
     for (int o = threadIdx.x; o < all; o += blockDim.x) {
         float sum = __hip_atomic_load(parts + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         for (int z = 1; z < g.split; ++z) sum += __hip_atomic_load(parts + z * all + o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (d0 + o % 16 < g.D) static_cast<typename XT::type*>(g.y)[o / 16 * g.ldy + d0 + o % 16] = XT::store(sum);
+        if (d0 + o % 16 < g.D) static_cast<typename XT::type*>(g.y)[o / 16 * g.ldy + d0 + o % 16] = XT::store(sum * kQ4Unit<false>);
     }
 }
 

@@ -1,5 +1,5 @@
-"""Expert layers where their numbers can go wrong: hidden values that cancel, router logits that are no number; and
-activations too long for LDS."""
+"""Expert layers where their numbers can go wrong: hidden values that cancel, router logits that are no number, sums that are
+larger than what they become; and activations too long for LDS."""
 import pytest
 import torch
 
@@ -74,3 +74,17 @@ def test_logits_that_are_no_number_come_last(T, E, dtype):
 def test_activations_too_long_to_be_brought_together(T, D, F, E, top_k):
     p = layer(T, D, F, E, 64, "f32", T + D)
     check(call(p, top_k, True), definition(p, top_k, True), "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 5, 20])
+def test_hidden_values_near_the_largest_number(T, dtype):
+    """Small scales of the second product times large hidden values: finite, though the sum of code times hidden value is not."""
+    p = layer(T, 64, 256, 2, 128, dtype, T)
+    a = torch.einsum("erd,td->etr", p["w1"], p["x"].double())
+    h = a[..., :256].clamp(min=0) * a[..., 256:]
+    by = 2.0 ** int((126 - float(h.abs().max().log2())) // 2)
+    p["x"], p["router"] = p["x"] * by, p["router"] / by
+    p["s2"] = (p["s2"] * 2.0**-7).half()
+    p["w2"] = values_of(p["c2"].reshape(128, -1), p["s2"].reshape(128, -1), 256, 128).reshape(2, 64, 256)
+    check(call(p, 2, True), definition(p, 2, True), dtype)

@@ -53,3 +53,33 @@ def test_many_rows(M, K, group, N, dtype, pitch):
 @pytest.mark.parametrize("M,K,group,N", [(16400, 4200, 64, 1), (16400, 4200, 64, 4), (16400, 8192, 32, 5), (9409, 22330, 128, 6), (5121, 9000, 64, 20)])
 def test_many_rows_that_are_long(M, K, group, N, dtype):
     check(M, K, group, N, dtype, K)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,group,N", [(40, 200, 128, 1), (40, 200, 32, 3), (5121, 304, 128, 2), (16400, 304, 128, 1), (33, 9000, 128, 5), (300, 1000, 128, 40)])
+def test_activations_near_the_largest_number(M, K, group, N, dtype):
+    """Small scales times large activations: finite, though the sum of code times activation is not."""
+    codes, scales, W = matrix(M, K, group)
+    scales, W = (scales * 2.0**-8).half(), W * 2.0**-8      # exact: scales are 0.1 to 1.1
+    x = (torch.randn((N, K), generator=torch.Generator().manual_seed(K)) * 2.0**(125 if K <= 1000 else 122)).to(TYPES[dtype]).cuda()
+    y = bs.bs_q4_gemv(codes, scales, group, x)
+    X, Wt = x.double(), W.t().contiguous()
+    want, size = X @ Wt, X.abs() @ Wt.abs()
+    assert float(size.max()) < 3.4e38
+    off = (y.double() - want).abs()
+    allowed = 2.0**-23 * (K / 32 + 64) * size + ROUNDING[TYPES[dtype]] * want.abs()
+    assert bool((off <= allowed).all()), float((off / allowed).max())
+
+
+@pytest.mark.parametrize("dtype,size_of", [("f32", 2.0**-98), ("bf16", 2.0**-110), ("f16", 2.0**-15)])
+@pytest.mark.parametrize("M,K,group,N", [(40, 200, 128, 1), (40, 200, 32, 3), (33, 9000, 128, 5), (300, 1000, 128, 40)])
+def test_small_activations(M, K, group, N, dtype, size_of):
+    """Products are small numbers, still normal ones, and keep their bits (binary16's own smallest numbers among the activations)."""
+    codes, scales, W = matrix(M, K, group)
+    x = (torch.randn((N, K), generator=torch.Generator().manual_seed(K)) * size_of).to(TYPES[dtype]).cuda()
+    y = bs.bs_q4_gemv(codes, scales, group, x)
+    X, Wt = x.double(), W.t().contiguous()
+    want, size = X @ Wt, X.abs() @ Wt.abs()
+    off = (y.double() - want).abs()
+    allowed = 2.0**-23 * (K / 32 + 64) * size + ROUNDING[TYPES[dtype]] * want.abs() + (2.0**-25 if dtype == "f16" else 0.0)
+    assert bool((off <= allowed).all()), float((off / allowed).max())
