@@ -336,7 +336,8 @@ int bs_lstm_sequence_plan(int dtype, int64_t H, int64_t I, int bank, int k, int 
  * What a model needs beside its pruned matrices: matrices that do not bear pruning (output
  * products, experts) in 4 bits, and what is made of the last product.  dtype here is the type
  * of the dense matrix, of activations and of logits: BS_F32, BS_F16 or BS_BF16; results have
- * the type of what they are made from.  All sums are fp32, each result is rounded once.
+ * the type of what they are made from.  All sums are fp32, each result is rounded once.  Outputs must not overlap inputs or one
+ * another, but for the gradient, as it says there.
  *
  * Format of a 4-bit matrix M x K: codes are E2M1 numbers, bit 3 the sign, bits 0..2 one of the
  * magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6.  Element k of a row is in byte k / 2, in the low half
@@ -411,7 +412,8 @@ int bs_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
  * The gradient with respect to the logits, from those with respect to logprob and entropy:
  *   grad[t][v] = g_logprob[t] ([v == target] - p[t][v]) - g_entropy[t] p[t][v] (log p[t][v] + entropy[t])
  * lse, entropy  DEVICE in   as bs_logprobs gave them          g_logprob, g_entropy  DEVICE in  T fp32 each
- * grad          DEVICE out  T rows of V, same type as the logits, ldg >= V apart; may be the logits themselves
+ * grad          DEVICE out  T rows of V, same type as the logits, ldg >= V apart; may be the logits themselves, or lie beside
+ *               them (rows that share memory with theirs otherwise: BS_ERR_UNSUPPORTED)
  * entropy and g_entropy may both be NULL: the log probability's gradient alone.  A row without a target has that of its
  * entropy alone, one with a target that is not below V NaN; a row in which nothing is left (lse <= -1e30: all words -inf, or all
  * the lowest fp32 / bfloat16 number) 0.  lse's rounding is a factor of the row's p: 1e-5 at most, or a sixteenth of the rounding of

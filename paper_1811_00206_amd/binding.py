@@ -823,7 +823,7 @@ def bs_logprobs(logits, targets, top_n: int = 0, workspace=None):
 
 def bs_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entropy, out=None):
     """The gradient [T, V], of the logits' type, from those of logprob and entropy [T]; lse and entropy as bs_logprobs gave
-    them.  entropy and g_entropy may both be None.  `out` may be the logits."""
+    them.  entropy and g_entropy may both be None.  `out` may be the logits, or lie beside them, but not overlap them at another place."""
     done = (_native or _calls()).logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entropy, out)
     if done is not None:
         return done

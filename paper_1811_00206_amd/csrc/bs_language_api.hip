@@ -28,6 +28,21 @@ bool aligned4(const void* a, const void* b, const void* c, const void* d) {
     return aligned(a, 4) && aligned(b, 4) && aligned(c, 4) && aligned(d, 4);
 }
 
+// Whether a row at a + i * pa and one at b + j * pb, of n bytes each, share any: rows of one tensor do not, and n <= pa, pb.
+bool rows_meet(uintptr_t a, int64_t pa, uintptr_t b, int64_t pb, int64_t rows, int64_t n) {
+    const int64_t d = (int64_t)(b - a);
+    if (d >= (rows - 1) * pa + n || -d >= (rows - 1) * pb + n) return false;
+    // rows of a to look at: where both are equally far apart the same distances come again, so that one with all b beside it will do
+    const auto meets = [&](int64_t i) {
+        const int64_t to = i * pa - d, j = to >= 0 ? to / pb : -1;      // the last row of b that starts at or before it
+        return (j >= 0 && j < rows && to - j * pb < n) || (j + 1 < rows && (j + 1) * pb - to < n);
+    };
+    if (pa == pb) return meets(d >= 0 ? rows - 1 : 0);
+    for (int64_t i = 0; i < rows; ++i)
+        if (meets(i)) return true;
+    return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -124,8 +139,12 @@ int bs_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, in
     const int st = check_logits(logits, dtype, T, V, ld, targets);
     if (st) return st;
     if (ldg < V) return BS_ERR_SHAPE;
-    if (grad == logits && ldg != ld) return BS_ERR_UNSUPPORTED;
-    if (!aligned(grad, bs::dtype_bytes(dtype)) || !aligned4(lse, entropy, g_logprob, g_entropy)) return BS_ERR_ALIGN;
+    const int64_t size = bs::dtype_bytes(dtype);
+    if (!aligned(grad, size)) return BS_ERR_ALIGN;
+    if ((grad != logits || ldg != ld) &&
+        rows_meet(reinterpret_cast<uintptr_t>(logits), ld * size, reinterpret_cast<uintptr_t>(grad), ldg * size, T, V * size))
+        return BS_ERR_UNSUPPORTED;
+    if (!aligned4(lse, entropy, g_logprob, g_entropy)) return BS_ERR_ALIGN;
     return bs::launch_logprobs_backward(logits, dtype, T, V, ld, targets, lse, entropy, g_logprob, g_entropy, grad, ldg,
                                         static_cast<hipStream_t>(stream));
 }

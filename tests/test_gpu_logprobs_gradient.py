@@ -67,3 +67,22 @@ def test_rows_as_far_as_lse_is_not_rounded_away(V, dtype, lost):
     x = torch.randn((9, V), generator=torch.Generator().manual_seed(V)) * 3 + at
     targets = torch.randint(-1, V, (9,), generator=torch.Generator().manual_seed(V + 1))
     check(x.to(TYPES[dtype]).cuda(), targets.cuda(), V, lost)
+
+
+def test_gradient_beside_the_logits_and_on_them():
+    """The other half of the logits' rows holds it, or the logits do; a place in between is refused."""
+    V = 301
+    wide = torch.zeros((5, 2 * V), device="cuda")
+    x, targets = torch.randn((5, V), generator=torch.Generator().manual_seed(1)).cuda(), torch.tensor([0, 5, -1, 300, 7]).cuda()
+    _, entropy, lse, _, _ = bs.bs_logprobs(x, targets)
+    one = torch.ones(5, device="cuda")
+    want = bs.bs_logprobs_backward(x, targets, lse, entropy, one, one)
+    wide[:, :V] = x
+    got = bs.bs_logprobs_backward(wide[:, :V], targets, lse, entropy, one, one, out=wide[:, V:])
+    torch.testing.assert_close(got, want, rtol=1e-6, atol=1e-7)
+    assert torch.equal(wide[:, :V], x)
+    for out in (wide[:, 1:V + 1], wide[:, V - 1:2 * V - 1]):
+        with pytest.raises(bs.BsError) as e:
+            bs.bs_logprobs_backward(wide[:, :V], targets, lse, entropy, one, one, out=out)
+        assert e.value.status == 3
+    assert torch.equal(wide[:, :V], x)
