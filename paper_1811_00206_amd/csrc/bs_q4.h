@@ -412,6 +412,7 @@ __device__ __forceinline__ float sum_of_wave(float v) { return add_across_32(add
 // and may load all of them with that scope.  Sums stored that way are where everybody sees them as soon as each lane has waited
 // for its own; a fence of that scope would write back all that the cache holds, which took 16 us.  `found`: a word of LDS.
 __device__ __forceinline__ bool last_of(uint32_t* done, int all, int* found) {
+    pin_order();      // the wait is for all stores before it, and the count comes after it
     wait_vm_and_lds<0>();
     pin_order();
     __syncthreads();
