@@ -622,6 +622,15 @@ __device__ __forceinline__ Shift shift_of(const Row<XT>& row) {
     return {m, logf(s)};
 }
 
+// exp(x).  EXACT: with what x log2(e) loses as one rounded product (2^-18 of the result at x = -80), by a first-order factor.
+template <bool EXACT>
+__device__ __forceinline__ float exp_of(float x) {
+    const float u = x * kLog2e, p = exp2_hw(u);
+    if constexpr (!EXACT) return p;
+    constexpr float kLow = 1.92596299112662e-8f, kLn2 = 0.693147180559945f;      // log2(e) - kLog2e
+    return fmaf(p, fmaf(x, kLow, fmaf(x, kLog2e, -u)) * kLn2, p);
+}
+
 // |lse| up to which the gradient goes by it.  It is rounded, and what it lost is a factor of all of the row's p: up to 2^-17 below 256, less
 // than a row's sums are off by; 2^-15 below 1024 and 2^-13 below 4096, a sixteenth of a binary16 result's rounding and less of a
 // bfloat16 one's.
@@ -653,7 +662,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(BackArgs g)
     const auto gradient = [&](float logp, bool hit) {
         if (empty) logp = -1e4f;
         logp = at_least(logp, -1e4f);      // exp of which is 0
-        const float v = exp2_hw(logp * kLog2e) * fmaf(-gh, logp, at0);
+        const float v = exp_of<sizeof(T) == 4>(logp) * fmaf(-gh, logp, at0);
         return XT::store(hit ? v + gl : v);
     };
     const auto write = [&](int64_t v, const float (&x)[E], auto&& logp) {

@@ -86,3 +86,19 @@ def test_gradient_beside_the_logits_and_on_them():
             bs.bs_logprobs_backward(wide[:, :V], targets, lse, entropy, one, one, out=out)
         assert e.value.status == 3
     assert torch.equal(wide[:, :V], x)
+
+
+@pytest.mark.parametrize("together", [True, False])
+def test_small_probabilities_in_fp32(together):
+    """Logits that are log probabilities already, lse 0: exp(x) is off by a unit of the power of two's last place and two roundings,
+    whatever the size of x.  (Sums of what remains are within a rounding of 1, and lse = 0 is what they have.)"""
+    V = 4001
+    x = torch.linspace(-87.0, -1e-3, V + 2).unsqueeze(0).cuda()
+    x = x[:, 1:V + 1] if not together else x[:, :V].contiguous()
+    zero, one = torch.zeros(1, device="cuda"), torch.full((1,), -1.0, device="cuda")
+    target = torch.tensor([5], device="cuda")
+    got = bs.bs_logprobs_backward(x, target, zero, None, one, None).cpu().double()[0]
+    want = x.cpu().double()[0].exp()
+    off = ((got - want).abs() / want)
+    off[5] = 0.0
+    assert float(off.max()) <= 2.0**-21, float(off.max())
