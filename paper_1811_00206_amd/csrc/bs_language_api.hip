@@ -93,7 +93,7 @@ int bs_q4_gemv(const uint8_t* codes, const uint16_t* scales, int64_t M, int64_t 
 }
 
 size_t bs_q4_moe_workspace_bytes(int dtype, int64_t T, int64_t D, int64_t F, int E, int top_k, int group) {
-    if (T < 1 || T > BS_MOE_TOKENS_MAX || !matrix_ok(D, F) || 2 * F > kMost || !limits_ok(D, F, group) || !type_ok(dtype)) return 0;
+    if (T < 1 || T > BS_MOE_TOKENS_MAX || !matrix_ok(D, F) || F > kMost / 2 || !limits_ok(D, F, group) || !type_ok(dtype)) return 0;
     if (E < 1 || E > BS_MOE_EXPERTS_MAX || top_k < 1 || top_k > E || top_k > BS_MOE_TOP_K_MAX) return 0;
     return bs::q4_moe_workspace_bytes(dtype, T, D, F, E, top_k);
 }

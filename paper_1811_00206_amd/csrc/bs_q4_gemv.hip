@@ -356,16 +356,12 @@ Plan plan_for(int dtype, int64_t M, int64_t K, int64_t N) {
 template <typename XT, int GL, int U>
 int launch_staged(const GemvArgs& g, const Plan& p, hipStream_t st) {
     using Reg = LdsKernelOf<q4_gemv_kernel<XT, GL, U>>;
+    using Own = LdsKernelOf<q4_gemv_own_kernel<XT, GL, U>>;
     if (p.lds > kLdsWithoutLimit) {
-        const int rc = ensure_lds_limit(Reg::reg, st);
+        const int rc = p.own ? ensure_lds_limit(Own::reg, st) : ensure_lds_limit(Reg::reg, st);
         if (rc != BS_OK) return rc;
     }
     if (p.own) {
-        using Own = LdsKernelOf<q4_gemv_own_kernel<XT, GL, U>>;
-        if (p.lds > kLdsWithoutLimit) {
-            const int rc = ensure_lds_limit(Own::reg, st);
-            if (rc != BS_OK) return rc;
-        }
         hipLaunchKernelGGL((q4_gemv_own_kernel<XT, GL, U>), dim3((unsigned)((g.M + 15) / 16)), dim3(64 * p.ways), p.lds, st, g);
         return hip_status(hipGetLastError());
     }

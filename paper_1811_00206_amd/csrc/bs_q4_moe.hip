@@ -570,7 +570,7 @@ int launch_up(MoeArgs g, hipStream_t st) {
     if (rc != BS_OK) return rc;
     if (g.routed) {
         const int lds = route_bytes(g.pairs, g.E);
-        hipLaunchKernelGGL(moe_route_kernel, dim3(1), dim3(g.T < 4 ? 256 : g.T < 16 ? 64 * g.T : 1024), lds, st, g);
+        hipLaunchKernelGGL(moe_route_kernel, dim3(1), dim3(g.T < 16 ? 64 * g.T : 1024), lds, st, g);
         rc = hip_status(hipGetLastError());
         if (rc != BS_OK) return rc;
     }
