@@ -638,6 +638,7 @@ def bs_reprune(vals, idx, bank: int, k2: int, out=None):
 
 
 # ---- language models: 4-bit matrices, expert layers, log probabilities
+# (Results carry no autograd graph, whatever the inputs ask for: the gradient is bs_logprobs_backward's.)
 
 MOE_TOKENS_MAX, MOE_TOP_K_MAX, LOGPROBS_TOP_MAX = 65536, 32, 64      # as in bs.h
 _TYPES = {torch.float32: BS_F32, torch.float16: BS_F16, torch.bfloat16: BS_BF16}
@@ -802,7 +803,8 @@ def bs_logprobs_workspace_bytes(dtype: int, T: int, V: int, top_n: int) -> int:
 
 def bs_logprobs(logits, targets, top_n: int = 0, workspace=None):
     """Rows of logits [T, V] and an int64 target each (negative: none) -> (logprob [T], entropy [T], lse [T],
-    top_values [T, top_n], top_ids int32 [T, top_n]), all float32 but the ids."""
+    top_values [T, top_n], top_ids int32 [T, top_n]), all float32 but the ids.  No autograd: logits that require a gradient
+    get it from bs_logprobs_backward."""
     done = (_native or _calls()).logprobs(logits, targets, top_n, workspace)
     if done is not None:
         return done

@@ -20,8 +20,8 @@
 // Measured: 4096 rows of 32003 bfloat16 logits with the 5 largest in 59 us (4.4 TB/s; 45 at the rate of reads), 56 without
 // alternatives.  The vector ALU is busy about 40 us of it (conversion, maximum, two for u, an exponential of four, two sums, and two
 // of loads and copies, an element); eight wavefronts a SIMD instead of seven, and no checks of edges inside a row, changed
-// nothing.  One row of 131072 fp32
-// logits: 8.2 us in 16 slices, 4.6 to join them.  The gradient of 4096 x 32003: 106 us, 102 at the rate of a copy.
+// nothing.  One row of 131072 fp32 logits, a batch for every thread of 16 workgroups: 4.8 us, and 2.2 to join them; with the 20
+// largest 8.1 and 4.8.  The gradient of 4096 x 32003: 106 us, 102 at the rate of a copy.
 #include "bs_q4.h"
 
 namespace bs {
@@ -640,7 +640,7 @@ constexpr float kLseMost = sizeof(typename XT::type) == 4 ? 256.f : XT::kHalf ? 
 // d = p * -(g_lp + g_H (log p + H)), and g_lp at the target.  A large lse has lost what a difference of logits needs (1000 words that a mask of
 // -1e9 leaves alike would have a probability of 1 each): such rows are summed up once more, by one of the row's workgroups, which then
 // has all of it.  Not the first of each row: with eight workgroups a row those all run on the same XCD, and 4096 x 32003 in bfloat16 take 669
-// us instead of 363 (107 where lse serves).  700 x 10000 in fp32 19 us instead of 10.4, one row of 131072 60 instead of 4.5.
+// us instead of 363 (107 where lse serves).  700 x 10000 in fp32 19.5 us instead of 10.4, one row of 131072 64 instead of 4.5.
 template <typename XT>
 __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(BackArgs g) {
     using T = typename XT::type;

@@ -342,8 +342,11 @@ Plan plan_for(int dtype, int64_t M, int64_t K, int64_t N) {
         p.split = parts;
         p.part_chunks = part;
     }
-    // 16-bit vectors as they are, unless rows a power of two apart and half lines cost more than a kernel that lays them out
-    // (about 3 us): 16384 x 8192 for 32 vectors 32 us as they are, 23 + 3 as tiles; 6000 x 3000 for 16 vectors 5.5 and 5.6 + 2.
+    // 16-bit vectors as they are, unless the matrix is large: every 16 * R rows of it read all of x, in pieces of 16 rows of half a line
+    // each, which then costs more than a kernel that lays x out once.  A call for 7 / 16 / 32 bfloat16 vectors, as they are and as tiles:
+    // 6000 x 3000 6.2 / 6.5 / 9.2 and 7.6 / 7.6 / 8.8 us, 4096 x 8192 9.8 / 12.9 / 20.5 and 10.4 / 10.5 / 13.0, 8192 x 8192 12.9 / 16.7 / 23.8
+    // and 13.9 / 14.1 / 16.9, 8192 x 8200 12.1 / 13.5 / 19.2 and 13.8 / 14.0 / 17.0, 4096 x 25088 21 / 31 / 53 and 20 / 20 / 27.  (The size alone does
+    // not tell all: more vectors, and rows a power of two apart, favour tiles sooner.)
     p.tiled = dtype == BS_F32 || p.nt == 4 || p.split > 1 || M * K >= ((int64_t)1 << 26);
     p.lds = (size_t)p.ways * p.r * p.nt * tpt * 16 * 4;
     p.parts = (size_t)((N + tpt - 1) / tpt) * 32 * q4_padded(K);

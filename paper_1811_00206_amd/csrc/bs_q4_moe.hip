@@ -17,9 +17,9 @@
 // bfloat16 parts, all 24 bits, for 16-bit activations too: in two parts, 16 bits, their rounding was seen where the sum over F
 // cancels.
 //
-// Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 38 to 42 us (logits 4.8, route 4.8, up 18 to 22 as 32 or
-// more experts are chosen, down 14.6; 18.4 at the rate of reads).  16 tokens, 8 each: up 31, down 30.  One token of 1500 x 1500 in
-// fp32, 2 of 8: 14.9 us, up 10, down 5.5.
+// Measured: 7 tokens of 2048 x 1024 in bfloat16, 6 of 64 experts each: 40 to 42 us a call (logits 4, route 3.8, up 18 to 22 as 32 or
+// more experts are chosen, down 14.8; 18.4 at the rate of reads).  16 tokens, 8 each: up 32, down 32.  One token of 1500 x 1500 in
+// fp32, 2 of 8: 15.2 us, up 9.5, down 4.9.  More than 64 tokens pay for each 64 anew: 256 of those 64 experts, 6 each, 430 us.
 #include "bs_q4.h"
 
 #include <algorithm>
