@@ -424,6 +424,83 @@ int bs_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, in
                          const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,
                          void* grad, int64_t ldg, void* stream);
 
+/* ---- language models: several hypotheses at once -----------------------------------
+ *
+ * Matrices and activations in MX 4-bit with their products, one step of beam search, and the states that follow it.
+ * Types, streams, errors and outputs as in the section before.
+ *
+ * Format of an MX matrix M x K: codes are the E2M1 numbers of a 4-bit matrix above, and every 32 consecutive elements of a row
+ * (a block) share one scale byte s, which stands for 2^(s - 127); 255 makes the block NaN.  A row takes 64 * ceil(K / 128) bytes of
+ * codes and 4 * ceil(K / 128) of scales; behind K codes are 0, and scales of blocks that hold no element 127.  M, K <= 2^24.
+ * Codes must be 16-byte aligned, scales 4-byte.
+ */
+size_t bs_mx4_codes_bytes(int64_t M, int64_t K);               /* 0 if the shape is invalid */
+size_t bs_mx4_scales_bytes(int64_t M, int64_t K);
+
+/*
+ * W  DEVICE in   M rows of K, ld >= K elements apart
+ * With e the biased exponent of a block's largest magnitude as fp32 (0 for subnormal numbers): s = max(e - 2, 0), and the code is the
+ * number nearest to w * 2^(127 - s), the even code of two that are equally near, 6 for all that is larger; its sign is w's.
+ * A block that holds an infinity or a NaN: s = 255, codes 0.
+ */
+int bs_mx4_pack(const void* W, int dtype, int64_t M, int64_t K, int64_t ld, uint8_t* codes, uint8_t* scales, void* stream);
+/* W  DEVICE out  M x K, contiguous: the values the codes stand for, rounded to dtype */
+int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, void* W, int dtype, void* stream);
+
+/*
+ * y[n][r] = sum_k W[r][k] * X[n][k] (+ bias[r]) for N rows of activations, where X is x as bs_mx4_pack would round it: the matrix
+ * unit multiplies 4-bit numbers on both sides.
+ * x     DEVICE in   N rows of K of type dtype, ldx >= K apart       y  DEVICE out  N rows of M, same type, ldy >= M apart
+ * bias  DEVICE in   M fp32, may be NULL
+ * bs_mx4_gemm_packed takes x packed already (an activation that several matrices multiply); dtype is y's type there.
+ * Products are exact, sums fp32.  The order of the additions depends on M, K, N and dtype alone, and is the same in both calls but for
+ * N <= BS_MX4_FUSED_MAX.  A NaN or an infinity in x makes its row of y NaN, a block of W that is NaN its column.  N <= 2^24.
+ * workspace as for bs_spmm.
+ */
+#define BS_MX4_FUSED_MAX 2
+size_t bs_mx4_gemm_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N);
+int bs_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int dtype, int64_t N, int64_t ldx,
+                const float* bias, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+size_t bs_mx4_gemm_packed_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N);
+int bs_mx4_gemm_packed(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const uint8_t* x_codes,
+                       const uint8_t* x_scales, int64_t N, const float* bias, void* y, int dtype, int64_t ldy, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * One step of beam search for B sequences of W beams each: of all continuations, the n with the best score.
+ *   a beam w that goes on offers every word v:  scores[b][w] + logits[b][w][v] - lse(logits[b][w])
+ *   a beam that is finished offers itself:      scores[b][w], with the word `end`
+ * logits    DEVICE in   B * W rows of V, ld >= V apart (V < 2^31; only as aligned as the type)
+ * scores    DEVICE in   B x W fp32, the beams' log probabilities
+ * finished  DEVICE in   B x W bytes, not 0 where a beam is finished; may be NULL.  Rows of finished beams are not read.
+ * end       the word that finishes a beam; negative: none does (finished ones then offer word 0)
+ * out_scores, out_tokens, out_parents, out_finished  DEVICE out  B x n, best first: score, word, the beam it continues, and whether it
+ *           is finished (one byte, 0 or 1)
+ * Scores are compared in 64 bits before they are rounded to fp32; the lower beam, then the lower word comes first among equals.
+ * What offers nothing: a word whose logit is -inf; a beam whose score is not finite; a beam that goes on with a logit that is NaN or
+ * +inf.  Where fewer than n continuations are left the rest have score -inf, word max(end, 0), parent min(place, W - 1), and are finished.
+ * 1 <= W <= BS_BEAM_WIDTH_MAX, 1 <= n <= BS_BEAM_WIDTH_MAX.  workspace as for bs_spmm.
+ */
+#define BS_BEAM_WIDTH_MAX 64
+size_t bs_beam_step_workspace_bytes(int dtype, int64_t B, int W, int64_t V, int n);
+int bs_beam_step(const void* logits, int dtype, int64_t B, int W, int64_t V, int64_t ld, const float* scores, const uint8_t* finished,
+                 int64_t end, int n, float* out_scores, int32_t* out_tokens, int32_t* out_parents, uint8_t* out_finished,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * States of beams follow their parents: row b * W + j of outs[i] becomes row b * W + parents[b][j] of states[i], for `count` tensors
+ * of B * W rows in one launch.  The arrays themselves are HOST memory and are not kept.
+ * states[i]  DEVICE in   rows of row_bytes[i] bytes, pitch[i] >= row_bytes[i] bytes apart
+ * outs[i]    DEVICE out  the same, out_pitch[i] bytes apart; may be states[i] with the same pitch (each row is read before any is
+ *            overwritten); what overlaps another output, or an input otherwise: BS_ERR_UNSUPPORTED
+ * parents    DEVICE in   B x W int32; a number outside 0 .. W - 1 stands for the beam itself
+ * 1 <= count <= BS_REORDER_STATES_MAX, 1 <= W <= BS_BEAM_WIDTH_MAX, B <= 2^24; the states of one beam have 2^30 bytes together at most,
+ * pitches are below 2^32.  Bytes between rows stay as they are.
+ */
+#define BS_REORDER_STATES_MAX 32
+int bs_beam_reorder(int count, const void* const* states, void* const* outs, const int64_t* row_bytes, const int64_t* pitch,
+                    const int64_t* out_pitch, int64_t B, int W, const int32_t* parents, void* stream);
+
 /* ---- dense baseline the sparse path is compared with (Sec. 4: the paper's
  *      dense column; here a hand-written kernel on the same GPU) ----------- */
 

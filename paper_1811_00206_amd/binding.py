@@ -29,6 +29,8 @@ EXPORTS = (
     "bs_idx_bytes_wide", "bs_prune_pack_wide", "bs_spmv_wide", "bs_spmm_workspace_bytes_wide", "bs_spmm_plan_wide", "bs_spmm_wide",
     "bs_q4_codes_bytes", "bs_q4_scales_bytes", "bs_q4_pack", "bs_q4_unpack", "bs_q4_gemv_workspace_bytes", "bs_q4_gemv",
     "bs_q4_moe_workspace_bytes", "bs_q4_moe", "bs_logprobs_workspace_bytes", "bs_logprobs", "bs_logprobs_backward",
+    "bs_mx4_codes_bytes", "bs_mx4_scales_bytes", "bs_mx4_pack", "bs_mx4_unpack", "bs_mx4_gemm_workspace_bytes", "bs_mx4_gemm",
+    "bs_mx4_gemm_packed_workspace_bytes", "bs_mx4_gemm_packed", "bs_beam_step_workspace_bytes", "bs_beam_step", "bs_beam_reorder",
 )
 
 
@@ -112,6 +114,20 @@ def load_library():
     lib.bs_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.bs_logprobs_backward.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     for name in ("bs_q4_pack", "bs_q4_unpack", "bs_q4_gemv", "bs_q4_moe", "bs_logprobs", "bs_logprobs_backward"):
+        getattr(lib, name).restype = i32
+    lib.bs_mx4_codes_bytes.argtypes = lib.bs_mx4_scales_bytes.argtypes = [i64, i64]
+    lib.bs_mx4_gemm_workspace_bytes.argtypes = lib.bs_mx4_gemm_packed_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    lib.bs_beam_step_workspace_bytes.argtypes = [i32, i64, i32, i64, i32]
+    for name in ("bs_mx4_codes_bytes", "bs_mx4_scales_bytes", "bs_mx4_gemm_workspace_bytes", "bs_mx4_gemm_packed_workspace_bytes",
+                 "bs_beam_step_workspace_bytes"):
+        getattr(lib, name).restype = sz
+    lib.bs_mx4_pack.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+    lib.bs_mx4_unpack.argtypes = [vp, vp, i64, i64, vp, i32, vp]
+    lib.bs_mx4_gemm.argtypes = [vp, vp, i64, i64, vp, i32, i64, i64, vp, vp, i64, vp, sz, vp]
+    lib.bs_mx4_gemm_packed.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp, vp, i32, i64, vp, sz, vp]
+    lib.bs_beam_step.argtypes = [vp, i32, i64, i32, i64, i64, vp, vp, i64, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.bs_beam_reorder.argtypes = [i32, vp, vp, vp, vp, vp, i64, i32, vp, vp]
+    for name in ("bs_mx4_pack", "bs_mx4_unpack", "bs_mx4_gemm", "bs_mx4_gemm_packed", "bs_beam_step", "bs_beam_reorder"):
         getattr(lib, name).restype = i32
     lib.bs_init.argtypes = []
     for name in ("bs_init", "bs_prune_pack", "bs_spmv", "bs_spmv_ex", "bs_spmm", "bs_spmm_static", "bs_dense_gemv",
@@ -845,3 +861,219 @@ def bs_logprobs_backward(logits, targets, lse, entropy, g_logprob, g_entropy, ou
     _check(load_library().bs_logprobs_backward(_ptr(logits), code, T, V, ld, _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(g_logprob),
                                                _ptr(g_entropy), _ptr(grad), ldg, _stream()), "bs_logprobs_backward")
     return grad
+
+
+# ---- language models: several hypotheses at once (MX 4-bit matrices, beam search)
+# Tensors of these calls have to be on the current device, whose current stream takes the work.
+
+BEAM_WIDTH_MAX, REORDER_STATES_MAX = 64, 32      # as in bs.h
+
+
+def _here(t, what: str):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a tensor on the GPU")
+    if t.device.index != _calls().device():
+        raise ValueError(f"{what} is not on the current device")
+    return t
+
+
+def _mx4(codes, scales, K: int, what: str = "codes"):
+    """Checks an MX matrix [.., M, K]: returns the number of its rows."""
+    _dev(_here(codes, what), what, torch.uint8)
+    _dev(_here(scales, "scales"), "scales", torch.uint8)
+    chunks = -(-K // 128)
+    if codes.dim() < 2 or K < 1 or codes.shape[-1] != 64 * chunks:
+        raise ValueError(f"{what} must be [.., M, {64 * chunks}] for K = {K}")
+    if tuple(scales.shape) != (*codes.shape[:-1], 4 * chunks):
+        raise ValueError(f"scales must be {[*codes.shape[:-1], 4 * chunks]}")
+    return codes.numel() // codes.shape[-1]
+
+
+def bs_mx4_codes_bytes(M: int, K: int) -> int:
+    return load_library().bs_mx4_codes_bytes(M, K)
+
+
+def bs_mx4_scales_bytes(M: int, K: int) -> int:
+    return load_library().bs_mx4_scales_bytes(M, K)
+
+
+def bs_mx4_pack(W):
+    """W [.., M, K] on the GPU (float32, float16 or bfloat16; contiguous, or 2-D with contiguous rows) -> (codes uint8
+    [.., M, 64 * ceil(K / 128)], scales uint8 [.., M, 4 * ceil(K / 128)]): E2M1 numbers, two a byte, with a power of two for every
+    32 elements of a row."""
+    done = (_native or _calls()).mx4_pack(W)
+    if done is not None:
+        return done
+    code = _type_code(_here(W, "W"), "W")
+    if W.dim() < 2:
+        raise ValueError("W must be [.., M, K]")
+    K = W.shape[-1]
+    M = W.numel() // max(K, 1)
+    ld = K if W.is_contiguous() else _rows(W, "W", W.dtype)
+    chunks = -(-K // 128)
+    codes = torch.empty((*W.shape[:-1], 64 * chunks), dtype=torch.uint8, device=W.device)
+    scales = torch.empty((*W.shape[:-1], 4 * chunks), dtype=torch.uint8, device=W.device)
+    _check(load_library().bs_mx4_pack(_ptr(W), code, M, K, ld, _ptr(codes), _ptr(scales), _stream()), "bs_mx4_pack")
+    return codes, scales
+
+
+def bs_mx4_unpack(codes, scales, K: int, dtype=torch.float32, out=None):
+    """The values [.., M, K] that an MX matrix stands for, rounded to dtype (of `out`, if it is given)."""
+    done = (_native or _calls()).mx4_unpack(codes, scales, K, _TYPES.get(dtype), out)
+    if done is not None:
+        return done
+    M = _mx4(codes, scales, K)
+    if out is None:
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+        out = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
+    code = _type_code(_dev(_here(out, "out"), "out"), "out")
+    if out.numel() != M * K:
+        raise ValueError(f"out must be {[*codes.shape[:-1], K]}")
+    _check(load_library().bs_mx4_unpack(_ptr(codes), _ptr(scales), M, K, _ptr(out), code, _stream()), "bs_mx4_unpack")
+    return out
+
+
+def bs_mx4_gemm_workspace_bytes(dtype: int, M: int, K: int, N: int) -> int:
+    return load_library().bs_mx4_gemm_workspace_bytes(dtype, M, K, N)
+
+
+def bs_mx4_gemm_packed_workspace_bytes(dtype: int, M: int, K: int, N: int) -> int:
+    return load_library().bs_mx4_gemm_packed_workspace_bytes(dtype, M, K, N)
+
+
+def _bias(bias, M: int):
+    if bias is not None:
+        _dev(_here(bias, "bias"), "bias", torch.float32)
+        if tuple(bias.shape) != (M,):
+            raise ValueError(f"bias must be [{M}]")
+    return bias
+
+
+def _product(out, shape, like, dtype):
+    """The place of a product and its leading dimension."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=like.device), shape[-1]
+    if tuple(_here(out, "out").shape) != tuple(shape):
+        raise ValueError(f"out must be {list(shape)}")
+    return out, _rows(out if out.dim() == 2 else _dev(out, "out").unsqueeze(0), "out", dtype)
+
+
+def bs_mx4_gemm(codes, scales, x, bias=None, out=None, workspace=None):
+    """W . x (+ bias) for an MX matrix [M, K] and x [K] -> y [M], or one row per vector, x [N, K] -> y [N, M], of x's type
+    (float32, float16, bfloat16); x is rounded to MX 4-bit on the way, as bs_mx4_pack does.  bias: float32 [M].  Rows of x and `out` may be
+    slices of wider ones.  `workspace`: at least bs_mx4_gemm_workspace_bytes(...) bytes, or one from torch's allocator."""
+    y = (_native or _calls()).mx4_gemm(codes, scales, x, bias, out, workspace)
+    if y is not None:
+        return y
+    code = _type_code(_here(x, "x"), "x")
+    if x.dim() not in (1, 2):
+        raise ValueError("x must be [K] or [N, K]")
+    X = x if x.dim() == 2 else _dev(x, "x").unsqueeze(0)
+    ldx, (N, K) = _rows(X, "x", x.dtype), X.shape
+    M = _mx4(codes, scales, K)
+    if codes.dim() != 2:
+        raise ValueError("codes must be [M, ..]")
+    _bias(bias, M)
+    lib = load_library()
+    workspace, ws_bytes = _own_workspace(workspace, lib.bs_mx4_gemm_workspace_bytes(code, M, K, N), x.device)
+    y, ldy = _product(out, (*x.shape[:-1], M), x, x.dtype)
+    _check(lib.bs_mx4_gemm(_ptr(codes), _ptr(scales), M, K, _ptr(x), code, N, ldx, _ptr(bias), _ptr(y), ldy, _ptr(workspace), ws_bytes,
+                           _stream()), "bs_mx4_gemm")
+    return y
+
+
+def bs_mx4_gemm_packed(codes, scales, x_codes, x_scales, K: int, dtype=torch.float32, bias=None, out=None, workspace=None):
+    """The same for activations that are MX rows already (bs_mx4_pack of x [N, K]): y [N, M] of type dtype."""
+    y = (_native or _calls()).mx4_gemm_packed(codes, scales, x_codes, x_scales, K, _TYPES.get(dtype), bias, out, workspace)
+    if y is not None:
+        return y
+    if dtype not in _TYPES:
+        raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+    M, N, code = _mx4(codes, scales, K), _mx4(x_codes, x_scales, K, "x_codes"), _TYPES[dtype]
+    if codes.dim() != 2 or x_codes.dim() != 2:
+        raise ValueError("codes must be [M, ..] and x_codes [N, ..]")
+    _bias(bias, M)
+    lib = load_library()
+    workspace, ws_bytes = _own_workspace(workspace, lib.bs_mx4_gemm_packed_workspace_bytes(code, M, K, N), codes.device)
+    y, ldy = _product(out, (N, M), codes, dtype)
+    _check(lib.bs_mx4_gemm_packed(_ptr(codes), _ptr(scales), M, K, _ptr(x_codes), _ptr(x_scales), N, _ptr(bias), _ptr(y), code, ldy,
+                                  _ptr(workspace), ws_bytes, _stream()), "bs_mx4_gemm_packed")
+    return y
+
+
+def bs_beam_step_workspace_bytes(dtype: int, B: int, W: int, V: int, n: int) -> int:
+    return load_library().bs_beam_step_workspace_bytes(dtype, B, W, V, n)
+
+
+def bs_beam_step(logits, scores, finished=None, end: int = -1, n=None, workspace=None):
+    """One step of beam search: logits [B * W, V] (float32, float16, bfloat16) and the beams' scores float32 [B, W] -> the n (W, unless it is
+    given) best continuations of each sequence, best first: (scores float32, tokens int32, parents int32, finished bool), all [B, n].
+    finished [B, W] (bool or uint8): beams that stay as they are.  `end`: the word that finishes a beam, -1 for none."""
+    if n is None:
+        n = scores.shape[-1] if isinstance(scores, torch.Tensor) and scores.dim() else 0
+    done = (_native or _calls()).beam_step(logits, scores, finished, end, n, workspace)
+    if done is not None:
+        return done
+    code = _type_code(_here(logits, "logits"), "logits")
+    ld = _rows(logits, "logits", logits.dtype)
+    _dev(_here(scores, "scores"), "scores", torch.float32)
+    if scores.dim() != 2 or scores.numel() != logits.shape[0]:
+        raise ValueError("scores must be [B, W] for logits [B * W, V]")
+    if finished is not None:
+        _dev(_here(finished, "finished"), "finished")
+        if finished.dtype not in (torch.bool, torch.uint8) or finished.shape != scores.shape:
+            raise ValueError("finished must be bool or uint8, shaped like scores")
+    (B, W), V, n, end = scores.shape, logits.shape[1], int(n), int(end)
+    if n < 1 or not -(1 << 63) <= end < 1 << 63:
+        raise BsError(2, "bs_beam_step")
+    lib = load_library()
+    W, n = min(W, BEAM_WIDTH_MAX + 1), min(n, BEAM_WIDTH_MAX + 1)      # more are refused
+    workspace, ws_bytes = _own_workspace(workspace, lib.bs_beam_step_workspace_bytes(code, B, W, V, n), logits.device)
+    out = [torch.empty((B, n), dtype=t, device=logits.device) for t in (torch.float32, torch.int32, torch.int32, torch.bool)]
+    _check(lib.bs_beam_step(_ptr(logits), code, B, W, V, ld, _ptr(scores), _ptr(finished), end, n, *(_ptr(t) for t in out),
+                            _ptr(workspace), ws_bytes, _stream()), "bs_beam_step")
+    return tuple(out)
+
+
+def _beam_rows(t, what: str, B: int, W: int):
+    """Bytes of a row and between the rows of a state [B * W, ..] or [B, W, ..]."""
+    _here(t, what)
+    flat = t.dim() >= 1 and t.shape[0] == B * W
+    if not flat and tuple(t.shape[:2]) != (B, W):
+        raise ValueError(f"{what} must be [{B * W}, ..] or [{B}, {W}, ..]")
+    if t.is_contiguous():
+        size = t.numel() // (B * W) * t.element_size()
+        return size, size
+    if not flat or t.dim() != 2:
+        raise ValueError(f"{what} must be contiguous, or [{B * W}, n] with contiguous rows")
+    return t.shape[1] * t.element_size(), _rows(t, what, t.dtype) * t.element_size()
+
+
+def bs_beam_reorder(states, parents, out=None):
+    """States follow their parents (int32 [B, W], as bs_beam_step gives them): row b * W + j of each state becomes row b * W +
+    parents[b, j].  `states`: a tensor or a list of up to 32, of any type, [B * W, ..] or [B, W, ..]; in place, or to `out` (the same
+    shapes and types), which is returned."""
+    single = isinstance(states, torch.Tensor)
+    given = states if out is None else out
+    states = [states] if single else list(states)
+    to = states if out is None else [out] if isinstance(out, torch.Tensor) else list(out)
+    if (_native or _calls()).beam_reorder(states, parents, None if to is states else to) is not None:
+        return given
+    _dev(_here(parents, "parents"), "parents", torch.int32)
+    if parents.dim() != 2 or not parents.numel():
+        raise ValueError("parents must be [B, W]")
+    B, W = parents.shape
+    if len(to) != len(states):
+        raise ValueError("as many outputs as states")
+    rows = []
+    for i, (s, o) in enumerate(zip(states, to)):
+        a, b = _beam_rows(s, f"state {i}", B, W), _beam_rows(o, f"output {i}", B, W)
+        if s.dtype != o.dtype or s.shape != o.shape:
+            raise ValueError(f"output {i} must have its state's shape and type")
+        rows.append((*a, b[1]))
+    count = len(states)
+    size, pitch, out_pitch = ((ctypes.c_int64 * max(count, 1))(*column) for column in (zip(*rows) if rows else ((), (), ())))
+    pointers = [(ctypes.c_void_p * max(count, 1))(*(t.data_ptr() for t in tensors)) for tensors in (states, to)]
+    _check(load_library().bs_beam_reorder(count, *pointers, size, pitch, out_pitch, B, W, _ptr(parents), _stream()), "bs_beam_reorder")
+    return given

@@ -587,6 +587,264 @@ PyObject* logprobs_backward(PyObject* self, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- several hypotheses at once.  These calls take tensors of the current device only: the stream is that device's.
+
+const at::Tensor* tensor_here(PyObject* obj) {
+    const at::Tensor* t = gpu_tensor(obj);
+    return t && t->device().index() == c10::hip::getCurrentHIPStream().device_index() ? t : nullptr;
+}
+const at::Tensor* tensor_here(PyObject* obj, at::ScalarType type) {
+    const at::Tensor* t = tensor_here(obj);
+    return t && t->scalar_type() == type && t->is_contiguous() ? t : nullptr;
+}
+
+// an MX matrix: codes [.., M, 64 * ceil(K / 128)] and scales [.., M, 4 * ceil(K / 128)]
+struct Mx4 {
+    const at::Tensor *codes, *scales;
+    int64_t M;
+    bool read(PyObject* c, PyObject* s, int64_t K) {
+        codes = tensor_here(c, at::kByte);
+        scales = tensor_here(s, at::kByte);
+        if (!codes || !scales || K < 1) return false;
+        const int64_t d = codes->dim(), chunks = (K + 127) / 128;
+        if (d < 2 || scales->dim() != d || codes->size(d - 1) != 64 * chunks || scales->size(d - 1) != 4 * chunks) return false;
+        for (int64_t i = 0; i < d - 1; ++i)
+            if (codes->size(i) != scales->size(i)) return false;
+        M = codes->numel() / codes->size(d - 1);
+        return M >= 1;
+    }
+    const uint8_t* c() const { return static_cast<const uint8_t*>(codes->const_data_ptr()); }
+    const uint8_t* s() const { return static_cast<const uint8_t*>(scales->const_data_ptr()); }
+};
+
+at::ScalarType type_of(int dtype) { return dtype == BS_F32 ? at::kFloat : dtype == BS_F16 ? at::kHalf : at::kBFloat16; }
+
+// (W) -> (codes, scales)
+PyObject* mx4_pack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 1) Py_RETURN_NONE;
+    const at::Tensor* W = tensor_here(args[0]);
+    if (!W || W->dim() < 2 || !W->numel()) Py_RETURN_NONE;
+    const int dtype = any_dtype(*W);
+    const int64_t K = W->size(-1), M = W->numel() / K;
+    const int64_t ld = W->is_contiguous() ? K : row_pitch(*W, W->scalar_type());
+    if (dtype < 0 || ld < 0) Py_RETURN_NONE;
+    at::Tensor out[2];
+    const int status = enqueue([&](void* st) {
+        at::DimVector size(W->sizes());
+        size.back() = 64 * ((K + 127) / 128);
+        out[0] = at::empty(size, W->options().dtype(at::kByte));
+        size.back() = 4 * ((K + 127) / 128);
+        out[1] = at::empty(size, W->options().dtype(at::kByte));
+        return bs_mx4_pack(W->const_data_ptr(), dtype, M, K, ld, static_cast<uint8_t*>(out[0].mutable_data_ptr()),
+                           static_cast<uint8_t*>(out[1].mutable_data_ptr()), st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_mx4_pack");
+    return tuple_of(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, K, dtype code, out) -> W
+PyObject* mx4_unpack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int K, dtype;
+    Mx4 w;
+    if (n != 5 || !int_arg(args[2], K) || !w.read(args[0], args[1], K)) Py_RETURN_NONE;
+    at::Tensor W;
+    const at::Tensor* out = &W;
+    if (args[4] != Py_None) {
+        if (!(out = tensor_here(args[4])) || !out->is_contiguous() || out->numel() != w.M * K || (dtype = any_dtype(*out)) < 0) Py_RETURN_NONE;
+    } else if (!int_arg(args[3], dtype)) {
+        Py_RETURN_NONE;
+    }
+    const int status = enqueue([&](void* st) {
+        if (out == &W) {
+            at::DimVector size(w.codes->sizes());
+            size.back() = K;
+            W = at::empty(size, w.codes->options().dtype(type_of(dtype)));
+        }
+        return bs_mx4_unpack(w.c(), w.s(), w.M, K, out->mutable_data_ptr(), dtype, st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_mx4_unpack");
+    return result(args[4], W);
+    END_HANDLE_TH_ERRORS
+}
+
+// the place of a product [N, M], or [M] for one row: the caller's or a new one
+struct Product {
+    PyObject* given;
+    at::Tensor own;
+    const at::Tensor* out = &own;
+    int64_t ld;
+    bool read(PyObject* o, at::ScalarType type, bool one, int64_t N, int64_t M) {
+        given = o;
+        ld = M;
+        if (given == Py_None) return true;
+        if (!(out = tensor_here(given)) || out->scalar_type() != type || out->dim() != (one ? 1 : 2)) return false;
+        ld = one ? (out->is_contiguous() ? M : -1) : row_pitch(*out, type);
+        return ld >= 0 && out->size(-1) == M && (one || out->size(0) == N);
+    }
+    void* allocate(const at::TensorOptions& options, bool one, int64_t N, int64_t M) {
+        if (out == &own) own = one ? at::empty({M}, options) : at::empty({N, M}, options);
+        return out->mutable_data_ptr();
+    }
+};
+
+// fp32 [M] or None
+bool bias_arg(PyObject* obj, int64_t M, const float*& p) {
+    p = nullptr;
+    if (obj == Py_None) return true;
+    const at::Tensor* t = tensor_here(obj, at::kFloat);
+    if (!t || t->dim() != 1 || t->size(0) != M) return false;
+    p = static_cast<const float*>(t->const_data_ptr());
+    return true;
+}
+
+// (codes, scales, x, bias, out, workspace) -> y
+PyObject* mx4_gemm(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 6) Py_RETURN_NONE;
+    const at::Tensor* x = tensor_here(args[2]);
+    if (!x || x->dim() < 1 || x->dim() > 2) Py_RETURN_NONE;
+    const int dtype = any_dtype(*x);
+    const bool one = x->dim() == 1;
+    const int64_t N = one ? 1 : x->size(0), K = x->size(-1);
+    const int64_t ldx = one ? (K > 1 && x->stride(0) != 1 ? -1 : K) : row_pitch(*x, x->scalar_type());
+    Mx4 w;
+    Product y;
+    const float* bias;
+    Workspace ws{args[5]};
+    if (dtype < 0 || ldx < 0 || N < 1 || !w.read(args[0], args[1], K) || w.codes->dim() != 2 || !bias_arg(args[3], w.M, bias) ||
+        !y.read(args[4], x->scalar_type(), one, N, w.M) || !ws.read())
+        Py_RETURN_NONE;
+    const size_t need = bs_mx4_gemm_workspace_bytes(dtype, w.M, K, N);
+    const int status = enqueue([&](void* st) {
+        void* yp = y.allocate(x->options(), one, N, w.M);
+        ws.allocate(need, *x);
+        return bs_mx4_gemm(w.c(), w.s(), w.M, K, x->const_data_ptr(), dtype, N, ldx, bias, yp, y.ld, ws.p, ws.bytes, st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_mx4_gemm");
+    return result(args[4], y.own);
+    END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, x_codes, x_scales, K, dtype code, bias, out, workspace) -> y
+PyObject* mx4_gemm_packed(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int K, dtype;
+    Mx4 w, x;
+    if (n != 9 || !int_arg(args[4], K) || !int_arg(args[5], dtype) || !w.read(args[0], args[1], K) || !x.read(args[2], args[3], K)) Py_RETURN_NONE;
+    Product y;
+    const float* bias;
+    Workspace ws{args[8]};
+    if (w.codes->dim() != 2 || x.codes->dim() != 2 || !bias_arg(args[6], w.M, bias) || !y.read(args[7], type_of(dtype), false, x.M, w.M) ||
+        !ws.read())
+        Py_RETURN_NONE;
+    const size_t need = bs_mx4_gemm_packed_workspace_bytes(dtype, w.M, K, x.M);
+    const int status = enqueue([&](void* st) {
+        void* yp = y.allocate(w.codes->options().dtype(type_of(dtype)), false, x.M, w.M);
+        ws.allocate(need, *w.codes);
+        return bs_mx4_gemm_packed(w.c(), w.s(), w.M, K, x.c(), x.s(), x.M, bias, yp, dtype, y.ld, ws.p, ws.bytes, st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_mx4_gemm_packed");
+    return result(args[7], y.own);
+    END_HANDLE_TH_ERRORS
+}
+
+// (logits, scores, finished, end, n, workspace) -> (scores, tokens, parents, finished)
+PyObject* beam_step(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int end, keep;
+    if (n != 6 || !int_arg(args[3], end) || !int_arg(args[4], keep) || keep < 1) Py_RETURN_NONE;
+    const at::Tensor *x = tensor_here(args[0]), *scores = tensor_here(args[1], at::kFloat), *done = nullptr;
+    if (!x || !scores || scores->dim() != 2) Py_RETURN_NONE;
+    const int dtype = any_dtype(*x);
+    const int64_t ld = row_pitch(*x, x->scalar_type()), B = scores->size(0), W = scores->size(1);
+    if (dtype < 0 || ld < 0 || B < 1 || W < 1 || W > BS_BEAM_WIDTH_MAX || x->size(0) != B * W) Py_RETURN_NONE;
+    if (args[2] != Py_None) {
+        done = tensor_here(args[2]);
+        if (!done || !done->is_contiguous() || (done->scalar_type() != at::kBool && done->scalar_type() != at::kByte) || done->sizes() != scores->sizes())
+            Py_RETURN_NONE;
+    }
+    Workspace ws{args[5]};
+    if (!ws.read()) Py_RETURN_NONE;
+    const int64_t V = x->size(1);
+    at::Tensor out[4];
+    const size_t need = bs_beam_step_workspace_bytes(dtype, B, (int)W, V, keep);
+    const int status = enqueue([&](void* st) {
+        const int64_t width = std::min(keep, BS_BEAM_WIDTH_MAX);      // more are refused
+        out[0] = at::empty({B, width}, scores->options());
+        for (int i = 1; i < 4; ++i) out[i] = at::empty({B, width}, scores->options().dtype(i < 3 ? at::kInt : at::kBool));
+        ws.allocate(need, *x);
+        return bs_beam_step(x->const_data_ptr(), dtype, B, (int)W, V, ld, static_cast<const float*>(scores->const_data_ptr()),
+                            done ? static_cast<const uint8_t*>(done->const_data_ptr()) : nullptr, end, keep,
+                            static_cast<float*>(out[0].mutable_data_ptr()), static_cast<int32_t*>(out[1].mutable_data_ptr()),
+                            static_cast<int32_t*>(out[2].mutable_data_ptr()), static_cast<uint8_t*>(out[3].mutable_data_ptr()), ws.p,
+                            ws.bytes, st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_beam_step");
+    return tuple_of(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// rows of a state of B sequences of W beams, [B * W, ..] or [B, W, ..]: bytes of a row and between rows; false if it is none
+bool beam_rows(const at::Tensor& t, int64_t B, int64_t W, int64_t& bytes, int64_t& pitch) {
+    const bool flat = t.dim() >= 1 && t.size(0) == B * W;
+    if (!flat && !(t.dim() >= 2 && t.size(0) == B && t.size(1) == W)) return false;
+    const int64_t size = t.element_size();
+    if (t.is_contiguous()) {
+        bytes = pitch = t.numel() / (B * W) * size;
+        return true;
+    }
+    if (!flat || t.dim() != 2) return false;
+    const int64_t ld = row_pitch(t, t.scalar_type());
+    bytes = t.size(1) * size;
+    pitch = ld * size;
+    return ld >= 0;
+}
+
+// (states, parents, outs): lists of tensors, the second or None -> True
+PyObject* beam_reorder(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 3 || !PyList_CheckExact(args[0]) || (args[2] != Py_None && !PyList_CheckExact(args[2]))) Py_RETURN_NONE;
+    PyObject* const outs = args[2] == Py_None ? args[0] : args[2];
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    const at::Tensor* parents = tensor_here(args[1], at::kInt);
+    if (!parents || parents->dim() != 2 || !parents->numel() || parents->size(1) > BS_BEAM_WIDTH_MAX || count < 1 ||
+        count > BS_REORDER_STATES_MAX || PyList_GET_SIZE(outs) != count)
+        Py_RETURN_NONE;
+    const int64_t B = parents->size(0), W = parents->size(1);
+    const at::Tensor *in[BS_REORDER_STATES_MAX], *to[BS_REORDER_STATES_MAX];
+    int64_t bytes[BS_REORDER_STATES_MAX], pitch[BS_REORDER_STATES_MAX], out_pitch[BS_REORDER_STATES_MAX], out_bytes;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        in[i] = tensor_here(PyList_GET_ITEM(args[0], i));
+        to[i] = tensor_here(PyList_GET_ITEM(outs, i));
+        if (!in[i] || !to[i] || in[i]->scalar_type() != to[i]->scalar_type() || in[i]->sizes() != to[i]->sizes() ||
+            !beam_rows(*in[i], B, W, bytes[i], pitch[i]) || !beam_rows(*to[i], B, W, out_bytes, out_pitch[i]))
+            Py_RETURN_NONE;
+    }
+    const int status = enqueue([&](void* st) {
+        const void* from[BS_REORDER_STATES_MAX];
+        void* into[BS_REORDER_STATES_MAX];
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            into[i] = to[i]->mutable_data_ptr();
+            from[i] = in[i]->const_data_ptr();
+        }
+        return bs_beam_reorder((int)count, from, into, bytes, pitch, out_pitch, B, (int)W, static_cast<const int32_t*>(parents->const_data_ptr()),
+                               st);
+    });
+    if (status != BS_OK) return failed(self, status, "bs_beam_reorder");
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// () -> the number of torch's current device
+PyObject* device(PyObject*, PyObject*) {
+    HANDLE_TH_ERRORS
+    return PyLong_FromLong(c10::hip::getCurrentHIPStream().device_index());
+    END_HANDLE_TH_ERRORS
+}
+
 // () -> torch's current stream as an integer
 PyObject* stream(PyObject*, PyObject*) {
     HANDLE_TH_ERRORS
@@ -598,6 +856,8 @@ PyObject* stream(PyObject*, PyObject*) {
 PyMethodDef methods[] = {
     BS_FAST(spmv), BS_FAST(spmm), BS_FAST(prune_pack), BS_FAST(reprune), BS_FAST(lstm_step), BS_FAST(lstm_sequence),
     BS_FAST(q4_pack), BS_FAST(q4_unpack), BS_FAST(q4_gemv), BS_FAST(q4_moe), BS_FAST(logprobs), BS_FAST(logprobs_backward),
+    BS_FAST(mx4_pack), BS_FAST(mx4_unpack), BS_FAST(mx4_gemm), BS_FAST(mx4_gemm_packed), BS_FAST(beam_step), BS_FAST(beam_reorder),
+    {"device", device, METH_NOARGS, nullptr},
     {"stream", stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

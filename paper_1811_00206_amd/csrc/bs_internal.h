@@ -89,6 +89,20 @@ int launch_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t
 int launch_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets, const float* lse,
                              const float* entropy, const float* g_logprob, const float* g_entropy, void* grad, int64_t ldg,
                              hipStream_t st);
+// MX 4-bit matrices (bs_mx4_pack.hip, bs_mx4_gemm.hip) and beam search (bs_beam.hip)
+int launch_mx4_pack(const void* W, int dtype, int64_t M, int64_t K, int64_t ld, uint8_t* codes, uint8_t* scales, hipStream_t st);
+int launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, void* W, int dtype, hipStream_t st);
+// x: a dense one of type dtype, or nullptr where it is packed already
+size_t mx4_gemm_workspace_bytes(bool packed, int dtype, int64_t M, int64_t K, int64_t N);
+int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int64_t ldx, const uint8_t* x_codes,
+                    const uint8_t* x_scales, int dtype, int64_t N, const float* bias, void* y, int64_t ldy, void* workspace,
+                    size_t workspace_bytes, hipStream_t st);
+size_t beam_step_workspace_bytes(int dtype, int64_t B, int W, int64_t V, int n);
+int launch_beam_step(const void* logits, int dtype, int64_t B, int W, int64_t V, int64_t ld, const float* scores, const uint8_t* finished,
+                     int64_t end, int n, float* out_scores, int32_t* out_tokens, int32_t* out_parents, uint8_t* out_finished,
+                     void* workspace, size_t workspace_bytes, hipStream_t st);
+int launch_beam_reorder(int count, const void* const* states, void* const* outs, const int64_t* row_bytes, const int64_t* pitch,
+                        const int64_t* out_pitch, int64_t B, int W, const int32_t* parents, hipStream_t st);
 inline int hip_status(hipError_t e) { return e == hipSuccess ? BS_OK : BS_ERR_HIP; }
 
 // ---- kernels that may use more than 48 KB of LDS --------------------------------

@@ -1,5 +1,5 @@
 // C-ABI entry points of the calls on 4-bit matrices and logits: argument validation on the host, then the launchers.
-#include "bs_q4.h"
+#include "bs_mx4.h"
 
 namespace {
 
@@ -24,21 +24,29 @@ int check_logits(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld
     return aligned(logits, bs::dtype_bytes(dtype)) && aligned(targets, 8) ? BS_OK : BS_ERR_ALIGN;
 }
 
+int check_mx4(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K) {
+    if (!codes || !scales) return BS_ERR_NULL;
+    if (!matrix_ok(M, K)) return BS_ERR_SHAPE;
+    if (M > kMost || K > kMost) return BS_ERR_UNSUPPORTED;
+    return aligned(codes, 16) && aligned(scales, 4) ? BS_OK : BS_ERR_ALIGN;
+}
+
 bool aligned4(const void* a, const void* b, const void* c, const void* d) {
     return aligned(a, 4) && aligned(b, 4) && aligned(c, 4) && aligned(d, 4);
 }
 
-// Whether a row at a + i * pa and one at b + j * pb, of n bytes each, share any: rows of one tensor do not, and n <= pa, pb.
-bool rows_meet(uintptr_t a, int64_t pa, uintptr_t b, int64_t pb, int64_t rows, int64_t n) {
+// Whether one of `ra` rows of `na` bytes, pa apart from a on, and one of `rb` rows of nb bytes, pb apart from b on, share any: rows of one
+// tensor do not, and na <= pa, nb <= pb.
+bool rows_meet(uintptr_t a, int64_t pa, uintptr_t b, int64_t pb, int64_t ra, int64_t na, int64_t rb, int64_t nb) {
     const int64_t d = (int64_t)(b - a);
-    if (d >= (rows - 1) * pa + n || -d >= (rows - 1) * pb + n) return false;
+    if (d >= (ra - 1) * pa + na || -d >= (rb - 1) * pb + nb) return false;
     // rows of a to look at: where both are equally far apart the same distances come again, so that one with all b beside it will do
     const auto meets = [&](int64_t i) {
         const int64_t to = i * pa - d, j = to >= 0 ? to / pb : -1;      // the last row of b that starts at or before it
-        return (j >= 0 && j < rows && to - j * pb < n) || (j + 1 < rows && (j + 1) * pb - to < n);
+        return (j >= 0 && j < rb && to - j * pb < nb) || (j + 1 < rb && (j + 1) * pb - to < na);
     };
-    if (pa == pb) return meets(d >= 0 ? rows - 1 : 0);
-    for (int64_t i = 0; i < rows; ++i)
+    if (pa == pb && ra == rb) return meets(d >= 0 ? ra - 1 : 0);
+    for (int64_t i = 0; i < ra; ++i)
         if (meets(i)) return true;
     return false;
 }
@@ -142,11 +150,123 @@ int bs_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, in
     const int64_t size = bs::dtype_bytes(dtype);
     if (!aligned(grad, size)) return BS_ERR_ALIGN;
     if ((grad != logits || ldg != ld) &&
-        rows_meet(reinterpret_cast<uintptr_t>(logits), ld * size, reinterpret_cast<uintptr_t>(grad), ldg * size, T, V * size))
+        rows_meet(reinterpret_cast<uintptr_t>(logits), ld * size, reinterpret_cast<uintptr_t>(grad), ldg * size, T, V * size, T, V * size))
         return BS_ERR_UNSUPPORTED;
     if (!aligned4(lse, entropy, g_logprob, g_entropy)) return BS_ERR_ALIGN;
     return bs::launch_logprobs_backward(logits, dtype, T, V, ld, targets, lse, entropy, g_logprob, g_entropy, grad, ldg,
                                         static_cast<hipStream_t>(stream));
+}
+
+size_t bs_mx4_codes_bytes(int64_t M, int64_t K) {
+    return matrix_ok(M, K) && M <= kMost && K <= kMost ? (size_t)M * bs::mx4_row_bytes(K) : 0;
+}
+
+size_t bs_mx4_scales_bytes(int64_t M, int64_t K) {
+    return matrix_ok(M, K) && M <= kMost && K <= kMost ? (size_t)M * bs::mx4_scale_pitch(K) : 0;
+}
+
+int bs_mx4_pack(const void* W, int dtype, int64_t M, int64_t K, int64_t ld, uint8_t* codes, uint8_t* scales, void* stream) {
+    if (!W) return BS_ERR_NULL;
+    const int st = check_mx4(codes, scales, M, K);
+    if (st) return st;
+    if (ld < K) return BS_ERR_SHAPE;
+    if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
+    if (!aligned(W, bs::dtype_bytes(dtype))) return BS_ERR_ALIGN;
+    return bs::launch_mx4_pack(W, dtype, M, K, ld, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, void* W, int dtype, void* stream) {
+    if (!W) return BS_ERR_NULL;
+    const int st = check_mx4(codes, scales, M, K);
+    if (st) return st;
+    if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
+    if (!aligned(W, bs::dtype_bytes(dtype))) return BS_ERR_ALIGN;
+    return bs::launch_mx4_unpack(codes, scales, M, K, W, dtype, static_cast<hipStream_t>(stream));
+}
+
+size_t bs_mx4_gemm_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N) {
+    if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost) return 0;
+    return bs::mx4_gemm_workspace_bytes(false, dtype, M, K, N);
+}
+
+size_t bs_mx4_gemm_packed_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N) {
+    if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost) return 0;
+    return bs::mx4_gemm_workspace_bytes(true, dtype, M, K, N);
+}
+
+int bs_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int dtype, int64_t N, int64_t ldx,
+                const float* bias, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!x || !y) return BS_ERR_NULL;
+    const int st = check_mx4(codes, scales, M, K);
+    if (st) return st;
+    if (N < 1 || ldx < K || ldy < M) return BS_ERR_SHAPE;
+    if (!type_ok(dtype) || N > kMost) return BS_ERR_UNSUPPORTED;
+    const size_t size = bs::dtype_bytes(dtype);
+    if (!aligned(x, size) || !aligned(y, size) || !aligned(bias, 4)) return BS_ERR_ALIGN;
+    return bs::launch_mx4_gemm(codes, scales, M, K, x, ldx, nullptr, nullptr, dtype, N, bias, y, ldy, workspace, workspace_bytes,
+                               static_cast<hipStream_t>(stream));
+}
+
+int bs_mx4_gemm_packed(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const uint8_t* x_codes,
+                       const uint8_t* x_scales, int64_t N, const float* bias, void* y, int dtype, int64_t ldy, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+    if (!y) return BS_ERR_NULL;
+    int st = check_mx4(codes, scales, M, K);
+    if (st) return st;
+    st = check_mx4(x_codes, x_scales, N, K);
+    if (st) return st;
+    if (ldy < M) return BS_ERR_SHAPE;
+    if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
+    if (!aligned(y, bs::dtype_bytes(dtype)) || !aligned(bias, 4)) return BS_ERR_ALIGN;
+    return bs::launch_mx4_gemm(codes, scales, M, K, nullptr, 0, x_codes, x_scales, dtype, N, bias, y, ldy, workspace, workspace_bytes,
+                               static_cast<hipStream_t>(stream));
+}
+
+size_t bs_beam_step_workspace_bytes(int dtype, int64_t B, int W, int64_t V, int n) {
+    if (B < 1 || B > kMost || W < 1 || W > BS_BEAM_WIDTH_MAX || n < 1 || n > BS_BEAM_WIDTH_MAX || V < 1 ||
+        V >= ((int64_t)1 << 31) - 64 || !type_ok(dtype))
+        return 0;
+    return bs::beam_step_workspace_bytes(dtype, B, W, V, n);
+}
+
+int bs_beam_step(const void* logits, int dtype, int64_t B, int W, int64_t V, int64_t ld, const float* scores, const uint8_t* finished,
+                 int64_t end, int n, float* out_scores, int32_t* out_tokens, int32_t* out_parents, uint8_t* out_finished,
+                 void* workspace, size_t workspace_bytes, void* stream) {
+    if (!logits || !scores || !out_scores || !out_tokens || !out_parents || !out_finished) return BS_ERR_NULL;
+    if (B < 1 || W < 1 || V < 1 || n < 1 || ld < V || end >= V) return BS_ERR_SHAPE;
+    if (!type_ok(dtype) || B > kMost || W > BS_BEAM_WIDTH_MAX || n > BS_BEAM_WIDTH_MAX || V >= ((int64_t)1 << 31) - 64)
+        return BS_ERR_UNSUPPORTED;
+    if (!aligned(logits, bs::dtype_bytes(dtype)) || !aligned4(scores, out_scores, out_tokens, out_parents)) return BS_ERR_ALIGN;
+    return bs::launch_beam_step(logits, dtype, B, W, V, ld, scores, finished, end < 0 ? -1 : end, n, out_scores, out_tokens, out_parents,
+                                out_finished, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int bs_beam_reorder(int count, const void* const* states, void* const* outs, const int64_t* row_bytes, const int64_t* pitch,
+                    const int64_t* out_pitch, int64_t B, int W, const int32_t* parents, void* stream) {
+    if (!states || !outs || !row_bytes || !pitch || !out_pitch || !parents) return BS_ERR_NULL;
+    if (count < 1 || B < 1 || W < 1) return BS_ERR_SHAPE;
+    if (count > BS_REORDER_STATES_MAX || W > BS_BEAM_WIDTH_MAX || B > kMost) return BS_ERR_UNSUPPORTED;
+    constexpr int64_t kMostBytes = (int64_t)1 << 30;      // of a beam, all its states
+    int64_t bytes = 0;
+    for (int i = 0; i < count; ++i) {
+        if (!states[i] || !outs[i]) return BS_ERR_NULL;
+        if (row_bytes[i] < 1 || pitch[i] < row_bytes[i] || out_pitch[i] < row_bytes[i]) return BS_ERR_SHAPE;
+        if (row_bytes[i] > kMostBytes - bytes || pitch[i] >= (int64_t)1 << 32 || out_pitch[i] >= (int64_t)1 << 32) return BS_ERR_UNSUPPORTED;
+        bytes += row_bytes[i];
+    }
+    if (!aligned(parents, 4)) return BS_ERR_ALIGN;
+    const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+    for (int i = 0; i < count; ++i) {
+        if (rows_meet(at(parents), B * W * 4, at(outs[i]), out_pitch[i], 1, B * W * 4, B * W, row_bytes[i])) return BS_ERR_UNSUPPORTED;
+        for (int j = 0; j < count; ++j) {
+            const bool itself = i == j && states[j] == outs[i] && pitch[j] == out_pitch[i];
+            if (!itself && rows_meet(at(states[j]), pitch[j], at(outs[i]), out_pitch[i], B * W, row_bytes[j], B * W, row_bytes[i]))
+                return BS_ERR_UNSUPPORTED;
+            if (j < i && rows_meet(at(outs[j]), out_pitch[j], at(outs[i]), out_pitch[i], B * W, row_bytes[j], B * W, row_bytes[i]))
+                return BS_ERR_UNSUPPORTED;
+        }
+    }
+    return bs::launch_beam_reorder(count, states, outs, row_bytes, pitch, out_pitch, B, W, parents, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"
