@@ -1,7 +1,9 @@
 // Rows of activations times an MX 4-bit matrix (bs.h: bs_mx4_gemm, bs_mx4_gemm_packed).
 //
 // A workgroup has 16 rows of W and 16 * NT rows of x, its wavefronts take turns with the steps of K, and their sums meet in LDS.
-#include "bs_mx4.h"
+#include <type_traits>
+
+#include "bs_mx4_tiles.h"
 
 namespace bs {
 namespace {
@@ -59,8 +61,31 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(Args g) {
     }
 }
 
+// ---- tiles
+
+template <typename XT, int TN, int TM, int WN, int WM>
+int launch_tiles(Mx4Tiles g, hipStream_t st) {
+    constexpr auto kernel = mx4_tiles_kernel<XT, TN, TM, WN, WM, false>;
+    LdsKernel& reg = LdsKernelOf<kernel>::reg;
+    const int rc = ensure_lds_limit(reg, st);
+    if (rc != BS_OK) return rc;
+    g.m_tiles = (int)((g.M + TM - 1) / TM);
+    g.n_tiles = (int)((g.N + TN - 1) / TN);
+    g.split = 1;
+    g.stages = (g.chunks + 1) / 2;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(g.m_tiles * g.n_tiles)), dim3(256), (kMx4LdsBytes<TN, TM>), st, g);
+    return hip_status(hipGetLastError());
+}
+
 template <typename XT>
 int launch(Args g, hipStream_t st) {
+    if (g.N > 16) {
+        Mx4Tiles t{};
+        t.codes = g.codes; t.scales = g.scales; t.x_codes = g.x_codes; t.x_scales = g.x_scales;
+        t.M = g.M; t.N = g.N; t.chunks = g.chunks; t.bias = g.bias; t.y = g.y; t.ldy = g.ldy;
+        if (g.N > 1024) return launch_tiles<XT, 256, 256, 2, 2>(t, st);
+        return launch_tiles<XT, 128, 128, 2, 2>(t, st);
+    }
     constexpr int NT = 4;
     const int64_t most = (int64_t)65535 * 16 * NT;      // tokens of a launch
     const int64_t N = g.N;
