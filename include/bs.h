@@ -453,11 +453,10 @@ int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_
  * x     DEVICE in   N rows of K of type dtype, ldx >= K apart       y  DEVICE out  N rows of M, same type, ldy >= M apart
  * bias  DEVICE in   M fp32, may be NULL
  * bs_mx4_gemm_packed takes x packed already (an activation that several matrices multiply); dtype is y's type there.
- * Products are exact, sums fp32.  The order of the additions depends on M, K, N and dtype alone, and is the same in both calls but for
- * N <= BS_MX4_FUSED_MAX.  A NaN or an infinity in x makes its row of y NaN, a block of W that is NaN its column.  N <= 2^24.
+ * Products are exact, sums fp32.  The order of the additions depends on M, K and N alone, and is the same in both calls.
+ * A NaN or an infinity in x makes its row of y NaN, a block of W that is NaN its column.  N <= 2^24, M N <= 2^36.
  * workspace as for bs_spmm.
  */
-#define BS_MX4_FUSED_MAX 2
 size_t bs_mx4_gemm_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N);
 int bs_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int dtype, int64_t N, int64_t ldx,
                 const float* bias, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);

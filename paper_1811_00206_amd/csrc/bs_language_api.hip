@@ -5,6 +5,8 @@ namespace {
 
 constexpr int64_t kMost = (int64_t)1 << 24;      // rows, columns
 
+constexpr int64_t kMostOutputs = (int64_t)1 << 36;      // of an MX product
+
 bool type_ok(int dtype) { return dtype == BS_F32 || dtype == BS_F16 || dtype == BS_BF16; }
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 bool matrix_ok(int64_t M, int64_t K) { return M >= 1 && K >= 1; }
@@ -185,12 +187,12 @@ int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_
 }
 
 size_t bs_mx4_gemm_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N) {
-    if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost) return 0;
+    if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost || M * N > kMostOutputs) return 0;
     return bs::mx4_gemm_workspace_bytes(false, dtype, M, K, N);
 }
 
 size_t bs_mx4_gemm_packed_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N) {
-    if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost) return 0;
+    if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost || M * N > kMostOutputs) return 0;
     return bs::mx4_gemm_workspace_bytes(true, dtype, M, K, N);
 }
 
@@ -200,7 +202,7 @@ int bs_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t 
     const int st = check_mx4(codes, scales, M, K);
     if (st) return st;
     if (N < 1 || ldx < K || ldy < M) return BS_ERR_SHAPE;
-    if (!type_ok(dtype) || N > kMost) return BS_ERR_UNSUPPORTED;
+    if (!type_ok(dtype) || N > kMost || M * N > kMostOutputs) return BS_ERR_UNSUPPORTED;
     const size_t size = bs::dtype_bytes(dtype);
     if (!aligned(x, size) || !aligned(y, size) || !aligned(bias, 4)) return BS_ERR_ALIGN;
     return bs::launch_mx4_gemm(codes, scales, M, K, x, ldx, nullptr, nullptr, dtype, N, bias, y, ldy, workspace, workspace_bytes,
@@ -216,7 +218,7 @@ int bs_mx4_gemm_packed(const uint8_t* codes, const uint8_t* scales, int64_t M, i
     st = check_mx4(x_codes, x_scales, N, K);
     if (st) return st;
     if (ldy < M) return BS_ERR_SHAPE;
-    if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
+    if (!type_ok(dtype) || M * N > kMostOutputs) return BS_ERR_UNSUPPORTED;
     if (!aligned(y, bs::dtype_bytes(dtype)) || !aligned(bias, 4)) return BS_ERR_ALIGN;
     return bs::launch_mx4_gemm(codes, scales, M, K, nullptr, 0, x_codes, x_scales, dtype, N, bias, y, ldy, workspace, workspace_bytes,
                                static_cast<hipStream_t>(stream));

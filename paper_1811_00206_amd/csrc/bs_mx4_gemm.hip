@@ -1,6 +1,8 @@
 // Rows of activations times an MX 4-bit matrix (bs.h: bs_mx4_gemm, bs_mx4_gemm_packed).
 //
-// A workgroup has 16 rows of W and 16 * NT rows of x, its wavefronts take turns with the steps of K, and their sums meet in LDS.
+// Few rows: a wavefront has 16 rows of W, which go from memory to the matrix unit, and reads x beside them.  Many: tiles that pass
+// through LDS (bs_mx4_tiles.h), with K split between workgroups where there are few of them; a second kernel then adds their sums up,
+// in order.  Dense x is rounded by a kernel of its own first, or for one or two rows by every workgroup for itself.
 #include <type_traits>
 
 #include "bs_mx4_tiles.h"
@@ -10,49 +12,144 @@ namespace {
 
 struct Args {
     const uint8_t *codes, *scales, *x_codes, *x_scales;
-    int64_t M, N;
-    int chunks;
+    const void* x;              // dense
+    int64_t ldx;
+    int64_t M, K, N;
+    int chunks, ways, tiles;    // chunks of 128 columns; wavefronts that share K, and groups of them
     const float* bias;
     void* y;
     int64_t ldy;
 };
 
-template <typename XT, int NT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(Args g) {
-    __shared__ f32x4 sums[WAVES][NT][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, kb = lane >> 4;
-    const int64_t m0 = (int64_t)blockIdx.x * 16, n0 = (int64_t)blockIdx.y * 16 * NT;
-    const int64_t wrow = min(m0 + r, g.M - 1);
-    const uint8_t* const w = g.codes + wrow * 64 * g.chunks + 16 * kb;
-    const uint32_t* const ws = reinterpret_cast<const uint32_t*>(g.scales) + wrow * g.chunks;
+constexpr int kStep = 4;      // chunks of 128 columns that a wavefront takes at a time: 256 bytes of a row
+constexpr int kFusedRows = 2, kFusedBytes = 48 * 1024;
+
+typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(4)));
+
+// What a wavefront brings for a step: R pieces of 16 rows, a lane 16 bytes of its row for each chunk and the chunks' scale bytes.
+template <int R>
+struct Piece {
+    uint4 q[R][kStep], s[R];
+};
+
+// 16 * R rows of W by 16 * NT of x for each wavefront.  Of a workgroup's wavefronts `ways` take turns with the steps of K and add their
+// sums up in LDS, in order; `tiles` groups of them have different rows of W and the same of x.  x comes from memory in MX form, or
+// (FUSED, for few rows) dense: then the workgroup first rounds it into LDS, while its first pieces of W are on their way.
+template <typename XT, int R, int NT, bool FUSED>
+__global__ __launch_bounds__(R * NT == 1 ? 1024 : 512) void mx4_rows_kernel(Args g) {
+    static_assert(!FUSED || NT == 1);
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, kb = lane >> 4;
+    const int way = wave % g.ways, tile = wave / g.ways;
+    const int64_t m0 = ((int64_t)blockIdx.x * g.tiles + tile) * 16 * R, n0 = (int64_t)blockIdx.y * 16 * NT;
+    const int chunks = g.chunks, whole = chunks / kStep;      // steps of four chunks
+    const uint8_t* w[R];
+    const uint32_t* ws[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int64_t row = min(m0 + 16 * i + r, g.M - 1);
+        w[i] = g.codes + row * 64 * chunks + 16 * kb;
+        ws[i] = reinterpret_cast<const uint32_t*>(g.scales) + row * chunks;
+    }
+    const auto load = [&](Piece<R>& p, int step) {
+        const uint32_t at = (uint32_t)step * (64 * kStep);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) p.q[i][u] = *reinterpret_cast<const uint4*>(w[i] + at + 64 * u);
+            const Words v = *reinterpret_cast<const Words*>(reinterpret_cast<const uint8_t*>(ws[i]) + (at >> 4));
+            p.s[i] = uint4{v[0], v[1], v[2], v[3]};
+        }
+    };
+    // Two pieces are on their way while one is multiplied.  (Where there is no whole step nothing is loaded here.)
+    Piece<R> a, b;
+    if (way < whole) load(a, way);
+    if (way + g.ways < whole) load(b, way + g.ways);
     const uint8_t* x[NT];
     const uint32_t* xs[NT];
-    f32x4 acc[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t row = min(n0 + 16 * t + r, g.N - 1);
-        x[t] = g.x_codes + row * 64 * g.chunks + 16 * kb;
-        xs[t] = reinterpret_cast<const uint32_t*>(g.x_scales) + row * g.chunks;
-        acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    for (int c = wave; c < g.chunks; c += WAVES) {
-        const uint4 a = *reinterpret_cast<const uint4*>(w + (int64_t)c * 64);
-        const uint32_t sa = ws[c] >> (8 * kb);
+    if constexpr (FUSED) {
+        const int pitch = (chunks + 3) & ~3;
+        uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + g.N * 64 * chunks);
+        const int pieces = 16 * chunks;      // of a row, 8 elements each
+        for (int n = 0; n < (int)g.N; ++n)
+            for (int p0 = 0; p0 < pieces; p0 += blockDim.x) {
+                const int p = p0 + threadIdx.x;
+                const int64_t k = (int64_t)p * 8;
+                float v[8] = {};
+                if (k < g.K) load8<XT>(static_cast<const typename XT::type*>(g.x) + n * g.ldx, k, g.K, v);
+                const uint32_t e = mx4_scale(max_of_4(mx4_most(v)));
+                const uint32_t word = mx4_codes(v, mx4_factor(e));
+                uint32_t bytes = e << (p / 4 % 4 * 8);
+                bytes |= (uint32_t)dpp_move_i<0x141>((int)bytes);
+                bytes |= (uint32_t)dpp_move_i<0x140>((int)bytes);
+                if (p >= pieces) continue;
+                reinterpret_cast<uint32_t*>(lds)[n * pieces + p] = word;
+                if (p % 16 == 0) scales[n * pitch + p / 16] = bytes;
+            }
+        const int row = min(r, (int)g.N - 1);
+        x[0] = lds + row * 64 * chunks + 16 * kb;
+        xs[0] = scales + row * pitch;
+        __syncthreads();
+    } else {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const uint4 b = *reinterpret_cast<const uint4*>(x[t] + (int64_t)c * 64);
-            const uint32_t sb = xs[t][c] >> (8 * kb);
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(a), mx4_operand(b), acc[t], 4, 4, 0, (int)sa, 0, (int)sb);
+            const int64_t row = min(n0 + 16 * t + r, g.N - 1);
+            x[t] = g.x_codes + row * 64 * chunks + 16 * kb;
+            xs[t] = reinterpret_cast<const uint32_t*>(g.x_scales) + row * chunks;
         }
     }
+    f32x4 acc[R][NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) sums[wave][t][lane] = acc[t];
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto multiply = [&](const Piece<R>& p, int u, int t, uint4 xv, uint32_t xsv) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(p.q[i][u]), mx4_operand(xv), acc[i][t], 4, 4, 0,
+                                                                         (int)(word_of(p.s[i], u) >> (8 * kb)), 0, (int)(xsv >> (8 * kb)));
+    };
+    const auto eat = [&](const Piece<R>& p, int step) {
+        const uint32_t at = (uint32_t)step * (64 * kStep);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            uint4 xv[kStep];
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) xv[u] = *reinterpret_cast<const uint4*>(x[t] + at + 64 * u);
+            const Words sv = *reinterpret_cast<const Words*>(reinterpret_cast<const uint8_t*>(xs[t]) + (at >> 4));
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) multiply(p, u, t, xv[u], sv[u]);
+        }
+    };
+    for (int step = way; step < whole; step += 2 * g.ways) {
+        eat(a, step);
+        if (step + 2 * g.ways < whole) load(a, step + 2 * g.ways);
+        if (step + g.ways >= whole) break;
+        eat(b, step + g.ways);
+        if (step + 3 * g.ways < whole) load(b, step + 3 * g.ways);
+    }
+    if (whole % g.ways == way)      // the rest, one to three chunks
+        for (int c = whole * kStep; c < chunks; ++c) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                a.q[i][0] = *reinterpret_cast<const uint4*>(w[i] + (int64_t)c * 64);
+                a.s[i].x = ws[i][c];
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) multiply(a, 0, t, *reinterpret_cast<const uint4*>(x[t] + (int64_t)c * 64), xs[t][c]);
+        }
+    if constexpr (FUSED) __syncthreads();
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds);      // [tile][way][R * NT][lane]
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sums[(wave * R * NT + i * NT + t) * 64 + lane] = acc[i][t];
     __syncthreads();
-    for (int i = threadIdx.x; i < NT * 64; i += 64 * WAVES) {
-        const int t = i >> 6, l = i & 63;
-        f32x4 s = sums[0][t][l];
-        for (int v = 1; v < WAVES; ++v) s += sums[v][t][l];
-        const int64_t n = n0 + 16 * t + (l & 15), m = m0 + 4 * (l >> 4);
+    for (int e = threadIdx.x; e < g.tiles * R * NT * 64; e += blockDim.x) {
+        const int l = e & 63, in = e >> 6, part = in % (R * NT), group = in / (R * NT);
+        f32x4 s = sums[(group * g.ways * R * NT + part) * 64 + l];
+        for (int v = 1; v < g.ways; ++v) s += sums[((group * g.ways + v) * R * NT + part) * 64 + l];
+        const int64_t n = n0 + 16 * (part % NT) + (l & 15), m = (((int64_t)blockIdx.x * g.tiles + group) * R + part / NT) * 16 + 4 * (l >> 4);
         if (n >= g.N) continue;
         typename XT::type* const y = static_cast<typename XT::type*>(g.y) + n * g.ldy;
 #pragma unroll
@@ -61,73 +158,185 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_rows_kernel(Args g) {
     }
 }
 
-// ---- tiles
-
-template <typename XT, int TN, int TM, int WN, int WM>
-int launch_tiles(Mx4Tiles g, hipStream_t st) {
-    constexpr auto kernel = mx4_tiles_kernel<XT, TN, TM, WN, WM, false>;
-    LdsKernel& reg = LdsKernelOf<kernel>::reg;
-    const int rc = ensure_lds_limit(reg, st);
-    if (rc != BS_OK) return rc;
-    g.m_tiles = (int)((g.M + TM - 1) / TM);
-    g.n_tiles = (int)((g.N + TN - 1) / TN);
-    g.split = 1;
-    g.stages = (g.chunks + 1) / 2;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(g.m_tiles * g.n_tiles)), dim3(256), (kMx4LdsBytes<TN, TM>), st, g);
+template <typename XT, int R, int NT, bool FUSED>
+int launch_rows(Args g, hipStream_t st) {
+    const size_t sums = (size_t)g.ways * g.tiles * R * NT * 1024, x = FUSED ? (size_t)g.N * (64 * g.chunks + 4 * ((g.chunks + 3) & ~3)) : 0;
+    const int64_t rows = 16 * R * g.tiles;
+    const dim3 grid((unsigned)((g.M + rows - 1) / rows), (unsigned)((g.N + 16 * NT - 1) / (16 * NT)));
+    hipLaunchKernelGGL((mx4_rows_kernel<XT, R, NT, FUSED>), grid, dim3(64 * g.ways * g.tiles), sums > x ? sums : x, st, g);
     return hip_status(hipGetLastError());
 }
 
+// ---- tiles
+
+// sums of the shares of K, in order
 template <typename XT>
-int launch(Args g, hipStream_t st) {
-    if (g.N > 16) {
-        Mx4Tiles t{};
-        t.codes = g.codes; t.scales = g.scales; t.x_codes = g.x_codes; t.x_scales = g.x_scales;
-        t.M = g.M; t.N = g.N; t.chunks = g.chunks; t.bias = g.bias; t.y = g.y; t.ldy = g.ldy;
-        if (g.N > 1024) return launch_tiles<XT, 256, 256, 2, 2>(t, st);
-        return launch_tiles<XT, 128, 128, 2, 2>(t, st);
+__global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Tiles g, int64_t n0) {
+    typedef float Floats __attribute__((ext_vector_type(4), aligned(4)));
+    const int64_t m = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = n0 + blockIdx.y, all = g.N * g.M;
+    if (m >= g.M) return;
+    const float* const from = g.sums + n * g.M + m;
+    typename XT::type* const to = static_cast<typename XT::type*>(g.y) + n * g.ldy + m;
+    if (m + 4 <= g.M) {
+        Floats s = *reinterpret_cast<const Floats*>(from);
+        for (int i = 1; i < g.split; ++i) s += *reinterpret_cast<const Floats*>(from + i * all);
+        if (g.bias) s += *reinterpret_cast<const Floats*>(g.bias + m);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e] = XT::store(s[e]);
+    } else {
+        for (int e = 0; m + e < g.M; ++e) {
+            float s = from[e];
+            for (int i = 1; i < g.split; ++i) s += from[e + i * all];
+            to[e] = XT::store(g.bias ? s + g.bias[m + e] : s);
+        }
     }
-    constexpr int NT = 4;
-    const int64_t most = (int64_t)65535 * 16 * NT;      // tokens of a launch
-    const int64_t N = g.N;
-    for (int64_t n = 0; n < N; n += most) {
-        Args p = g;
-        p.N = N - n < most ? N - n : most;
-        p.x_codes += n * 64 * g.chunks;
-        p.x_scales += n * 4 * g.chunks;
-        p.y = static_cast<typename XT::type*>(g.y) + n * g.ldy;
-        const unsigned m = (unsigned)((g.M + 15) / 16);
-        if (p.N <= 16) hipLaunchKernelGGL((mx4_rows_kernel<XT, 1, 4>), dim3(m, 1), dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((mx4_rows_kernel<XT, NT, 4>), dim3(m, (unsigned)((p.N + 16 * NT - 1) / (16 * NT))), dim3(256), 0, st, p);
-        const int rc = hip_status(hipGetLastError());
-        if (rc != BS_OK) return rc;
+}
+
+constexpr int kTileGroup = 400;      // these kernels' LDS limits are raised together: which one a product takes is a matter of its sizes
+
+template <typename XT, int TN, int TM, int WN, int WM, bool SPLIT>
+int launch_tiles(const Mx4Tiles& g, hipStream_t st) {
+    constexpr auto kernel = mx4_tiles_kernel<XT, TN, TM, WN, WM, SPLIT>;
+    const int rc = ensure_lds_limit(LdsKernelOf<kernel, kTileGroup>::reg, st, nullptr, kTileGroup);
+    if (rc != BS_OK) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(g.m_tiles * g.n_tiles * g.split)), dim3(256), (kMx4LdsBytes<TN, TM>), st, g);
+    return hip_status(hipGetLastError());
+}
+
+template <typename XT, int TN, int TM, int WN, int WM>
+int launch_tiles(Mx4Tiles g, hipStream_t st) {
+    g.m_tiles = (int)((g.M + TM - 1) / TM);
+    g.n_tiles = (int)((g.N + TN - 1) / TN);
+    if (g.split == 1) return launch_tiles<XT, TN, TM, WN, WM, false>(g, st);
+    const int rc = launch_tiles<F32, TN, TM, WN, WM, true>(g, st);
+    if (rc != BS_OK) return rc;
+    const int64_t most = 65535;      // rows of a launch
+    for (int64_t n = 0; n < g.N; n += most) {
+        hipLaunchKernelGGL(mx4_join_kernel<XT>, dim3((unsigned)((g.M + 1023) / 1024), (unsigned)(g.N - n < most ? g.N - n : most)), dim3(256), 0, st, g, n);
+        const int code = hip_status(hipGetLastError());
+        if (code != BS_OK) return code;
     }
     return BS_OK;
 }
 
+template <typename XT>
+int launch_tiles(const Mx4Tiles& t, int tn, hipStream_t st) {
+    switch (tn) {
+        case 32: return launch_tiles<XT, 32, 128, 1, 4>(t, st);
+        case 64: return launch_tiles<XT, 64, 128, 1, 4>(t, st);
+        case 96: return launch_tiles<XT, 96, 128, 1, 4>(t, st);
+        case 128: return launch_tiles<XT, 128, 128, 2, 2>(t, st);
+        default: return launch_tiles<XT, 256, 256, 2, 2>(t, st);
+    }
+}
+
+// ---- which
+
+struct Plan {
+    int tile;                      // rows of x in a tile; 0: no tiles
+    int split, stages;             // workgroups that share K, and the stages of 256 columns of each
+    int r, nt, ways, groups;       // without tiles
+};
+
+// Microseconds of a product in tiles.  A stage takes a compute unit `alone` with one workgroup, `full` with as many as fit; measured with
+// 16384 x 8192, 4096 x 4096, 4096 x 25088 and 6600 x 13448 for 16 to 4096 rows, and right within a quarter for most of them.
+struct Tile {
+    int n, m, fit;
+    double alone, full;
+};
+constexpr Tile kTiles[] = {{32, 128, 3, 0.65, 1.2}, {64, 128, 2, 0.8, 1.03}, {96, 128, 2, 0.85, 1.1}, {128, 128, 2, 0.9, 1.15}, {256, 256, 1, 1.8, 1.8}};
+
+double cost_of(const Tile& t, int64_t M, int64_t N, int stages, int split) {
+    const double groups = (double)((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) * split, sums = (double)M * N * 4;
+    const double rounds = groups <= 256 ? 1 : (double)(int64_t)((groups + 256 * t.fit - 1) / (256 * t.fit));
+    const double work = rounds * stages * (groups <= 256 ? t.alone : t.full), bytes = (double)M * stages * split * 136 / 4.6e6;
+    return 3 + (work > bytes ? work : bytes) + (split > 1 ? 2 + (2 * split + 0.5) * sums / 8e6 : 0);
+}
+
+Plan plan_for(int64_t M, int64_t K, int64_t N) {
+    const int chunks = (int)mx4_chunks(K), steps = (chunks + kStep - 1) / kStep;
+    const int64_t tiles = (M + 15) / 16;
+    Plan p{};
+    // Rows of W straight from memory: for up to 16 rows of x, and for up to 64 where W has few.  (16384 x 8192 for 4 / 16 / 32 / 64 rows
+    // 14.5 / 17.0 / 21.9 / 33.7 us, 16.3 / 16.9 / 17.3 / 19.3 in tiles; 4096 x 4096 for 32 6.4 and 9.3, 2000 x 8000 for 64 10.1 and 11.3,
+    // 10000 x 1500 for 8 / 32 5.0 / 7.8 and 6.9 / 6.8.)
+    if (N <= 16 || (N <= 64 && tiles <= 320)) {
+        p.nt = N <= 16 ? 1 : N <= 32 ? 2 : 4;
+        // Wavefronts that share K: as many as give the chip 2048 (eight for a compute unit), or what K has steps for; where two are
+        // enough, four groups of them share x in LDS.  16384 x 8192 for one row: 17.1 us with 2 x 4, 18.9 with 1 x 4, 17.8 with
+        // 4 x 2, 18.3 with 8 x 1.  With more rows x is what counts: twice as many rows of W for each of its pieces, 14.5 us instead
+        // of 16.0 for 4 rows and 17.0 instead of 20.9 for 16.
+        p.r = N > kFusedRows && N <= 16 && tiles >= 1024 && steps >= 8 ? 2 : 1;
+        p.ways = 1;
+        const int most = p.nt == 4 ? 8 : 16;
+        while (p.ways < most && tiles * p.ways < 2048 * p.r && p.ways < steps) p.ways *= 2;
+        p.groups = p.ways <= 2 ? 4 : p.r == 2 ? 2 : 1;
+        return p;
+    }
+    const int stages = (chunks + 1) / 2;
+    double least = 0;
+    for (const Tile& t : kTiles)
+        for (int split = 1; split <= 16 && split <= stages; ++split) {
+            const int each = (stages + split - 1) / split, parts = (stages + each - 1) / each;
+            if (parts != split) continue;
+            const double cost = cost_of(t, M, N, each, split);
+            if (p.tile && cost >= least) continue;
+            least = cost;
+            p.tile = t.n;
+            p.split = split;
+            p.stages = each;
+        }
+    return p;
+}
+
+size_t packed_bytes(int64_t K, int64_t N) { return (size_t)(N * (mx4_row_bytes(K) + mx4_scale_pitch(K)) + 15) / 16 * 16; }
+bool fused(int64_t K, int64_t N) { return N <= kFusedRows && N * 68 * (mx4_chunks(K) + 3) <= kFusedBytes; }
+
+template <typename XT>
+int launch(Args g, const Plan& p, float* sums, hipStream_t st) {
+    if (p.tile) {
+        Mx4Tiles t{};
+        t.codes = g.codes; t.scales = g.scales; t.x_codes = g.x_codes; t.x_scales = g.x_scales;
+        t.M = g.M; t.N = g.N; t.chunks = g.chunks; t.bias = g.bias; t.y = g.y; t.ldy = g.ldy;
+        t.split = p.split; t.stages = p.stages; t.sums = sums;
+        return launch_tiles<XT>(t, p.tile, st);
+    }
+    g.ways = p.ways;
+    g.tiles = p.groups;
+    if (g.x) return launch_rows<XT, 1, 1, true>(g, st);
+    if (p.r == 2) return launch_rows<XT, 2, 1, false>(g, st);
+    return p.nt == 1 ? launch_rows<XT, 1, 1, false>(g, st) : p.nt == 2 ? launch_rows<XT, 1, 2, false>(g, st) : launch_rows<XT, 1, 4, false>(g, st);
+}
+
 }  // namespace
 
-size_t mx4_gemm_workspace_bytes(bool packed, int, int64_t, int64_t K, int64_t N) {
-    return packed ? 0 : (size_t)(N * (mx4_row_bytes(K) + mx4_scale_pitch(K)) + 15) / 16 * 16;
+size_t mx4_gemm_workspace_bytes(bool packed, int, int64_t M, int64_t K, int64_t N) {
+    const Plan p = plan_for(M, K, N);
+    return (packed || fused(K, N) ? 0 : packed_bytes(K, N)) + (p.split > 1 ? (size_t)p.split * M * N * 4 : 0);
 }
 
 int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int64_t ldx, const uint8_t* x_codes,
                     const uint8_t* x_scales, int dtype, int64_t N, const float* bias, void* y, int64_t ldy, void* workspace,
                     size_t workspace_bytes, hipStream_t st) {
+    const Plan p = plan_for(M, K, N);
     const size_t need = mx4_gemm_workspace_bytes(!x, dtype, M, K, N);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))) return BS_ERR_WORKSPACE;
-    if (x) {
-        uint8_t* const c = static_cast<uint8_t*>(workspace);
-        uint8_t* const s = c + N * mx4_row_bytes(K);
-        const int rc = launch_mx4_pack(x, dtype, N, K, ldx, c, s, st);
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    const bool dense = x && fused(K, N);
+    if (x && !dense) {
+        uint8_t* const s = at + N * mx4_row_bytes(K);
+        const int rc = launch_mx4_pack(x, dtype, N, K, ldx, at, s, st);
         if (rc != BS_OK) return rc;
-        x_codes = c;
+        x_codes = at;
         x_scales = s;
+        at += packed_bytes(K, N);
     }
-    const Args g{codes, scales, x_codes, x_scales, M, N, (int)mx4_chunks(K), bias, y, ldy};
+    float* const sums = reinterpret_cast<float*>(at);
+    const Args g{codes, scales, x_codes, x_scales, dense ? x : nullptr, ldx, M, K, N, (int)mx4_chunks(K), 1, 1, bias, y, ldy};
     switch (dtype) {
-        case BS_F32: return launch<F32>(g, st);
-        case BS_F16: return launch<F16>(g, st);
-        default: return launch<BF16>(g, st);
+        case BS_F32: return launch<F32>(g, p, sums, st);
+        case BS_F16: return launch<F16>(g, p, sums, st);
+        default: return launch<BF16>(g, p, sums, st);
     }
 }
 
