@@ -23,6 +23,8 @@ constexpr int kCandidates = kWidth * kWidth;   // of a sequence, all its lists
 constexpr double kLog2e = 1.4426950408889634074;
 static_assert(kWidth <= kTopMax);
 
+typedef uint32_t Pair __attribute__((ext_vector_type(2)));
+
 // 2^u for -1000 < u < 1000, 1 for 0
 __device__ __forceinline__ double exp2_wide(double u) {
     constexpr double kMagic = 0x1.8p52;      // the whole part, in the low bits
@@ -35,9 +37,9 @@ __device__ __forceinline__ double exp2_wide(double u) {
     p = fma(p, f, 0x1.ebfbe07787485p-3);
     p = fma(p, f, 0x1.62e42ff0e1927p-1);
     p = fma(p, f, 1.0);
-    const uint64_t b = __builtin_bit_cast(uint64_t, p);
-    const uint32_t high = (uint32_t)(b >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, t) << 20);
-    return __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)b);
+    Pair v = __builtin_bit_cast(Pair, p);
+    v[1] += __builtin_bit_cast(Pair, t)[0] << 20;
+    return __builtin_bit_cast(double, v);
 }
 
 // the sum of exp(x - m) over some of a row; m is -inf before anything was seen
@@ -56,10 +58,24 @@ __device__ __forceinline__ double moved(double v, int by) {
     const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)b, by, 64), hi = (uint32_t)__shfl_xor((int)(b >> 32), by, 64);
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
+template <int CTRL>
+__device__ __forceinline__ double dpp_wide(double v) {
+    Pair p = __builtin_bit_cast(Pair, v);
+    p[0] = (uint32_t)dpp_move_i<CTRL>((int)p[0]);
+    p[1] = (uint32_t)dpp_move_i<CTRL>((int)p[1]);
+    return __builtin_bit_cast(double, p);
+}
+__device__ __forceinline__ double sum_of_16(double v) {
+    v += dpp_wide<0xB1>(v);
+    v += dpp_wide<0x4E>(v);
+    v += dpp_wide<0x141>(v);
+    return v + dpp_wide<0x140>(v);
+}
 __device__ __forceinline__ Sum join_wave(Sum a) {
     raise(a, max_of_wave(a.m));
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) a.s += moved(a.s, by);
+    a.s = sum_of_16(a.s);
+    a.s += moved(a.s, 16);
+    a.s += moved(a.s, 32);
     return a;
 }
 __device__ __forceinline__ Sum join(Sum a, Sum b) {
@@ -102,6 +118,7 @@ struct Args {
     const void* logits;
     int64_t B, V, ld, rows, end;
     int W, n, slices;
+    uint32_t beam_magic, list_magic;      // division by slices * n, by n
     int64_t slice_vectors;      // 16-byte pieces of a row in a slice
     int sharing, places;        // batches of a place, places of a thread
     const float* scores;
@@ -136,15 +153,35 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
     if (me == 0) l.count = l.eight_count = 0;
     Sum st{0.0, -__builtin_inff()};
     int batches = 0;
+    // Batches of whole pieces are on their way while the one before is added up.
+    const int64_t whole = min(v1, g.V / E);
+    uint4 next[U];
+    const auto load = [&](int64_t b) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) __builtin_memcpy(&next[u], row.p + (b + u * THREADS + me) * E, 16);
+    };
+    if (v0 + THREADS * U <= whole) load(v0);
     for (int64_t b = v0; b < v1; b += THREADS * U, ++batches) {
         float x[kBatch];
+        if (b + THREADS * U <= whole) {
+            uint4 now[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t v = b + u * THREADS + me;
-            if (v < v1) row.load(v, x + u * E);
-            else
+            for (int u = 0; u < U; ++u) {
+                now[u] = next[u];
+                asm volatile("" : "+v"(now[u].x), "+v"(now[u].y), "+v"(now[u].z), "+v"(now[u].w));
+            }
+            if (b + 2 * THREADS * U <= whole) load(b + THREADS * U);
 #pragma unroll
-                for (int i = 0; i < E; ++i) x[u * E + i] = -__builtin_inff();
+            for (int u = 0; u < U; ++u) R::values(now[u], x + u * E);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t v = b + u * THREADS + me;
+                if (v < v1) row.load(v, x + u * E);
+                else
+#pragma unroll
+                    for (int i = 0; i < E; ++i) x[u * E + i] = -__builtin_inff();
+            }
         }
         float part[kParts], most = -__builtin_inff();
 #pragma unroll
@@ -208,11 +245,12 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
     }
     G::sync();
     const int eights = l.eight_count;
-    const int64_t pieces = (int64_t)min(eights, kEights) * V8 * g.sharing;
-    for (int64_t j = me; j < pieces; j += THREADS) {
-        const uint32_t eight = l.eights[j / (V8 * g.sharing)], place = eight / THREADS;
-        const int64_t batch = place / kParts * (int64_t)g.sharing + j / V8 % g.sharing;
-        const int64_t v = v0 + (batch * U + place % kParts * V8 + j % V8) * THREADS + eight % THREADS;
+    const uint32_t each = V8 * (uint32_t)g.sharing, pieces = (uint32_t)min(eights, kEights) * each;      // pieces of an eight, of all
+    for (uint32_t j = me; j < pieces; j += THREADS) {
+        const uint32_t e = g.sharing == 1 ? j / V8 : j / each, rest = j - e * each;
+        const uint32_t eight = l.eights[e], place = eight / THREADS;
+        const int64_t batch = (int64_t)(place / kParts) * g.sharing + rest / V8;
+        const int64_t v = v0 + (batch * U + place % kParts * V8 + rest % V8) * THREADS + eight % THREADS;
         float x[E];
         if (v < v1) row.load(v, x);
 #pragma unroll
@@ -237,75 +275,147 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
     for (int i = me; i < g.n; i += THREADS) g.keys[(r * g.slices + slice) * g.n + i] = l.sorted[i];
 }
 
-// a sequence's n best of what its lists (one for each beam and slice) offer
+// the sum over 16 neighbouring lanes, in every one of them; m: the largest of theirs
+__device__ __forceinline__ Sum join_16(Sum a) {
+    float m = a.m;
+    m = fmaxf(m, dpp_move<0xB1>(m));
+    m = fmaxf(m, dpp_move<0x4E>(m));
+    m = fmaxf(m, dpp_move<0x141>(m));
+    m = fmaxf(m, dpp_move<0x140>(m));
+    raise(a, m);
+    a.s = sum_of_16(a.s);
+    return a;
+}
+
+// A sequence's n best of what its lists (one for each beam and slice) offer, EACH * 256 candidates at most: candidate i is the one of
+// place i % n in list i / n.
+template <int EACH>
 __global__ __launch_bounds__(kThreads) void beam_join_kernel(Args g) {
-    __shared__ double totals[kCandidates], bounds[kWidth * kSlices];
-    __shared__ uint16_t from[kCandidates];
-    __shared__ double log_s[kWidth];
+    constexpr int kMost = EACH * kThreads;
+    __shared__ __align__(16) double totals[kMost + 8];
+    __shared__ __align__(16) float logits[kMost + 8];
+    __shared__ __align__(16) uint16_t from[kMost + 8];
+    __shared__ double wave_bound[kWaves], wave_last[kWaves];
+    __shared__ double log_s[kWidth], scores[kWidth];
     __shared__ float most[kWidth];
     __shared__ int kind[kWidth], kept, full;      // kind of a beam: 0 offers nothing, 1 goes on, 2 is finished
-    const int64_t b = blockIdx.x;
-    const int lists = g.W * g.slices, all = lists * g.n;
+    const double none = -(double)__builtin_inff();
+    const int64_t b = blockIdx.x, row0 = b * g.W;
+    const int me = threadIdx.x, per_beam = g.slices * g.n, lists = g.W * g.slices, all = g.W * per_beam;
     const uint64_t* const keys = g.keys + b * all;
-    if (threadIdx.x == 0) kept = full = 0;
-    if ((int)threadIdx.x < g.W) {
-        const int64_t r = b * g.W + threadIdx.x;
-        int is = finite(g.scores[r]) ? g.finished && g.finished[r] ? 2 : 1 : 0;
-        if (is == 1) {
-            Sum st = g.sums[r * g.slices];
-            for (int i = 1; i < g.slices; ++i) st = join(st, g.sums[r * g.slices + i]);
-            log_s[threadIdx.x] = log(st.s);
-            most[threadIdx.x] = st.m;
-            if (!(st.s > 0.0)) is = 0;      // no words, or a logit that is NaN or +inf
+    // Keys are asked for before anything is waited for.  (Beams that offer nothing have written nothing: what is read of theirs is not
+    // looked at.)
+    uint64_t key[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) key[e] = keys[min(e * kThreads + me, all - 1)];
+    if (me == 0) kept = full = 0;
+#pragma unroll 1
+    for (int w = me / 16; w < g.W; w += kThreads / 16) {      // 16 lanes a beam
+        const int slice = me % 16;
+        Sum st = g.sums[(row0 + w) * g.slices + min(slice, g.slices - 1)];
+        const float score = g.scores[row0 + w];
+        const bool done = g.finished && g.finished[row0 + w];
+        int is = finite(score) ? done ? 2 : 1 : 0;
+        if (is != 1 || slice >= g.slices) st = Sum{0.0, -__builtin_inff()};
+        st = join_16(st);
+        if (slice == 0) {
+            if (is == 1 && !(st.s > 0.0)) is = 0;      // no words, or a logit that is NaN or +inf
+            if (is == 1) log_s[w] = log(st.s);
+            most[w] = st.m;
+            scores[w] = (double)score;
+            kind[w] = is;
         }
-        kind[threadIdx.x] = is;
     }
     __syncthreads();
-    // the total of candidate i, the one of place i % n in list i / n; -inf for what is none
-    const auto total_of = [&](int i) {
-        const int list = i / g.n, beam = list / g.slices, rank = i - list * g.n;
-        const double score = (double)g.scores[b * g.W + beam];
-        if (kind[beam] == 2) return rank == 0 && list % g.slices == 0 ? score : -(double)__builtin_inff();
-        if (kind[beam] == 0) return -(double)__builtin_inff();
-        const uint64_t key = keys[i];
-        const float x = value_of_key(key);
-        if (!key || x == -__builtin_inff()) return -(double)__builtin_inff();
-        return score + (((double)x - (double)most[beam]) - log_s[beam]);
-    };
-    for (int i = threadIdx.x; i < lists; i += kThreads)
-        if (total_of(i * g.n + g.n - 1) > -(double)__builtin_inff()) atomicAdd(&full, 1);
+    double mine[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int i = e * kThreads + me;
+        mine[e] = none;      // the total of what is none
+        if (i >= all) continue;
+        const int beam = (int)div_magic((uint32_t)i, (uint32_t)per_beam, g.beam_magic);
+        const float x = value_of_key(key[e]);
+        if (kind[beam] == 2) mine[e] = i == beam * per_beam ? scores[beam] : none;
+        else if (kind[beam] == 1 && key[e] && x != -__builtin_inff()) mine[e] = scores[beam] + (((double)x - (double)most[beam]) - log_s[beam]);
+        totals[i] = mine[e];
+        if (mine[e] > none && i - (int)div_magic((uint32_t)i, (uint32_t)g.n, g.list_magic) * g.n == g.n - 1) atomicAdd(&full, 1);
+    }
     __syncthreads();
-    // every full list answers for its share of the n
-    const int share = full ? (g.n + full - 1) / full : 0;
-    for (int i = threadIdx.x; i < lists; i += kThreads)
-        bounds[i] = full && total_of(i * g.n + g.n - 1) > -(double)__builtin_inff() ? total_of(i * g.n + share - 1) : (double)__builtin_inff();
+    // Every full list answers for its share of the n: as many are not below the least of those totals.  Nor are n below the last of any
+    // full list.
+    const int lists_full = full, share = lists_full ? (g.n + lists_full - 1) / lists_full : 0;
+    double bound = -none, last = none;
+#pragma unroll 1
+    for (int i = me; i < lists && share; i += kThreads) {
+        const double end = totals[i * g.n + g.n - 1];
+        if (end > none) bound = fmin(bound, totals[i * g.n + share - 1]);
+        last = fmax(last, end);
+    }
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) {
+        bound = fmin(bound, moved(bound, by));
+        last = fmax(last, moved(last, by));
+    }
+    if ((me & 63) == 0) {
+        wave_bound[me >> 6] = bound;
+        wave_last[me >> 6] = last;
+    }
     __syncthreads();
-    double bound = (double)__builtin_inff();
-    for (int i = 0; i < lists; ++i) bound = fmin(bound, bounds[i]);
-    if (!full) bound = -(double)__builtin_inff();
-    for (int i = threadIdx.x; i < all; i += kThreads) {
-        const double t = total_of(i);
-        if (t >= bound && t > -(double)__builtin_inff()) {
+    for (int w = 0; w < kWaves; ++w) {
+        bound = fmin(bound, wave_bound[w]);
+        last = fmax(last, wave_last[w]);
+    }
+    bound = share ? fmax(bound, last) : none;
+    // what is left takes the place of all
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if (mine[e] > none && mine[e] >= bound) {
             const int at = atomicAdd(&kept, 1);
-            totals[at] = t;
-            from[at] = (uint16_t)i;
+            totals[at] = mine[e];
+            from[at] = (uint16_t)(e * kThreads + me);
+            logits[at] = value_of_key(key[e]);
         }
-    }
     __syncthreads();
     const int count = kept;
-    for (int c = threadIdx.x; c < count; c += kThreads) {
+    if (me < 8) totals[count + me] = none;      // the walk below takes eight at a time
+    __syncthreads();
+    // Four lanes a candidate.  Of equals the lower beam comes first, of one beam's what comes first among its logits: the order of the
+    // candidates, unless slices have different logits that are equal as totals.
+#pragma unroll 1
+    for (int c0 = 0; c0 < count; c0 += kThreads / 4) {
+        const int c = min(c0 + me / 4, count - 1);
+        const int i = from[c], beam = (int)div_magic((uint32_t)i, (uint32_t)per_beam, g.beam_magic);
         const double t = totals[c];
-        const int i = from[c], list = i / g.n, beam = list / g.slices;
-        int before = 0;
-        for (int j = 0; j < count; ++j) {
-            if (totals[j] != t) {
-                before += totals[j] > t;
-                continue;
+        const float x = logits[c];
+        int before = 0, odd = 0;
+#pragma unroll 1
+        for (int j = me % 4 * 8; j < count; j += 32) {
+            double o[8];
+            float l[8];
+            uint32_t f[4];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] = totals[j + u];
+            __builtin_memcpy(f, from + j, 16);
+            __builtin_memcpy(l, logits + j, 32);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const bool same = o[u] == t;
+                before += o[u] > t || (same && (int)(f[u / 2] >> (16 * (u & 1)) & 0xffff) < i);
+                odd |= same && l[u] != x;
             }
-            // equals: the lower beam, then the beam's own order
-            const int other = from[j], other_list = other / g.n;
-            if (other_list == list || other_list / g.slices != beam) before += other < i;
-            else before += keys[other] > keys[i];
+        }
+        before = group_sum_i<4>(before);
+        odd = group_sum_i<4>(odd);
+        if (me % 4 || c0 + me / 4 >= count) continue;
+        if (odd && g.slices > 1) {
+            before = 0;
+#pragma unroll 1
+            for (int j = 0; j < count; ++j) {
+                const int o = from[j];
+                bool first = o < i;
+                if (totals[j] == t && (int)div_magic((uint32_t)o, (uint32_t)per_beam, g.beam_magic) == beam) first = keys[o] > keys[i];
+                before += totals[j] > t || (totals[j] == t && first);
+            }
         }
         if (before >= g.n) continue;
         const bool done = kind[beam] == 2;
@@ -316,7 +426,8 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(Args g) {
         g.out_parents[to] = beam;
         g.out_finished[to] = done || token == g.end;
     }
-    for (int j = count + threadIdx.x; j < g.n; j += kThreads) {
+#pragma unroll 1
+    for (int j = count + me; j < g.n; j += kThreads) {
         const int64_t to = b * g.n + j;
         g.out_scores[to] = -__builtin_inff();
         g.out_tokens[to] = (int32_t)(g.end < 0 ? 0 : g.end);
@@ -334,7 +445,7 @@ struct Plan {
 Plan plan_for(int dtype, int64_t rows, int W, int64_t V, int n) {
     const int E = 16 / dtype_bytes(dtype);
     const int64_t vectors = (V + E - 1) / E, batch = (int64_t)kThreads * (kBatch / E);
-    if (V <= 16384 && rows >= (V <= 2048 ? 1024 : 2048)) return {true, 1, vectors};
+    if (rows >= (V <= 2048 ? 1024 : 2048)) return {true, 1, vectors};
     // all lists of a sequence are joined by one workgroup, kCandidates at most
     const int64_t most = kCandidates / ((int64_t)W * n) < kSlices ? kCandidates / ((int64_t)W * n) : kSlices;
     int64_t slices = 1;
@@ -375,7 +486,10 @@ int launch(Args all, bool waves, hipStream_t st) {
         g.out_scores += out; g.out_tokens += out; g.out_parents += out; g.out_finished += out;
         int rc = waves ? launch_rows<XT, 64>(g, st) : launch_rows<XT, kThreads>(g, st);
         if (rc != BS_OK) return rc;
-        hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)g.B), dim3(kThreads), 0, st, g);
+        const int candidates = g.W * g.slices * g.n;
+        if (candidates <= kThreads) hipLaunchKernelGGL(beam_join_kernel<1>, dim3((unsigned)g.B), dim3(kThreads), 0, st, g);
+        else if (candidates <= 4 * kThreads) hipLaunchKernelGGL(beam_join_kernel<4>, dim3((unsigned)g.B), dim3(kThreads), 0, st, g);
+        else hipLaunchKernelGGL((beam_join_kernel<kCandidates / kThreads>), dim3((unsigned)g.B), dim3(kThreads), 0, st, g);
         rc = hip_status(hipGetLastError());
         if (rc != BS_OK) return rc;
     }
@@ -389,7 +503,7 @@ struct State {
     const char* in;
     char* out;
     int64_t pitch, out_pitch;
-    int32_t bytes, word;        // of a row; of a move: 16, 4 or 1, all rows being that much apart and as aligned
+    uint32_t pieces, rest;      // of a row: 16 bytes each, and the bytes behind them
     uint32_t first;             // workgroup, of those of a sequence
 };
 struct States {
@@ -397,38 +511,37 @@ struct States {
     int count;
     uint32_t groups;            // workgroups of a sequence
 };
+typedef uint32_t Anywhere __attribute__((ext_vector_type(4), aligned(1)));
 
-// A workgroup has some columns of all of a sequence's rows: every lane reads a word of each row before any is written, so a row may be
-// overwritten by another's.
+// A lane has 16 bytes (or one, behind the last 16) of all of a sequence's rows and reads all of them before it writes any: a row may be
+// overwritten by another's, and lanes have nothing to do with one another.  Rows behind the last are read as the last and go nowhere.
 template <typename T, int ROWS>
-__device__ __forceinline__ void move_rows(const State& s, int64_t row0, int W, uint32_t at, const int* parents) {
+__device__ __forceinline__ void move_rows(const State& s, int64_t row0, int W, uint32_t at, const int* parent) {
     T v[ROWS];
-    const bool mine = at < (uint32_t)s.bytes;
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) v[j] = *reinterpret_cast<const T*>(s.in + (row0 + parent[j]) * s.pitch + at);
 #pragma unroll
     for (int j = 0; j < ROWS; ++j)
-        if (mine && j < W) v[j] = *reinterpret_cast<const T*>(s.in + (row0 + parents[j]) * s.pitch + at);
-#pragma unroll
-    for (int j = 0; j < ROWS; ++j)
-        if (mine && j < W && !(parents[j] == j && s.in == s.out)) *reinterpret_cast<T*>(s.out + (row0 + j) * s.out_pitch + at) = v[j];
+        if (j < W && (parent[j] != j || s.in != s.out)) *reinterpret_cast<T*>(s.out + (row0 + j) * s.out_pitch + at) = v[j];
 }
 
+// ROWS >= W.  Bound: HBM, the parents' rows once and all rows once.
 template <int ROWS>
 __global__ __launch_bounds__(256) void beam_reorder_kernel(States all, int W, const int32_t* parents) {
-    __shared__ int parent[kWidth];
     const uint32_t b = blockIdx.x / all.groups, group = blockIdx.x % all.groups;
-    if ((int)threadIdx.x < ROWS) {
-        const int p = (int)threadIdx.x < W ? parents[(int64_t)b * W + threadIdx.x] : 0;
-        parent[threadIdx.x] = p >= 0 && p < W ? p : (int)threadIdx.x;
+    int parent[ROWS];
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        const int own = min(j, W - 1), p = parents[(int64_t)b * W + own];
+        parent[j] = p >= 0 && p < W ? p : own;
     }
     int i = 0;
     while (i + 1 < all.count && group >= all.s[i + 1].first) ++i;
     const State& s = all.s[i];
-    __syncthreads();
     const int64_t row0 = (int64_t)b * W;
-    const uint32_t at = ((group - s.first) * 256 + threadIdx.x) * (uint32_t)s.word;
-    if (s.word == 16) move_rows<uint4, ROWS>(s, row0, W, at, parent);
-    else if (s.word == 4) move_rows<uint32_t, ROWS>(s, row0, W, at, parent);
-    else move_rows<uint8_t, ROWS>(s, row0, W, at, parent);
+    const uint32_t piece = (group - s.first) * 256 + threadIdx.x;
+    if (piece < s.pieces) move_rows<Anywhere, ROWS>(s, row0, W, piece * 16, parent);
+    else if (piece - s.pieces < s.rest) move_rows<uint8_t, ROWS>(s, row0, W, s.pieces * 16 + (piece - s.pieces), parent);
 }
 
 }  // namespace
@@ -447,6 +560,7 @@ int launch_beam_step(const void* logits, int dtype, int64_t B, int W, int64_t V,
     Args g{};
     g.logits = logits; g.B = B; g.V = V; g.ld = ld; g.end = end; g.W = W; g.n = n;
     g.slices = p.slices; g.slice_vectors = p.slice_vectors;
+    g.beam_magic = magic_u32((uint32_t)(p.slices * n)); g.list_magic = magic_u32((uint32_t)n);
     g.scores = scores; g.finished = finished;
     g.out_scores = out_scores; g.out_tokens = out_tokens; g.out_parents = out_parents; g.out_finished = out_finished;
     g.sums = static_cast<Sum*>(workspace);
@@ -469,12 +583,10 @@ int launch_beam_reorder(int count, const void* const* states, void* const* outs,
         s.out = static_cast<char*>(outs[i]);
         s.pitch = pitch[i];
         s.out_pitch = out_pitch[i];
-        s.bytes = (int32_t)row_bytes[i];
-        const uint64_t bits = reinterpret_cast<uintptr_t>(states[i]) | reinterpret_cast<uintptr_t>(outs[i]) | (uint64_t)pitch[i] |
-                              (uint64_t)out_pitch[i] | (uint64_t)row_bytes[i];
-        s.word = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1;
+        s.pieces = (uint32_t)(row_bytes[i] / 16);
+        s.rest = (uint32_t)(row_bytes[i] % 16);
         s.first = (uint32_t)groups;
-        groups += ((uint64_t)row_bytes[i] + 256 * s.word - 1) / (256 * s.word);
+        groups += (s.pieces + s.rest + 255) / 256;
     }
     all.groups = (uint32_t)groups;
     // sequences of a launch: a grid has fewer than 2^32 lanes
@@ -482,7 +594,9 @@ int launch_beam_reorder(int count, const void* const* states, void* const* outs,
     for (int64_t b = 0; b < B; b += most) {
         const unsigned grid = (unsigned)((B - b < most ? B - b : most) * (int64_t)groups);
         if (W <= 4) hipLaunchKernelGGL(beam_reorder_kernel<4>, dim3(grid), dim3(256), 0, st, all, W, parents + b * W);
+        else if (W <= 8) hipLaunchKernelGGL(beam_reorder_kernel<8>, dim3(grid), dim3(256), 0, st, all, W, parents + b * W);
         else if (W <= 16) hipLaunchKernelGGL(beam_reorder_kernel<16>, dim3(grid), dim3(256), 0, st, all, W, parents + b * W);
+        else if (W <= 32) hipLaunchKernelGGL(beam_reorder_kernel<32>, dim3(grid), dim3(256), 0, st, all, W, parents + b * W);
         else hipLaunchKernelGGL(beam_reorder_kernel<64>, dim3(grid), dim3(256), 0, st, all, W, parents + b * W);
         const int rc = hip_status(hipGetLastError());
         if (rc != BS_OK) return rc;
