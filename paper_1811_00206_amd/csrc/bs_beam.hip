@@ -444,13 +444,12 @@ struct Plan {
 
 Plan plan_for(int dtype, int64_t rows, int W, int64_t V, int n) {
     const int E = 16 / dtype_bytes(dtype);
-    const int64_t vectors = (V + E - 1) / E, batch = (int64_t)kThreads * (kBatch / E);
+    const int64_t vectors = (V + E - 1) / E;
     if (rows >= (V <= 2048 ? 1024 : 2048)) return {true, 1, vectors};
     // all lists of a sequence are joined by one workgroup, kCandidates at most
     const int64_t most = kCandidates / ((int64_t)W * n) < kSlices ? kCandidates / ((int64_t)W * n) : kSlices;
     int64_t slices = 1;
-    if (vectors >= 2 * batch)
-        while (slices * 2 <= most && rows * slices < 512 && vectors / (slices * 2) >= kThreads) slices *= 2;
+    while (slices * 2 <= most && rows * slices < 512 && vectors / (slices * 2) >= 2 * kThreads) slices *= 2;
     Plan p{false, 1, (vectors + slices - 1) / slices};
     p.slices = (int)((vectors + p.slice_vectors - 1) / p.slice_vectors);
     return p;

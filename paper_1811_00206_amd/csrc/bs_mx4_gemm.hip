@@ -194,21 +194,21 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Tiles g, int64_t n0) {
 
 constexpr int kTileGroup = 400;      // these kernels' LDS limits are raised together: which one a product takes is a matter of its sizes
 
-template <typename XT, int TN, int TM, int WN, int WM, bool SPLIT>
+template <typename XT, int TN, int TM, int WN, int WM, int NB, bool SPLIT>
 int launch_tiles(const Mx4Tiles& g, hipStream_t st) {
-    constexpr auto kernel = mx4_tiles_kernel<XT, TN, TM, WN, WM, SPLIT>;
+    constexpr auto kernel = mx4_tiles_kernel<XT, TN, TM, WN, WM, NB, SPLIT>;
     const int rc = ensure_lds_limit(LdsKernelOf<kernel, kTileGroup>::reg, st, nullptr, kTileGroup);
     if (rc != BS_OK) return rc;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(g.m_tiles * g.n_tiles * g.split)), dim3(256), (kMx4LdsBytes<TN, TM>), st, g);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(g.m_tiles * g.n_tiles * g.split)), dim3(256), (kMx4LdsBytes<TN, TM, NB>), st, g);
     return hip_status(hipGetLastError());
 }
 
-template <typename XT, int TN, int TM, int WN, int WM>
+template <typename XT, int TN, int TM, int WN, int WM, int NB>
 int launch_tiles(Mx4Tiles g, hipStream_t st) {
     g.m_tiles = (int)((g.M + TM - 1) / TM);
     g.n_tiles = (int)((g.N + TN - 1) / TN);
-    if (g.split == 1) return launch_tiles<XT, TN, TM, WN, WM, false>(g, st);
-    const int rc = launch_tiles<F32, TN, TM, WN, WM, true>(g, st);
+    if (g.split == 1) return launch_tiles<XT, TN, TM, WN, WM, NB, false>(g, st);
+    const int rc = launch_tiles<F32, TN, TM, WN, WM, NB, true>(g, st);
     if (rc != BS_OK) return rc;
     const int64_t most = 65535;      // rows of a launch
     for (int64_t n = 0; n < g.N; n += most) {
@@ -222,45 +222,57 @@ int launch_tiles(Mx4Tiles g, hipStream_t st) {
 template <typename XT>
 int launch_tiles(const Mx4Tiles& t, int tn, hipStream_t st) {
     switch (tn) {
-        case 32: return launch_tiles<XT, 32, 128, 1, 4>(t, st);
-        case 64: return launch_tiles<XT, 64, 128, 1, 4>(t, st);
-        case 96: return launch_tiles<XT, 96, 128, 1, 4>(t, st);
-        case 128: return launch_tiles<XT, 128, 128, 2, 2>(t, st);
-        default: return launch_tiles<XT, 256, 256, 2, 2>(t, st);
+        case 32: return launch_tiles<XT, 32, 128, 1, 4, 4>(t, st);
+        case 64: return launch_tiles<XT, 64, 128, 1, 4, 4>(t, st);
+        case 96: return launch_tiles<XT, 96, 128, 1, 4, 4>(t, st);
+        case 127: return launch_tiles<XT, 128, 128, 2, 2, 4>(t, st);
+        case 128: return launch_tiles<XT, 128, 128, 2, 2, 2>(t, st);
+        default: return launch_tiles<XT, 256, 256, 2, 2, 2>(t, st);
     }
 }
 
 // ---- which
 
 struct Plan {
-    int tile;                      // rows of x in a tile; 0: no tiles
+    int tile;                      // kind of tiles; 0: none
     int split, stages;             // workgroups that share K, and the stages of 256 columns of each
     int r, nt, ways, groups;       // without tiles
 };
 
-// Microseconds of a product in tiles.  A stage takes a compute unit `alone` with one workgroup, `full` with as many as fit; measured with
-// 16384 x 8192, 4096 x 4096, 4096 x 25088 and 6600 x 13448 for 16 to 4096 rows, and right within a quarter for most of them.
+// What a product takes, in microseconds, as far as it takes to choose.  A round of tiles, `fit` for a compute unit, takes `begin` and for
+// each stage `full`, or `alone` where a compute unit has one; fitted to 300 x 600, 1024 x 1024, 4096 x 4096, 10000 x 1500, 32003 x 1500,
+// 4096 x 25088 and 16384 x 8192 for 16 to 4096 rows of x, which it meets within a quarter.  Large tiles read least for each product;
+// small ones leave room for four stages in LDS, and so has a second kind of 128 x 128, which two tiles of a compute unit are better than
+// where results count for more than the way to them (32003 x 1500 for 256 rows 13.9 us against 17.7, 16384 x 8192 28.0 against 24.3).
 struct Tile {
-    int n, m, fit;
-    double alone, full;
+    int kind, n, m, fit;
+    double alone, full, begin;
 };
-constexpr Tile kTiles[] = {{32, 128, 3, 0.65, 1.2}, {64, 128, 2, 0.8, 1.03}, {96, 128, 2, 0.85, 1.1}, {128, 128, 2, 0.9, 1.15}, {256, 256, 1, 1.8, 1.8}};
+constexpr Tile kTiles[] = {{32, 32, 128, 1, 0.45, 0.45, 2.2}, {64, 64, 128, 1, 0.5, 0.5, 2.8}, {96, 96, 128, 1, 0.56, 0.56, 3.2},
+                           {127, 128, 128, 1, 0.64, 0.64, 3.5}, {128, 128, 128, 2, 0.77, 1.1, 3.0}, {256, 256, 256, 1, 1.75, 1.75, 7.0}};
 
-double cost_of(const Tile& t, int64_t M, int64_t N, int stages, int split) {
+double matrix_us(int64_t M, int chunks) { return (double)M * chunks * 68 / 4.6e6; }
+
+double tiles_us(const Tile& t, int64_t M, int64_t N, int chunks, int stages, int split) {
     const double groups = (double)((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) * split, sums = (double)M * N * 4;
     const double rounds = groups <= 256 ? 1 : (double)(int64_t)((groups + 256 * t.fit - 1) / (256 * t.fit));
-    const double work = rounds * stages * (groups <= 256 ? t.alone : t.full), bytes = (double)M * stages * split * 136 / 4.6e6;
-    return 3 + (work > bytes ? work : bytes) + (split > 1 ? 2 + (2 * split + 0.5) * sums / 8e6 : 0);
+    const double work = rounds * (stages * (groups <= 256 ? t.alone : t.full) + t.begin), least = matrix_us(M, chunks);
+    return 2 + (work > least ? work : least) + (split > 1 ? 2 + (2 * split + 0.5) * sums / 8e6 : 0);
+}
+
+// the same for W straight from memory: every wavefront's steps one after the other, 2048 of them at a time
+double rows_us(const Plan& p, int64_t M, int chunks, int steps) {
+    const double waves = (double)((M + 16 * p.r - 1) / (16 * p.r)) * p.ways, rounds = waves < 2048 ? 1 : waves / 2048;
+    const double work = (steps + p.ways - 1) / p.ways * (1.3 + 0.65 * p.nt) * rounds, least = matrix_us(M, chunks);
+    return 2.5 + (work > least ? work : least);
 }
 
 Plan plan_for(int64_t M, int64_t K, int64_t N) {
-    const int chunks = (int)mx4_chunks(K), steps = (chunks + kStep - 1) / kStep;
+    const int chunks = (int)mx4_chunks(K), steps = (chunks + kStep - 1) / kStep, stages = (chunks + 1) / 2;
     const int64_t tiles = (M + 15) / 16;
     Plan p{};
-    // Rows of W straight from memory: for up to 16 rows of x, and for up to 64 where W has few.  (16384 x 8192 for 4 / 16 / 32 / 64 rows
-    // 14.5 / 17.0 / 21.9 / 33.7 us, 16.3 / 16.9 / 17.3 / 19.3 in tiles; 4096 x 4096 for 32 6.4 and 9.3, 2000 x 8000 for 64 10.1 and 11.3,
-    // 10000 x 1500 for 8 / 32 5.0 / 7.8 and 6.9 / 6.8.)
-    if (N <= 16 || (N <= 64 && tiles <= 320)) {
+    double least = 0;
+    if (N <= 64) {
         p.nt = N <= 16 ? 1 : N <= 32 ? 2 : 4;
         // Wavefronts that share K: as many as give the chip 2048 (eight for a compute unit), or what K has steps for; where two are
         // enough, four groups of them share x in LDS.  16384 x 8192 for one row: 17.1 us with 2 x 4, 18.9 with 1 x 4, 17.8 with
@@ -271,18 +283,18 @@ Plan plan_for(int64_t M, int64_t K, int64_t N) {
         const int most = p.nt == 4 ? 8 : 16;
         while (p.ways < most && tiles * p.ways < 2048 * p.r && p.ways < steps) p.ways *= 2;
         p.groups = p.ways <= 2 ? 4 : p.r == 2 ? 2 : 1;
-        return p;
+        least = rows_us(p, M, chunks, steps);
+        if (N <= kFusedRows) return p;
     }
-    const int stages = (chunks + 1) / 2;
-    double least = 0;
     for (const Tile& t : kTiles)
         for (int split = 1; split <= 16 && split <= stages; ++split) {
-            const int each = (stages + split - 1) / split, parts = (stages + each - 1) / each;
-            if (parts != split) continue;
-            const double cost = cost_of(t, M, N, each, split);
-            if (p.tile && cost >= least) continue;
+            const int each = (stages + split - 1) / split;
+            if ((stages + each - 1) / each != split) continue;
+            if (split > 1 && ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) * split > 1024) break;      // enough for the chip before
+            const double cost = tiles_us(t, M, N, chunks, each, split);
+            if (least && cost >= least) continue;
             least = cost;
-            p.tile = t.n;
+            p.tile = t.kind;
             p.split = split;
             p.stages = each;
         }
@@ -310,16 +322,18 @@ int launch(Args g, const Plan& p, float* sums, hipStream_t st) {
 
 }  // namespace
 
-size_t mx4_gemm_workspace_bytes(bool packed, int, int64_t M, int64_t K, int64_t N) {
-    const Plan p = plan_for(M, K, N);
+static size_t workspace_of(const Plan& p, bool packed, int64_t M, int64_t K, int64_t N) {
     return (packed || fused(K, N) ? 0 : packed_bytes(K, N)) + (p.split > 1 ? (size_t)p.split * M * N * 4 : 0);
+}
+size_t mx4_gemm_workspace_bytes(bool packed, int, int64_t M, int64_t K, int64_t N) {
+    return workspace_of(plan_for(M, K, N), packed, M, K, N);
 }
 
 int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int64_t ldx, const uint8_t* x_codes,
                     const uint8_t* x_scales, int dtype, int64_t N, const float* bias, void* y, int64_t ldy, void* workspace,
                     size_t workspace_bytes, hipStream_t st) {
     const Plan p = plan_for(M, K, N);
-    const size_t need = mx4_gemm_workspace_bytes(!x, dtype, M, K, N);
+    const size_t need = workspace_of(p, !x, M, K, N);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))) return BS_ERR_WORKSPACE;
     uint8_t* at = static_cast<uint8_t*>(workspace);
     const bool dense = x && fused(K, N);

@@ -1,8 +1,8 @@
 // Tiles of y = x W^T for MX 4-bit x and W (bs_mx4_gemm.hip).
 //
 // A workgroup makes TN rows of y by TM columns with four wavefronts, WN by WM of them, in 32x32x64 matrix instructions.  Both sides pass
-// through LDS in stages of 256 columns, which are whole cache lines of a row, two stages by turns: direct-to-LDS loads bring one while
-// the other is multiplied.  A row's eight 16-byte blocks lie in the order block ^ (row / 2 & 7): sixteen lanes' reads of one block, rows
+// through LDS in stages of 256 columns, which are whole cache lines of a row, NB stages in turns: direct-to-LDS loads bring the others
+// while one is multiplied.  A row's eight 16-byte blocks lie in the order block ^ (row / 2 & 7): sixteen lanes' reads of one block, rows
 // of 128 bytes, fall on all 64 LDS banks.  Scale bytes come for four stages at a time, 32 bytes of a row: a request to the cache takes as
 // long for a row's eight bytes as for a whole line, and those of every stage were half of all requests.  A wavefront's operands of the
 // next step are read while this one's are multiplied, over the end of a stage too: its last step first waits for the next stage, meets
@@ -32,8 +32,8 @@ template <int TN, int TM>
 constexpr int kMx4StageBytes = (TN + TM) * 128;
 template <int TN, int TM>
 constexpr int kMx4ScaleBytes = (TN + TM) * 8 * kMx4Group;
-template <int TN, int TM>
-constexpr int kMx4LdsBytes = 2 * (kMx4StageBytes<TN, TM> + kMx4ScaleBytes<TN, TM>);
+template <int TN, int TM, int NB>
+constexpr int kMx4LdsBytes = NB * kMx4StageBytes<TN, TM> + 2 * kMx4ScaleBytes<TN, TM>;
 
 // 16 (4) bytes for each lane of `lanes` (of the first 32 and of the last), from `base` + a lane's offset to LDS at `to`, lane after lane.  In assembly: the compiler takes
 // every read of LDS for one of what such a load brings, and would wait for all that are on their way.  Nothing in registers is written
@@ -65,7 +65,7 @@ __device__ __forceinline__ void mx4_tile_of(const Mx4Tiles& g, uint32_t id, int&
     m = first + id % rows;
 }
 
-template <typename XT, int TN, int TM, int WN, int WM, bool SPLIT>
+template <typename XT, int TN, int TM, int WN, int WM, int NB, bool SPLIT>
 __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
     static_assert(WN * WM == 4);
     constexpr int IN = TN / WN / 32, IM = TM / WM / 32, kSlots = IN * IM;
@@ -92,23 +92,23 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
     const auto row_of = [&](int r) { return r < TN ? min((uint32_t)r, x_last) : min((uint32_t)(r - TN), w_last); };
 #pragma unroll
     for (int i = 0; i < kCodeLoads; ++i) from[i] = row_of((i * 4 + wave) * 8 + (lane >> 3)) * pitch + 16 * block;
-    // Scales: two lanes bring a row's 32 bytes.  A group that is not whole comes by words, eight lanes a row, those behind the last again
+    // Scales: two lanes bring a row's 32 bytes, the second half in front in every other eight rows, for the sake of LDS banks.  A group that is not whole comes by words, eight lanes a row, those behind the last again
     // the last.  (Where rows are no multiple of 128 some wavefronts bring what another brings too.)
     const auto scale_row = [&](int i) { return min((i * 4 + wave) * 32, kRows - 32); };
     uint32_t scale_from[kScaleLoads];
     uint32_t word_from[kScaleLoads][4];
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
-        scale_from[i] = row_of(scale_row(i) + (lane >> 1)) * scale_pitch + 16 * (lane & 1);
+        scale_from[i] = row_of(scale_row(i) + (lane >> 1)) * scale_pitch + 16 * ((lane & 1) ^ (lane >> 4 & 1));
 #pragma unroll
         for (int j = 0; j < 4; ++j) word_from[i][j] = row_of(scale_row(i) + 8 * j + (lane >> 3)) * scale_pitch;
     }
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    constexpr int kScalesAt = 2 * kMx4StageBytes<TN, TM>;
+    constexpr int kScalesAt = NB * kMx4StageBytes<TN, TM>;
     // Lanes that bring blocks 4 .. 7 stay out of a last stage of one chunk, all of a stage behind the last one.
     const uint32_t first_blocks = wave & 1 ? 0xf0f0f0f0u : 0x0f0f0f0fu;
     const auto send = [&](int stage, int i0, int i1) {      // loads i0 .. i1 - 1 of a stage
-        const uint32_t to = lds_at + (stage & 1) * kMx4StageBytes<TN, TM>;
+        const uint32_t to = lds_at + stage % NB * kMx4StageBytes<TN, TM>;
         const uint32_t lanes = __builtin_amdgcn_readfirstlane(stage >= last ? 0u : 2 * stage + 2 > g.chunks ? first_blocks : ~0u);
 #pragma unroll
         for (int i = 0; i < kCodeLoads; ++i)
@@ -122,9 +122,9 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
         const uint32_t lanes = __builtin_amdgcn_readfirstlane(any && whole ? ~0u : 0u), by_words = __builtin_amdgcn_readfirstlane(any && !whole ? ~0u : 0u);
         const uint8_t* const base = r < TN ? xsc : wsc;
         send_to_lds<16>(base + (int64_t)chunk * 4, scale_from[i], to, lanes);
-        const uint32_t word = 4 * (uint32_t)min(chunk + (lane & 7), g.chunks - 1);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) send_to_lds<4>(base, word_from[i][j] + word, to + j * 256, by_words);
+        for (int j = 0; j < 4; ++j)
+            send_to_lds<4>(base, word_from[i][j] + 4 * (uint32_t)min(chunk + ((lane & 7) ^ 4 * (j & 1)), g.chunks - 1), to + j * 256, by_words);
     };
 
     const int wn = wave / WM * (IN * 32), wm = wave % WM * (IM * 32), half = lane >> 5;
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
         for (int j = 0; j < IM; ++j) asm volatile("" : "+a"(acc[i][j]));
     const auto read_scales = [&](int slot, int stage) {
         const int n = stage - first;
-        const uint8_t* const at = lds + kScalesAt + (n / kMx4Group & 1) * kMx4ScaleBytes<TN, TM> + n % kMx4Group * 8;
+        const uint8_t* const at = lds + kScalesAt + (n / kMx4Group & 1) * kMx4ScaleBytes<TN, TM> + ((n % kMx4Group * 8) ^ ((lane & 8) * 2));
 #pragma unroll
         for (int e = 0; e < IN + IM; ++e) {
             if (min(e / 2, kSlots - 1) != slot) continue;      // early in a step: they are the first that the next one needs
@@ -166,9 +166,11 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
             ws[j][1] = w_next[j].y >> (8 * half);
         }
     };
-    const auto arrive = [&]() {      // all that this wavefront has sent for is there, and all that it has read
+    // What this wavefront has read is there, and what it has sent for: all, or all but the loads of the last NB - 2 stages.  (Scales among
+    // those make it wait for a few more.)
+    const auto arrive = [&](auto LEFT) {
         pin_order();
-        wait_vm_and_lds<0>();
+        wait_vm_and_lds<decltype(LEFT)::value>();
         __builtin_amdgcn_s_barrier();
         pin_order();
     };
@@ -192,7 +194,7 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
     const std::integral_constant<int, 3> S3;
     // operands of step s of a stage, one read in each of the first slots
     const auto read = [&](int n, int stage, int s) {
-        const uint8_t* const at = lds + (stage & 1) * kMx4StageBytes<TN, TM> + 16 * ((2 * s + half) ^ (lane >> 1 & 7));
+        const uint8_t* const at = lds + stage % NB * kMx4StageBytes<TN, TM> + 16 * ((2 * s + half) ^ (lane >> 1 & 7));
 #pragma unroll
         for (int e = 0; e < IN + IM; ++e) {
             if (e * kSlots / (IN + IM) != n) continue;      // in the order in which they are needed
@@ -205,20 +207,23 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
 #pragma unroll
         for (int n = 0; n < kSlots; ++n) part(n);
     };
-    constexpr int kEarly = kCodeLoads / 2;
+        constexpr int kEarly = kCodeLoads / 2, kLeft = (NB - 2) * kCodeLoads;
+    static_assert(kLeft < 64);
+    const std::integral_constant<int, kLeft> ALL_BUT_LATER;
     const int whole = min(last, g.chunks / 2);      // stages of two chunks
-    send(first, 0, kCodeLoads);
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) send_scales(0, i);
-    arrive();
-    send(first + 1, 0, kEarly);
+#pragma unroll
+    for (int i = 0; i < NB - 1; ++i) send(first + i, 0, kCodeLoads);
+    arrive(ALL_BUT_LATER);
+    send(first + NB - 1, 0, kEarly);
     all_of([&](int n) { read(n, first, 0); });
     all_of([&](int n) { read_scales(n, first); });
     for (int k = first; k < whole; ++k) {
         take_scales();
         step(S0, [&](int n) {
             read(n, k, 1);
-            send(k + 1, kEarly + n * (kCodeLoads - kEarly) / kSlots, kEarly + (n + 1) * (kCodeLoads - kEarly) / kSlots);
+            send(k + NB - 1, kEarly + n * (kCodeLoads - kEarly) / kSlots, kEarly + (n + 1) * (kCodeLoads - kEarly) / kSlots);
         });
         // the next group's scales, all at the group's first stage: their place is free since the stage before
         if ((k - first) % kMx4Group == 0) {
@@ -227,11 +232,11 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
         }
         step(S1, [&](int n) { read(n, k, 2); });
         step(S2, [&](int n) { read(n, k, 3); });
-        arrive();
+        arrive(ALL_BUT_LATER);      // the next stage is there, and this one's place may be taken
         step(S3, [&](int n) {
             read(n, k + 1, 0);
             read_scales(n, k + 1);
-            send(k + 2, n * kEarly / kSlots, (n + 1) * kEarly / kSlots);
+            send(k + NB, n * kEarly / kSlots, (n + 1) * kEarly / kSlots);
         });
     }
     if (whole < last) {      // a stage of one chunk, which is the last one
@@ -244,11 +249,11 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
     // whole rows.
     using T = std::conditional_t<SPLIT, float, typename XT::type>;
     constexpr int kCols = IM * 32, kPitch = kCols + 16 / (int)sizeof(T);      // elements
-    static_assert(4 * 32 * kPitch * (int)sizeof(T) <= kMx4LdsBytes<TN, TM>);
+    static_assert(4 * 32 * kPitch * (int)sizeof(T) <= kMx4LdsBytes<TN, TM, NB>);
     __syncthreads();
     T* const mine = reinterpret_cast<T*>(lds) + wave * 32 * kPitch;
     float* const bias = reinterpret_cast<float*>(lds + 4 * 32 * kPitch * sizeof(T));
-    static_assert(4 * 32 * kPitch * (int)sizeof(T) + TM * 4 <= kMx4LdsBytes<TN, TM>);
+    static_assert(4 * 32 * kPitch * (int)sizeof(T) + TM * 4 <= kMx4LdsBytes<TN, TM, NB>);
     if constexpr (!SPLIT) {
         for (int i = threadIdx.x; i < TM; i += 256) bias[i] = g.bias ? g.bias[min(m0 + i, g.M - 1)] : 0.f;
         __syncthreads();
@@ -287,9 +292,18 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
                 *reinterpret_cast<Anywhere*>(to + r0 * ld) = Anywhere{v.x, v.y, v.z, v.w};
             }
         } else {
+            const bool piece = mw + col + kPer <= g.M;
+#pragma unroll
             for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
-                if (n0 + wn + 32 * i + r0 + r >= g.N) break;
-                for (int e = 0; e < kPer && mw + col + e < g.M; ++e) to[r0 * ld + e] = mine[(r0 + r) * kPitch + col + e];
+                if (n0 + wn + 32 * i + r0 + r >= g.N) continue;
+                const T* const v = mine + (r0 + r) * kPitch + col;
+                if (piece) {
+                    const uint4 a = *reinterpret_cast<const uint4*>(v);
+                    *reinterpret_cast<Anywhere*>(to + r0 * ld) = Anywhere{a.x, a.y, a.z, a.w};
+                } else {
+#pragma unroll 1
+                    for (int e = 0; mw + col + e < g.M; ++e) to[r0 * ld + e] = v[e];
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
