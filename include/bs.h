@@ -464,6 +464,10 @@ size_t bs_mx4_gemm_packed_workspace_bytes(int dtype, int64_t M, int64_t K, int64
 int bs_mx4_gemm_packed(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const uint8_t* x_codes,
                        const uint8_t* x_scales, int64_t N, const float* bias, void* y, int dtype, int64_t ldy, void* workspace,
                        size_t workspace_bytes, void* stream);
+/* HOST ONLY: how such a product is made.  out: rows and columns of y of a tile (0: W goes straight from memory to the matrix unit), stages
+ * in LDS, workgroups that share K, stages of 256 columns of each; 16 rows of W of a wavefront, 16 rows of x, wavefronts that share K,
+ * groups of them in a workgroup (0 for tiles); workgroups, bytes of LDS. */
+int bs_mx4_gemm_plan(int64_t M, int64_t K, int64_t N, int64_t* out, int n_out);
 
 /*
  * One step of beam search for B sequences of W beams each: of all continuations, the n with the best score.

@@ -30,7 +30,7 @@ EXPORTS = (
     "bs_q4_codes_bytes", "bs_q4_scales_bytes", "bs_q4_pack", "bs_q4_unpack", "bs_q4_gemv_workspace_bytes", "bs_q4_gemv",
     "bs_q4_moe_workspace_bytes", "bs_q4_moe", "bs_logprobs_workspace_bytes", "bs_logprobs", "bs_logprobs_backward",
     "bs_mx4_codes_bytes", "bs_mx4_scales_bytes", "bs_mx4_pack", "bs_mx4_unpack", "bs_mx4_gemm_workspace_bytes", "bs_mx4_gemm",
-    "bs_mx4_gemm_packed_workspace_bytes", "bs_mx4_gemm_packed", "bs_beam_step_workspace_bytes", "bs_beam_step", "bs_beam_reorder",
+    "bs_mx4_gemm_packed_workspace_bytes", "bs_mx4_gemm_packed", "bs_mx4_gemm_plan", "bs_beam_step_workspace_bytes", "bs_beam_step", "bs_beam_reorder",
 )
 
 
@@ -125,9 +125,10 @@ def load_library():
     lib.bs_mx4_unpack.argtypes = [vp, vp, i64, i64, vp, i32, vp]
     lib.bs_mx4_gemm.argtypes = [vp, vp, i64, i64, vp, i32, i64, i64, vp, vp, i64, vp, sz, vp]
     lib.bs_mx4_gemm_packed.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp, vp, i32, i64, vp, sz, vp]
+    lib.bs_mx4_gemm_plan.argtypes = [i64, i64, i64, ctypes.POINTER(ctypes.c_int64), i32]
     lib.bs_beam_step.argtypes = [vp, i32, i64, i32, i64, i64, vp, vp, i64, i32, vp, vp, vp, vp, vp, sz, vp]
     lib.bs_beam_reorder.argtypes = [i32, vp, vp, vp, vp, vp, i64, i32, vp, vp]
-    for name in ("bs_mx4_pack", "bs_mx4_unpack", "bs_mx4_gemm", "bs_mx4_gemm_packed", "bs_beam_step", "bs_beam_reorder"):
+    for name in ("bs_mx4_pack", "bs_mx4_unpack", "bs_mx4_gemm", "bs_mx4_gemm_packed", "bs_mx4_gemm_plan", "bs_beam_step", "bs_beam_reorder"):
         getattr(lib, name).restype = i32
     lib.bs_init.argtypes = []
     for name in ("bs_init", "bs_prune_pack", "bs_spmv", "bs_spmv_ex", "bs_spmm", "bs_spmm_static", "bs_dense_gemv",
@@ -1000,6 +1001,16 @@ def bs_mx4_gemm_packed(codes, scales, x_codes, x_scales, K: int, dtype=torch.flo
     _check(lib.bs_mx4_gemm_packed(_ptr(codes), _ptr(scales), M, K, _ptr(x_codes), _ptr(x_scales), N, _ptr(bias), _ptr(y), code, ldy,
                                   _ptr(workspace), ws_bytes, _stream()), "bs_mx4_gemm_packed")
     return y
+
+
+MX4_PLAN_FIELDS = ("tile_rows", "tile_columns", "buffers", "split", "stages", "r", "nt", "ways", "groups", "workgroups", "lds_bytes")
+
+
+def bs_mx4_gemm_plan(M: int, K: int, N: int) -> dict:
+    """How a product of an MX matrix [M, K] with N rows is made (host only)."""
+    out = (ctypes.c_int64 * len(MX4_PLAN_FIELDS))()
+    _check(load_library().bs_mx4_gemm_plan(M, K, N, out, len(MX4_PLAN_FIELDS)), "bs_mx4_gemm_plan")
+    return dict(zip(MX4_PLAN_FIELDS, (int(v) for v in out)))
 
 
 def bs_beam_step_workspace_bytes(dtype: int, B: int, W: int, V: int, n: int) -> int:

@@ -97,6 +97,7 @@ size_t mx4_gemm_workspace_bytes(bool packed, int dtype, int64_t M, int64_t K, in
 int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int64_t ldx, const uint8_t* x_codes,
                     const uint8_t* x_scales, int dtype, int64_t N, const float* bias, void* y, int64_t ldy, void* workspace,
                     size_t workspace_bytes, hipStream_t st);
+void mx4_gemm_plan_describe(int64_t M, int64_t K, int64_t N, int64_t* out, int n_out);
 size_t beam_step_workspace_bytes(int dtype, int64_t B, int W, int64_t V, int n);
 int launch_beam_step(const void* logits, int dtype, int64_t B, int W, int64_t V, int64_t ld, const float* scores, const uint8_t* finished,
                      int64_t end, int n, float* out_scores, int32_t* out_tokens, int32_t* out_parents, uint8_t* out_finished,

@@ -224,6 +224,14 @@ int bs_mx4_gemm_packed(const uint8_t* codes, const uint8_t* scales, int64_t M, i
                                static_cast<hipStream_t>(stream));
 }
 
+int bs_mx4_gemm_plan(int64_t M, int64_t K, int64_t N, int64_t* out, int n_out) {
+    if (!out) return BS_ERR_NULL;
+    if (!matrix_ok(M, K) || N < 1 || n_out < 1) return BS_ERR_SHAPE;
+    if (M > kMost || K > kMost || N > kMost || M * N > kMostOutputs) return BS_ERR_UNSUPPORTED;
+    bs::mx4_gemm_plan_describe(M, K, N, out, n_out);
+    return BS_OK;
+}
+
 size_t bs_beam_step_workspace_bytes(int dtype, int64_t B, int W, int64_t V, int n) {
     if (B < 1 || B > kMost || W < 1 || W > BS_BEAM_WIDTH_MAX || n < 1 || n > BS_BEAM_WIDTH_MAX || V < 1 ||
         V >= ((int64_t)1 << 31) - 64 || !type_ok(dtype))

@@ -179,7 +179,14 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Tiles g, int64_t n0) {
     typename XT::type* const to = static_cast<typename XT::type*>(g.y) + n * g.ldy + m;
     if (m + 4 <= g.M) {
         Floats s = *reinterpret_cast<const Floats*>(from);
-        for (int i = 1; i < g.split; ++i) s += *reinterpret_cast<const Floats*>(from + i * all);
+        for (int i = 1; i < g.split; i += 4) {      // four on their way together; those behind the last are the last one again
+            Floats v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const Floats*>(from + min(i + u, g.split - 1) * all);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u < g.split) s += v[u];
+        }
         if (g.bias) s += *reinterpret_cast<const Floats*>(g.bias + m);
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[e] = XT::store(s[e]);
@@ -280,7 +287,7 @@ Plan plan_for(int64_t M, int64_t K, int64_t N) {
         // of 16.0 for 4 rows and 17.0 instead of 20.9 for 16.
         p.r = N > kFusedRows && N <= 16 && tiles >= 1024 && steps >= 8 ? 2 : 1;
         p.ways = 1;
-        const int most = p.nt == 4 ? 8 : 16;
+        const int most = p.nt * p.r > 1 ? 8 : 16;      // wavefronts of a workgroup
         while (p.ways < most && tiles * p.ways < 2048 * p.r && p.ways < steps) p.ways *= 2;
         p.groups = p.ways <= 2 ? 4 : p.r == 2 ? 2 : 1;
         least = rows_us(p, M, chunks, steps);
@@ -321,6 +328,27 @@ int launch(Args g, const Plan& p, float* sums, hipStream_t st) {
 }
 
 }  // namespace
+
+void mx4_gemm_plan_describe(int64_t M, int64_t K, int64_t N, int64_t* out, int n_out) {
+    const Plan p = plan_for(M, K, N);
+    int64_t v[11] = {};
+    if (p.tile) {
+        for (const Tile& t : kTiles) {
+            if (t.kind != p.tile) continue;
+            v[0] = t.n, v[1] = t.m, v[2] = t.fit == 1 && t.n < 256 ? 4 : 2;
+            v[9] = ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) * p.split;
+            v[10] = (t.n + t.m) * (128 * v[2] + 2 * 8 * kMx4Group);
+        }
+        v[3] = p.split, v[4] = p.stages;
+    } else {
+        v[5] = p.r, v[6] = p.nt, v[7] = p.ways, v[8] = p.groups;
+        const int64_t rows = 16 * p.r * p.groups, sums = (int64_t)p.ways * p.groups * p.r * p.nt * 1024,
+                      x = fused(K, N) ? N * (64 * mx4_chunks(K) + 4 * ((mx4_chunks(K) + 3) & ~(int64_t)3)) : 0;
+        v[9] = (M + rows - 1) / rows;
+        v[10] = sums > x ? sums : x;
+    }
+    for (int i = 0; i < n_out && i < 11; ++i) out[i] = v[i];
+}
 
 static size_t workspace_of(const Plan& p, bool packed, int64_t M, int64_t K, int64_t N) {
     return (packed || fused(K, N) ? 0 : packed_bytes(K, N)) + (p.split > 1 ? (size_t)p.split * M * N * 4 : 0);

@@ -191,3 +191,38 @@ def test_products_are_the_same_every_time():
         room = torch.empty(N, K + 1, device=DEV)[:, 1:]
         room.copy_(x)
         assert torch.equal(bs.bs_mx4_gemm(*W, room), y)
+
+
+# one of every kind: rows of W from memory (16 rows of W of a wavefront, 16 rows of x, wavefronts that share K, groups), tiles (rows, columns,
+# stages in LDS, whether K is split)
+KINDS = [((1, 619, 1), (1, 1, 2, 4)), ((40, 1108, 1), (1, 1, 4, 1)), ((17, 2269, 2), (1, 1, 8, 1)), ((33, 4893, 1), (1, 1, 16, 1)), ((5, 308, 22), (1, 2, 1, 4)),
+         ((100, 530, 17), (1, 2, 2, 4)), ((30, 1092, 18), (1, 2, 4, 1)), ((50, 2137, 21), (1, 2, 8, 1)), ((60, 1088, 34), (1, 4, 4, 1)),
+         ((90, 2060, 50), (1, 4, 8, 1)), ((17199, 3899, 10), (2, 1, 4, 2)), ((300, 200, 100), (32, 128, 4, False)), ((3, 1480, 66), (32, 128, 4, True)),
+         ((134, 2, 4413), (64, 128, 4, False)), ((3, 1541, 2054), (64, 128, 4, True)), ((20052, 4, 67), (96, 128, 4, False)), ((3, 3154, 1812), (96, 128, 4, True)),
+         ((19690, 200, 97), (128, 128, 2, False)), ((2, 2648, 2441), (128, 128, 2, True)), ((2139, 849, 1587), (128, 128, 4, False)),
+         ((1314, 7772, 527), (128, 128, 4, True)), ((2562, 538, 3608), (256, 256, 2, False)), ((2876, 13468, 1504), (256, 256, 2, True))]
+
+
+@pytest.mark.parametrize("shape,kind", KINDS)
+def test_every_kind_of_product(shape, kind):
+    M, K, N = shape
+    p = bs.bs_mx4_gemm_plan(M, K, N)
+    found = (p["tile_rows"], p["tile_columns"], p["buffers"], p["split"] > 1) if p["tile_rows"] else (p["r"], p["nt"], p["ways"], p["groups"])
+    assert found == kind
+    g = torch.Generator().manual_seed(M + K + N)
+    x, W = torch.randn(N, K, generator=g).to(DEV), bs.bs_mx4_pack(torch.randn(M, K, generator=g).to(DEV))
+    bias = torch.randn(M, generator=g).to(DEV)
+    Xq, Wq = bs.bs_mx4_unpack(*bs.bs_mx4_pack(x), K).double(), bs.bs_mx4_unpack(*W, K).double()
+    for dtype in TYPES:
+        xd = x.to(dtype)
+        q = Xq if dtype == torch.float32 else bs.bs_mx4_unpack(*bs.bs_mx4_pack(xd), K).double()
+        want = q @ Wq.t() + bias.double()
+        y = bs.bs_mx4_gemm(*W, xd, bias=bias)
+        size = q.abs() @ Wq.abs().t() + bias.double().abs()
+        assert bool(((y.double() - want).abs() <= (-(-K // 64) + 18) * 2.0**-23 * size + torch.finfo(dtype).eps / 2 * want.abs() + 2.0**-149).all())
+        # a place whose rows lie further apart, and nothing beside them
+        place = torch.full((N + 2, M + 3), 7.0, dtype=dtype, device=DEV)
+        bs.bs_mx4_gemm(*W, xd, bias=bias, out=place[1:N + 1, 1:M + 1])
+        assert torch.equal(place[1:N + 1, 1:M + 1], y)
+        place[1:N + 1, 1:M + 1] = 7.0
+        assert bool((place == 7.0).all())

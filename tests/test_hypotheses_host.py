@@ -2,6 +2,7 @@
 launched, the native marshalling behind a stand-in for the library, and what the compiler made of the kernels."""
 import ctypes
 import os
+import random
 import re
 import subprocess
 import sys
@@ -47,6 +48,33 @@ def test_workspaces():
     for args in ((5, 1, 4, 100, 4), (0, 0, 4, 100, 4), (0, 1, 0, 100, 4), (0, 1, 65, 100, 4), (0, 1, 4, 0, 4), (0, 1, 4, 100, 0), (0, 1, 4, 100, 65),
                  (0, 1, 4, 1 << 31, 4), (0, (1 << 24) + 1, 4, 100, 4)):
         assert beam(*args) == 0
+
+
+def test_plans_of_products():
+    """What the kernels assume of their launch, over random shapes and the largest ones."""
+    g = random.Random(3)
+    shapes = [(round(2 ** g.uniform(0, 24)), round(2 ** g.uniform(0, 24)), round(2 ** g.uniform(0, 12))) for _ in range(4000)]
+    shapes += [(round(2 ** g.uniform(0, 18)), round(2 ** g.uniform(0, 14)), round(2 ** g.uniform(0, 18))) for _ in range(2000)]
+    for M, K, N in shapes + [(1 << 24, 1 << 24, 1), (1 << 24, 128, 4096), (4096, 128, 1 << 24), (1 << 18, 1 << 24, 1 << 18)]:
+        p = b.bs_mx4_gemm_plan(M, K, N)
+        chunks = -(-K // 128)
+        if p["tile_rows"]:
+            stages = -(-chunks // 2)
+            assert p["split"] * p["stages"] >= stages > (p["split"] - 1) * p["stages"], (M, K, N)
+            assert p["lds_bytes"] == (p["tile_rows"] + p["tile_columns"]) * (128 * p["buffers"] + 64) <= 160 * 1024
+            assert p["workgroups"] == -(-M // p["tile_columns"]) * -(-N // p["tile_rows"]) * p["split"] and p["workgroups"] * 256 < 1 << 32, (M, K, N, p)
+        else:
+            assert p["workgroups"] * 16 * p["r"] * p["groups"] >= M and 16 * p["nt"] >= N and p["lds_bytes"] <= 48 * 1024, (M, K, N, p)
+            threads = 64 * p["ways"] * p["groups"]
+            assert threads <= (1024 if p["r"] * p["nt"] == 1 else 512) and p["workgroups"] * threads < 1 << 32
+    for args in ((0, 8, 8), (8, 0, 8), (8, 8, 0)):
+        with pytest.raises(b.BsError) as e:
+            b.bs_mx4_gemm_plan(*args)
+        assert e.value.status == 2
+    for args in (((1 << 24) + 1, 8, 8), (8, (1 << 24) + 1, 8), (8, 8, (1 << 24) + 1), (1 << 20, 8, (1 << 16) + 1)):
+        with pytest.raises(b.BsError) as e:
+            b.bs_mx4_gemm_plan(*args)
+        assert e.value.status == 3
 
 
 def test_bad_arguments_are_refused_before_launch():
