@@ -1,10 +1,11 @@
 // One step of beam search, and the states that follow it (bs.h: bs_beam_step, bs_beam_reorder).
 //
-// The step.  Bound: HBM, the logits of the beams that go on once.  What orders the words of one beam are its logits; what orders those
-// of different beams is a difference of two sums, which must not depend on how either was rounded, so sums are made in 64 bits: with
-// u = (x - m) log2(e), the sum of 2^u by a polynomial of degree 7 between -1/2 and 1/2 (off by 5e-11, and exact at 0: a word that is
-// certain has log probability 0), its exponent added to the number's own.  64-bit operations run at the rate of 32-bit ones here, and one exponential is about as many as a 32-bit one takes
-// with the transcendental unit's four.  Elements come to threads by their index, wherever a row starts in memory: beams with the same
+// The step.  Bound: HBM, the logits of the beams that go on once; measured: the vector ALU.  What orders the words of one beam are its
+// logits; what orders those of different beams is a difference of two sums, which must not depend on how either was rounded, so sums are
+// made in 64 bits: 2^u by a polynomial of degree 7 between -1/2 and 1/2 (off by 5e-11, and exact at 0: a word that is certain has log
+// probability 0), its exponent, less that of the row's largest, added to the number's own.  64-bit operations run at the rate of 32-bit
+// ones here (2.4 ns a wavefront's instruction on a SIMD), so the exponential of an element is 15 of them; with unpacking and the largest
+// of every eight an element is 17.  Elements come to threads by their index, wherever a row starts in memory: beams with the same
 // logits have the same sums to the last bit, and tie.  A row's n largest are found as bs_logprobs finds them.
 // A second kernel joins the rows of a sequence: a candidate's total is scores + ((x - m) - log s); of the lists that are full each
 // answers for its share of the n, the least of those totals is a bound, and what reaches it is ordered by counting what comes before.
@@ -25,10 +26,10 @@ static_assert(kWidth <= kTopMax);
 
 typedef uint32_t Pair __attribute__((ext_vector_type(2)));
 
-// 2^u for -1000 < u < 1000, 1 for 0
-__device__ __forceinline__ double exp2_wide(double u) {
-    constexpr double kMagic = 0x1.8p52;      // the whole part, in the low bits
-    const double t = u + kMagic, f = u - (t - kMagic);
+constexpr double kMagic = 0x1.8p52;      // added to a number, its whole part is in the low bits
+
+// 2^f times 2^(the number in t's low bits), -1/2 <= f <= 1/2; 1 for 0 and 0
+__device__ __forceinline__ double exp2_parts(double f, double t) {
     double p = 0x1.fde5fe3497e78p-17;
     p = fma(p, f, 0x1.445c8421d1ed2p-13);
     p = fma(p, f, 0x1.5d8a85ff048c0p-10);
@@ -40,6 +41,15 @@ __device__ __forceinline__ double exp2_wide(double u) {
     Pair v = __builtin_bit_cast(Pair, p);
     v[1] += __builtin_bit_cast(Pair, t)[0] << 20;
     return __builtin_bit_cast(double, v);
+}
+// exp(x) 2^-c, given magic = kMagic - c; c is whole, |x log2(e) - c| < 1000
+__device__ __forceinline__ double exp_over(float x, double magic) {
+    const double wide = (double)x, t = fma(wide, kLog2e, magic);
+    return exp2_parts(fma(wide, kLog2e, -(t - magic)), t);
+}
+__device__ __forceinline__ double exp2_wide(double u) {      // -1000 < u < 1000
+    const double t = u + kMagic;
+    return exp2_parts(u - (t - kMagic), t);
 }
 
 // the sum of exp(x - m) over some of a row; m is -inf before anything was seen
@@ -58,6 +68,33 @@ __device__ __forceinline__ double moved(double v, int by) {
     const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)b, by, 64), hi = (uint32_t)__shfl_xor((int)(b >> 32), by, 64);
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
+// A thread's sum while it is made, in units of 2^c: c is the whole number next to m log2(e) when it was set, which the exponents absorb
+// for nothing.  Far from 0 the unit is exp(m), and logits are taken as differences from m in fp32, exact or far beyond -600.
+struct Running {
+    double s = 0.0, magic = kMagic;      // kMagic - c
+    float m = -__builtin_inff();
+    bool far = false;
+    __device__ __forceinline__ void raise(float to) {
+        const bool now_far = !(fabsf(to) <= 0x1p20f);
+        const double exponent = (double)to * kLog2e;
+        const bool same = !now_far && !far && m != -__builtin_inff() && fabs(exponent - (kMagic - magic)) < 300.0;
+        if (!same) {
+            const double now = now_far ? kMagic : kMagic - rint(exponent);
+            // both units as powers of 2
+            const double before = (far ? (double)m * kLog2e : 0.0) + (kMagic - magic), after = (now_far ? exponent : 0.0) + (kMagic - now);
+            if (m == -__builtin_inff()) s = s != s ? s : 0.0;      // what was cut off at -600 from nothing
+            else if (to == __builtin_inff()) s = __builtin_nan("");
+            else s *= exp2_wide(fmin(fmax(before - after, -900.0), 900.0));
+            magic = now;
+        }
+        m = to;
+        far = now_far;
+    }
+    // in units of exp(m), by the same exponential: a certain word's sum is 1
+    __device__ __forceinline__ Sum sum() const {
+        return Sum{m == -__builtin_inff() ? (s != s ? s : 0.0) : far ? s : s / exp_over(m, magic), m};
+    }
+};
 template <int CTRL>
 __device__ __forceinline__ double dpp_wide(double v) {
     Pair p = __builtin_bit_cast(Pair, v);
@@ -151,7 +188,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
     const R row(g.logits, r, g.ld, g.V);
     const int64_t v0 = slice * g.slice_vectors, v1 = min(row.vectors(), v0 + g.slice_vectors);
     if (me == 0) l.count = l.eight_count = 0;
-    Sum st{0.0, -__builtin_inff()};
+    Running own;
     int batches = 0;
     // Batches of whole pieces are on their way while the one before is added up.
     const int64_t whole = min(v1, g.V / E);
@@ -197,28 +234,27 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
             for (int i = 0; i < kParts; ++i) part[i] = fmaxf(part[i], place[i]);
         }
         place = f32x4{part[0], part[1], part[2], part[3]};
-        if (most > st.m) raise(st, most);
-        // Differences are at least -600, where the exponential counts for nothing.  Far from 0 they are taken in fp32, where they are
-        // exact or beyond that; else in 64 bits.
-        const bool none = st.m == -__builtin_inff(), far = !(fabsf(st.m) <= 0x1p20f);
-        const double m = none || far ? 0.0 : (double)st.m;
-        if (far && !none) {
+        if (most > own.m) own.raise(most);
+        // At least -600 from the largest, where the exponential counts for nothing.
+        const bool none = own.m == -__builtin_inff();
+        if (own.far) {
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) x[i] -= st.m;
+            for (int i = 0; i < kBatch; ++i) x[i] -= own.m;
         }
-        const float least = none || far ? -600.f : st.m - 600.f;
+        const float least = none || own.far ? -600.f : own.m - 600.f;
         double s0 = 0.0, s1 = 0.0;
 #pragma unroll
         for (int j = 0; j < kParts; ++j) {
             if (b + j * V8 * THREADS >= v1) break;      // no thread has more
 #pragma unroll
             for (int i = 8 * j; i < 8 * j + 8; i += 2) {
-                s0 += exp2_wide(((double)__builtin_elementwise_maximum(x[i], least) - m) * kLog2e);
-                s1 += exp2_wide(((double)__builtin_elementwise_maximum(x[i + 1], least) - m) * kLog2e);
+                s0 += exp_over(__builtin_elementwise_maximum(x[i], least), own.magic);
+                s1 += exp_over(__builtin_elementwise_maximum(x[i + 1], least), own.magic);
             }
         }
-        st.s += s0 + s1;
+        own.s += s0 + s1;
     }
+    Sum st = own.sum();
     G::sync();
     const int with_words = __popcll(__ballot(st.m > -__builtin_inff()));
     if (lane == 0) l.wave_count[wave] = with_words;

@@ -146,7 +146,17 @@ def test_far_logits():
     for offset in (1e3, -1e5, 3e6, -2e7, 1e30):
         logits, scores = draw(2, 4, 3000, torch.float32)
         check(logits + offset, scores)
+        # behind words that cannot be, as many as a thread looks at together
+        logits[:, :9000 if logits.shape[1] > 9000 else 2500] = -math.inf
+        check(logits + offset, scores)
     check(draw(2, 3, 4000, torch.float32, spread=2000.0)[0], torch.zeros(2, 3, device=DEV))
+    for offset in (-1e5, -700.0, 700.0, 1e5, -1e9, 1e9):
+        logits, scores = draw(1, 3, 30000, torch.float32)
+        logits += offset
+        logits[:, :17000] = -math.inf
+        logits[1, 17000:20000] -= 1e4           # then far ones, then nearer ones
+        logits[2, 17000:20000] = -3e38
+        check(logits, scores)
 
 
 def test_flat_and_clustered_rows():
