@@ -3,8 +3,8 @@
     embedding -> LSTM whose gate matrix is balanced-sparse -> expert layer in 4 bits (added to its input)
               -> output product in 4 bits -> log probabilities, entropies and the most likely words
 
-``score`` goes over a whole text, ``generate`` makes one word after the other, ``fit_bias`` adapts the output bias to a text
-with the gradient of its log probabilities.  Weights are random: the example shows the calls, not a trained model.
+``score`` goes over a whole text, ``generate`` makes one word after the other, ``search`` keeps several hypotheses and multiplies
+them by the output matrix in MX 4-bit, ``fit_bias`` adapts the output bias to a text with the gradient of its log probabilities.  Weights are random: the example shows the calls, not a trained model.
 
     python examples/word_model.py [--words 10000] [--units 1500]
 """
@@ -41,6 +41,7 @@ class WordModel:
         self.w2 = bs.bs_q4_pack(normal(experts, H, H, scale=H**-0.5), group)
         self.out = bs.bs_q4_pack(normal(words, H, scale=4 * H**-0.5), group)
         self.out_bias = torch.zeros(words, device="cuda")
+        self.out_mx = None      # the output matrix for `search`, made when it is first asked for
 
     def start(self):
         """State of an empty text: hidden and cell state."""
@@ -74,6 +75,31 @@ class WordModel:
                 logits, state = self.logits(words[-1], state)
         return torch.cat(words), torch.cat(logprobs)
 
+    def search(self, tokens, n, beams=4, end=-1):
+        """The `beams` best continuations of a text by n words that a beam search finds, best first: words int32 [beams, n] and log
+        probabilities [beams].  `end`: the word behind which a continuation stays as it is."""
+        if self.out_mx is None:      # the same matrix, as far as the format holds it
+            self.out_mx = bs.bs_mx4_pack(bs.bs_q4_unpack(*self.out, self.units, self.group))
+        _, (h, c) = self.logits(tokens[:-1], self.start()) if tokens.numel() > 1 else (None, self.start())
+        h, c = h.expand(beams, -1).contiguous(), c.expand(beams, -1).contiguous()
+        words = tokens[-1:].expand(beams)
+        text = torch.zeros((beams, n), dtype=torch.int32, device="cuda")
+        scores = torch.full((1, beams), -float("inf"), device="cuda")
+        scores[0, 0] = 0.0      # one hypothesis to begin with
+        finished = torch.zeros((1, beams), dtype=torch.bool, device="cuda")
+        for i in range(n):
+            x, after = self.embedding[words], torch.empty_like(h)
+            for j in range(beams):
+                bs.bs_lstm_step(*self.gates, self.bank, x[j], h[j], self.gate_bias, c[j], c_out=c[j], h_out=after[j])
+            h = after
+            y, _, _ = bs.bs_q4_moe(h, self.router, *self.w1, *self.w2, self.group, self.top_k)
+            logits = bs.bs_mx4_gemm(*self.out_mx, h + y, bias=self.out_bias)
+            scores, words, parents, finished = bs.bs_beam_step(logits, scores, finished, end=end)
+            bs.bs_beam_reorder([h, c, text], parents)
+            text[:, i] = words[0]
+            words = words[0].long()
+        return text, scores[0]
+
     def fit_bias(self, tokens, steps=5, rate=0.5, entropy_weight=0.0):
         """Gradient steps on the output bias: up the mean log probability of a text (and `entropy_weight` times the entropy).
         The mean before each step."""
@@ -106,6 +132,13 @@ def main():
     words, logprobs = model.generate(text[:20], 100)
     torch.cuda.synchronize()
     print(f"100 words behind 20: {(time.perf_counter() - began) * 1e4:.0f} us a word, the first ones {words[:8].tolist()}")
+    model.search(text[:20], 5)
+    torch.cuda.synchronize()
+    began = time.perf_counter()
+    found, scores = model.search(text[:20], 50, beams=8)
+    torch.cuda.synchronize()
+    print(f"50 words, 8 hypotheses: {(time.perf_counter() - began) * 2e4:.0f} us a word, log probability {float(scores[0]):.2f}, "
+          f"{float(logprobs[:50].sum()):.2f} one word after the other")
     means = model.fit_bias(text, rate=20.0)
     print("log probability while the output bias is fitted: " + " ".join(f"{m:.3f}" for m in means.tolist()))
 
