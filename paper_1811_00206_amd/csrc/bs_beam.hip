@@ -9,6 +9,8 @@
 // logits have the same sums to the last bit, and tie.  A row's n largest are found as bs_logprobs finds them.
 // A second kernel joins the rows of a sequence: a candidate's total is scores + ((x - m) - log s); of the lists that are full each
 // answers for its share of the n, the least of those totals is a bound, and what reaches it is ordered by counting what comes before.
+#include <type_traits>
+
 #include "bs_logits.h"
 
 namespace bs {
@@ -169,6 +171,22 @@ struct Args {
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
+// The k-th largest of the lanes' values, numbers of type XT, of which k are more than -inf.  Bit by bit, and the scalar unit
+// counts: comparing every lane with all is 320 vector instructions (256 x 16 rows of 32003 109.5 us, this way 106; of 2000 23.7 and 20.8).
+template <typename XT>
+__device__ __forceinline__ float kth_of_lanes(float v, int k) {
+    if (k == 1) return max_of_wave(v);
+    constexpr int low = std::is_same_v<XT, F32> ? 0 : std::is_same_v<XT, F16> ? 13 : 16;      // bits that the type leaves empty
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v), key = bits ^ ((uint32_t)((int)bits >> 31) | 0x80000000u);
+    uint32_t least = 0;
+#pragma unroll
+    for (int bit = 31; bit >= low; --bit) {
+        const uint32_t more = least | 1u << bit;
+        if (__popcll(__ballot(key >= more)) >= k) least = more;
+    }
+    return __builtin_bit_cast(float, least >> 31 ? least ^ 0x80000000u : ~(least | ((1u << low) - 1)));
+}
+
 // THREADS: a workgroup for a row (or a slice of one), or a wavefront
 template <typename XT, int THREADS>
 __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
@@ -263,7 +281,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
     int here = l.wave_count[wave], lanes = 0;
     for (int w = 0; w < G::kWaves; ++w) lanes += l.wave_count[w];
     const int k = lanes < g.n ? -1 : (g.n * here + lanes - 1) / lanes;
-    const float bound_here = k < 0 ? -__builtin_inff() : k ? kth_largest(st.m, k) : __builtin_inff();
+    const float bound_here = k < 0 ? -__builtin_inff() : k ? kth_of_lanes<XT>(st.m, k) : __builtin_inff();
     if (lane == 0) l.bound[wave] = bound_here;
     st = join_wave(st);
     if (lane == 0) sums[wave] = st;
