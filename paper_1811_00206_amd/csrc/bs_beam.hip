@@ -140,6 +140,20 @@ struct BeamRow {
             else out[i] = XT::load((uint16_t)(word_of(a, i >> 1) >> (16 * (i & 1))));
         }
     }
+    static __device__ __forceinline__ uint4 none() {      // -inf
+        const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same_v<XT, F16> ? 0xfc00fc00u : 0xff80ff80u;
+        return uint4{w, w, w, w};
+    }
+    __device__ __forceinline__ uint4 edge(int64_t v) const {      // a piece that is not whole
+        T out[E];
+        uint4 a = none();
+        __builtin_memcpy(out, &a, 16);
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (v * E + i < V) out[i] = p[v * E + i];
+        __builtin_memcpy(&a, out, 16);
+        return a;
+    }
     __device__ __forceinline__ void load(int64_t v, float* out) const {
         const int64_t e = v * E;
         if (e + E <= V) {
@@ -208,36 +222,36 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
     if (me == 0) l.count = l.eight_count = 0;
     Running own;
     int batches = 0;
-    // Batches of whole pieces are on their way while the one before is added up.
-    const int64_t whole = min(v1, g.V / E);
-    uint4 next[U];
-    const auto load = [&](int64_t b) {
+    // A batch's whole pieces are on their way while the one before is added up; those behind the last of them are that one again, and what
+    // is no whole piece comes in first.
+    const int first = (int)v0, behind = (int)v1, ragged = (int)(g.V / E), whole = min(behind, ragged);
+    uint4 next[U] = {}, edge = R::none();
+    const auto load = [&](int b) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) __builtin_memcpy(&next[u], row.p + (b + u * THREADS + me) * E, 16);
+        for (int u = 0; u < U; ++u)
+            if (b + u * THREADS < whole) __builtin_memcpy(&next[u], row.p + (int64_t)min(b + u * THREADS + me, whole - 1) * E, 16);
     };
-    if (v0 + THREADS * U <= whole) load(v0);
-    for (int64_t b = v0; b < v1; b += THREADS * U, ++batches) {
+    load(first);
+    if (ragged < behind && me == (ragged - first) % THREADS) edge = row.edge(ragged);
+    for (int b = first; b < behind; b += THREADS * U, ++batches) {
         float x[kBatch];
-        if (b + THREADS * U <= whole) {
-            uint4 now[U];
+        uint4 now[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            now[u] = next[u];
+            asm volatile("" : "+v"(now[u].x), "+v"(now[u].y), "+v"(now[u].z), "+v"(now[u].w));
+        }
+        load(b + THREADS * U);
+        if (b + THREADS * U > whole) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                now[u] = next[u];
-                asm volatile("" : "+v"(now[u].x), "+v"(now[u].y), "+v"(now[u].z), "+v"(now[u].w));
-            }
-            if (b + 2 * THREADS * U <= whole) load(b + THREADS * U);
-#pragma unroll
-            for (int u = 0; u < U; ++u) R::values(now[u], x + u * E);
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t v = b + u * THREADS + me;
-                if (v < v1) row.load(v, x + u * E);
-                else
-#pragma unroll
-                    for (int i = 0; i < E; ++i) x[u * E + i] = -__builtin_inff();
+                const int v = b + u * THREADS + me;
+                if (v >= whole) now[u] = R::none();
+                if (v == ragged) now[u] = edge;
             }
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) R::values(now[u], x + u * E);
         float part[kParts], most = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
@@ -263,7 +277,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(Args g) {
         double s0 = 0.0, s1 = 0.0;
 #pragma unroll
         for (int j = 0; j < kParts; ++j) {
-            if (b + j * V8 * THREADS >= v1) break;      // no thread has more
+            if (b + j * V8 * THREADS >= behind) break;      // no thread has more
 #pragma unroll
             for (int i = 8 * j; i < 8 * j + 8; i += 2) {
                 s0 += exp_over(__builtin_elementwise_maximum(x[i], least), own.magic);
