@@ -2,7 +2,7 @@
 //
 // Few rows: a wavefront has 16 rows of W, which go from memory to the matrix unit, and reads x beside them.  Many: tiles that pass
 // through LDS (bs_mx4_tiles.h), with K split between workgroups where there are few of them; a second kernel then adds their sums up,
-// in order.  Dense x is rounded by a kernel of its own first, or for one or two rows by every workgroup for itself.
+// in order.  Dense x is rounded by a kernel of its own first, or, where that is little work, by every workgroup for itself.
 #include <type_traits>
 
 #include "bs_mx4_tiles.h"
@@ -15,6 +15,7 @@ struct Args {
     const void* x;              // dense
     int64_t ldx;
     int64_t M, K, N;
+    uint32_t pieces_magic;      // division by 16 chunks
     int chunks, ways, tiles;    // chunks of 128 columns; wavefronts that share K, and groups of them
     const float* bias;
     void* y;
@@ -70,22 +71,31 @@ __global__ __launch_bounds__(R * NT == 1 ? 1024 : 512) void mx4_rows_kernel(Args
     if constexpr (FUSED) {
         const int pitch = (chunks + 3) & ~3;
         uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + g.N * 64 * chunks);
-        const int pieces = 16 * chunks;      // of a row, 8 elements each
-        for (int n = 0; n < (int)g.N; ++n)
-            for (int p0 = 0; p0 < pieces; p0 += blockDim.x) {
-                const int p = p0 + threadIdx.x;
-                const int64_t k = (int64_t)p * 8;
-                float v[8] = {};
-                if (k < g.K) load8<XT>(static_cast<const typename XT::type*>(g.x) + n * g.ldx, k, g.K, v);
-                const uint32_t e = mx4_scale(max_of_4(mx4_most(v)));
-                const uint32_t word = mx4_codes(v, mx4_factor(e));
-                uint32_t bytes = e << (p / 4 % 4 * 8);
-                bytes |= (uint32_t)dpp_move_i<0x141>((int)bytes);
-                bytes |= (uint32_t)dpp_move_i<0x140>((int)bytes);
-                if (p >= pieces) continue;
-                reinterpret_cast<uint32_t*>(lds)[n * pieces + p] = word;
-                if (p % 16 == 0) scales[n * pitch + p / 16] = bytes;
+        // all rows' pieces of 8 elements, one after the other; the next of a thread is on its way while one is rounded
+        const uint32_t pieces = 16 * chunks, all = (uint32_t)g.N * pieces;
+        const auto bring = [&](uint32_t e, float (&v)[8]) {
+            const uint32_t n = div_magic_any(e, pieces, g.pieces_magic), k = (e - n * pieces) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            if (e < all && k < g.K) load8<XT>(static_cast<const typename XT::type*>(g.x) + n * g.ldx, (int64_t)k, g.K, v);
+        };
+        float v[8], after[8];
+        bring(threadIdx.x, v);
+        for (uint32_t e = threadIdx.x; e - threadIdx.x < all; e += blockDim.x) {
+            bring(e + blockDim.x, after);
+            const uint32_t s = mx4_scale(max_of_4(mx4_most(v)));
+            const uint32_t word = mx4_codes(v, mx4_factor(s));
+            uint32_t bytes = s << (e / 4 % 4 * 8);
+            bytes |= (uint32_t)dpp_move_i<0x141>((int)bytes);
+            bytes |= (uint32_t)dpp_move_i<0x140>((int)bytes);
+            if (e < all) {
+                const uint32_t n = div_magic_any(e, pieces, g.pieces_magic);
+                reinterpret_cast<uint32_t*>(lds)[e] = word;
+                if (e % 16 == 0) scales[n * pitch + (e - n * pieces) / 16] = bytes;
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = after[i];
+        }
         const int row = min(r, (int)g.N - 1);
         x[0] = lds + row * 64 * chunks + 16 * kb;
         xs[0] = scales + row * pitch;
@@ -274,6 +284,15 @@ double rows_us(const Plan& p, int64_t M, int chunks, int steps) {
     return 2.5 + (work > least ? work : least);
 }
 
+// Whether every workgroup rounds x for itself, which spares a kernel of 3 us: a piece of a thread takes .8 us, in every round of
+// workgroups (10000 x 1500 for 4 rows, 3 pieces, 6.1 us instead of 8.2, for 8 rows, 6 pieces, 8.4 and 8.5, for 16 13.0 and 8.1;
+// 32306 x 651 for 12 rows 6.9 and 9.0, 200000 x 500 for 5 17.3 and 16.6).
+bool fused(const Plan& p, int64_t M, int64_t K, int64_t N) {
+    if (p.tile || p.r * p.nt > 1 || N * 68 * (mx4_chunks(K) + 3) > kFusedBytes) return false;
+    const int64_t threads = 64 * p.ways * p.groups, pieces = (N * 16 * mx4_chunks(K) + threads - 1) / threads;
+    return N <= kFusedRows || (pieces <= 5 && pieces * ((M + 16 * p.groups - 1) / (16 * p.groups)) <= 3200);
+}
+
 Plan plan_for(int64_t M, int64_t K, int64_t N) {
     const int chunks = (int)mx4_chunks(K), steps = (chunks + kStep - 1) / kStep, stages = (chunks + 1) / 2;
     const int64_t tiles = (M + 15) / 16;
@@ -291,7 +310,7 @@ Plan plan_for(int64_t M, int64_t K, int64_t N) {
         while (p.ways < most && tiles * p.ways < 2048 * p.r && p.ways < steps) p.ways *= 2;
         p.groups = p.ways <= 2 ? 4 : p.r == 2 ? 2 : 1;
         least = rows_us(p, M, chunks, steps);
-        if (N <= kFusedRows) return p;
+        if (N <= kFusedRows || fused(p, M, K, N)) return p;
     }
     for (const Tile& t : kTiles)
         for (int split = 1; split <= 16 && split <= stages; ++split) {
@@ -309,8 +328,6 @@ Plan plan_for(int64_t M, int64_t K, int64_t N) {
 }
 
 size_t packed_bytes(int64_t K, int64_t N) { return (size_t)(N * (mx4_row_bytes(K) + mx4_scale_pitch(K)) + 15) / 16 * 16; }
-bool fused(int64_t K, int64_t N) { return N <= kFusedRows && N * 68 * (mx4_chunks(K) + 3) <= kFusedBytes; }
-
 template <typename XT>
 int launch(Args g, const Plan& p, float* sums, hipStream_t st) {
     if (p.tile) {
@@ -343,7 +360,7 @@ void mx4_gemm_plan_describe(int64_t M, int64_t K, int64_t N, int64_t* out, int n
     } else {
         v[5] = p.r, v[6] = p.nt, v[7] = p.ways, v[8] = p.groups;
         const int64_t rows = 16 * p.r * p.groups, sums = (int64_t)p.ways * p.groups * p.r * p.nt * 1024,
-                      x = fused(K, N) ? N * (64 * mx4_chunks(K) + 4 * ((mx4_chunks(K) + 3) & ~(int64_t)3)) : 0;
+                      x = fused(p, M, K, N) ? N * (64 * mx4_chunks(K) + 4 * ((mx4_chunks(K) + 3) & ~(int64_t)3)) : 0;
         v[9] = (M + rows - 1) / rows;
         v[10] = sums > x ? sums : x;
     }
@@ -351,7 +368,7 @@ void mx4_gemm_plan_describe(int64_t M, int64_t K, int64_t N, int64_t* out, int n
 }
 
 static size_t workspace_of(const Plan& p, bool packed, int64_t M, int64_t K, int64_t N) {
-    return (packed || fused(K, N) ? 0 : packed_bytes(K, N)) + (p.split > 1 ? (size_t)p.split * M * N * 4 : 0);
+    return (packed || fused(p, M, K, N) ? 0 : packed_bytes(K, N)) + (p.split > 1 ? (size_t)p.split * M * N * 4 : 0);
 }
 size_t mx4_gemm_workspace_bytes(bool packed, int, int64_t M, int64_t K, int64_t N) {
     return workspace_of(plan_for(M, K, N), packed, M, K, N);
@@ -364,7 +381,7 @@ int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int6
     const size_t need = workspace_of(p, !x, M, K, N);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))) return BS_ERR_WORKSPACE;
     uint8_t* at = static_cast<uint8_t*>(workspace);
-    const bool dense = x && fused(K, N);
+    const bool dense = x && fused(p, M, K, N);
     if (x && !dense) {
         uint8_t* const s = at + N * mx4_row_bytes(K);
         const int rc = launch_mx4_pack(x, dtype, N, K, ldx, at, s, st);
@@ -374,7 +391,7 @@ int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int6
         at += packed_bytes(K, N);
     }
     float* const sums = reinterpret_cast<float*>(at);
-    const Args g{codes, scales, x_codes, x_scales, dense ? x : nullptr, ldx, M, K, N, (int)mx4_chunks(K), 1, 1, bias, y, ldy};
+    const Args g{codes, scales, x_codes, x_scales, dense ? x : nullptr, ldx, M, K, N, magic_u32((uint32_t)(16 * mx4_chunks(K))), (int)mx4_chunks(K), 1, 1, bias, y, ldy};
     switch (dtype) {
         case BS_F32: return launch<F32>(g, p, sums, st);
         case BS_F16: return launch<F16>(g, p, sums, st);

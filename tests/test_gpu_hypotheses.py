@@ -67,14 +67,14 @@ def test_a_search(dtype, beams, sequences):
 
 def _inputs(dtype=torch.float32, seed=0):
     g = torch.Generator().manual_seed(seed)
-    return {"x": torch.randn(12, 200, generator=g).to(dtype).cuda(), "scores": torch.sort(torch.randn(3, 4, generator=g), -1, descending=True).values.cuda(),
+    return {"x": torch.randn(12, 1500, generator=g).to(dtype).cuda(), "scores": torch.sort(torch.randn(3, 4, generator=g), -1, descending=True).values.cuda(),
             "state": torch.randn(12, 333, generator=g).cuda(), "text": torch.randint(0, 99, (3, 4, 9), generator=g, dtype=torch.int32).cuda()}
 
 
 def test_captured_steps_replay():
     """Two graphs that share a workspace, replayed in turns with eager work between them: every replay is the eager result."""
-    W, bias = bs.bs_mx4_pack(torch.randn(5000, 200, device="cuda")), torch.randn(5000, device="cuda")
-    need = max(bs.bs_mx4_gemm_workspace_bytes(bs.BS_F32, 5000, 200, 12), bs.bs_beam_step_workspace_bytes(bs.BS_F32, 3, 4, 5000, 4))
+    W, bias = bs.bs_mx4_pack(torch.randn(5000, 1500, device="cuda")), torch.randn(5000, device="cuda")
+    need = max(bs.bs_mx4_gemm_workspace_bytes(bs.BS_F32, 5000, 1500, 12), bs.bs_beam_step_workspace_bytes(bs.BS_F32, 3, 4, 5000, 4))
     workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
 
     def run(i):

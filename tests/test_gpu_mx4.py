@@ -209,6 +209,20 @@ def test_every_kind_of_product(shape, kind):
     p = bs.bs_mx4_gemm_plan(M, K, N)
     found = (p["tile_rows"], p["tile_columns"], p["buffers"], p["split"] > 1) if p["tile_rows"] else (p["r"], p["nt"], p["ways"], p["groups"])
     assert found == kind
+    _every_type(M, K, N)
+
+
+# rows of x that every workgroup rounds for itself, 1 to 5 pieces of each thread, and on the other side of that rule
+@pytest.mark.parametrize("shape,alone", [((219, 203, 11), True), ((40, 1, 16), True), ((32306, 651, 12), True), ((10000, 1500, 4), True), ((301, 700, 16), True),
+                                         ((1100, 3001, 6), True), ((1100, 3001, 7), False), ((77, 8191, 4), True), ((10000, 1500, 8), False), ((200001, 500, 5), False)])
+def test_rows_rounded_on_the_way(shape, alone):
+    M, K, N = shape
+    p = bs.bs_mx4_gemm_plan(M, K, N)
+    assert (p["tile_rows"] == 0 and bs.bs_mx4_gemm_workspace_bytes(bs.BS_F32, M, K, N) == 0) == alone
+    _every_type(M, K, N)
+
+
+def _every_type(M, K, N):
     g = torch.Generator().manual_seed(M + K + N)
     x, W = torch.randn(N, K, generator=g).to(DEV), bs.bs_mx4_pack(torch.randn(M, K, generator=g).to(DEV))
     bias = torch.randn(M, generator=g).to(DEV)

@@ -100,7 +100,7 @@ def test_bad_arguments_are_refused_before_launch():
     refused(lib.bs_mx4_gemm, (p, p, 40, 64, p, 0, 1, 64, null, p, 40, null, 0, null),
             (*((1, {at: null}) for at in (0, 1, 4, 9)), (2, {2: 0}), (2, {3: 0}), (2, {6: 0}), (2, {7: 63}), (2, {10: 39}), (3, {5: 3}), (3, {6: big}),
              (3, {2: 1 << 20, 6: (1 << 16) + 1, 10: 1 << 20}), (4, {0: four}), (4, {1: two}), (4, {4: two}), (4, {8: two}), (4, {9: two}), (4, {9: odd, 5: 1}),
-             (6, {6: 9}), (6, {6: 9, 11: p, 12: 9 * 68 - 1}), (6, {6: 9, 11: four, 12: 1 << 30})))
+             (6, {6: 60}), (6, {6: 60, 11: p, 12: 60 * 68 - 1}), (6, {6: 60, 11: four, 12: 1 << 30})))
     refused(lib.bs_mx4_gemm_packed, (p, p, 40, 64, p, p, 9, null, p, 0, 40, null, 0, null),
             (*((1, {at: null}) for at in (0, 1, 4, 5, 8)), (2, {6: 0}), (2, {10: 39}), (2, {3: 0}), (3, {9: 3}), (3, {6: big}), (3, {2: big, 10: big}),
              (4, {4: four}), (4, {5: two}), (4, {7: odd}), (4, {8: two}), (6, {2: 4096, 10: 4096, 3: 25088, 6: 77}),
@@ -176,10 +176,10 @@ CALLS = """
         kept.append(host)
         storage = torch._C._construct_storage_from_data_pointer(host.data_ptr(), torch.device("cuda", 0), host.numel() * host.element_size())
         return torch._C._construct_CUDA_Tensor_From_Storage_And_Metadata(dict(size=size, stride=stride, dtype=dtype, storage_offset=3), storage)
-    def calls(dtype=torch.float32):
+    def calls(dtype=torch.float32, rows=13):
         '''name -> call; all but the last two allocate what they return'''
         codes, scales, x_codes, x_scales = gpu(40, 64, dtype=u8), gpu(40, 4, dtype=u8), gpu(13, 64, dtype=u8), gpu(13, 4, dtype=u8)
-        x, x1, bias, logits, scores = gpu(13, 100, dtype=dtype), gpu(100, dtype=dtype), gpu(40), gpu(6, 500, dtype=dtype), gpu(2, 3)
+        x, x1, bias, logits, scores = gpu(rows, 100, dtype=dtype), gpu(100, dtype=dtype), gpu(40), gpu(6, 500, dtype=dtype), gpu(2, 3)
         W, y, states, parents = gpu(2, 5, 130, dtype=dtype), gpu(40, dtype=dtype), [gpu(6, 7, dtype=dtype), gpu(2, 3, 5, dtype=torch.int32)], gpu(2, 3, dtype=torch.int32)
         done = gpu(2, 3, dtype=torch.bool)
         return {"bs_mx4_pack": lambda **k: bs.bs_mx4_pack(W),
@@ -345,7 +345,7 @@ def test_a_workspace_in_host_memory_is_refused(stand_in):
     _run(stand_in, """
         ctypes.c_int.in_dll(stand_in, "host_memory").value = 1
         ctypes.c_int.in_dll(stand_in, "status").value = 0
-        c = calls()
+        c = calls(rows=60)      # more than every workgroup rounds for itself
         for name in ("bs_mx4_gemm", "bs_beam_step"):
             for host in (torch.empty(1 << 20, dtype=u8), bytearray(1 << 20)):
                 attempts.value = 0
