@@ -62,6 +62,18 @@ __global__ __launch_bounds__(R * NT == 1 ? 1024 : 512) void mx4_rows_kernel(Args
             p.s[i] = uint4{v[0], v[1], v[2], v[3]};
         }
     };
+    // FUSED: all rows' pieces of 8 elements, one after the other; the next of a thread is on its way while one is rounded
+    const uint32_t pieces = 16 * chunks, all = (uint32_t)g.N * pieces;
+    const auto row_of = [&](uint32_t e) { return g.N == 1 ? 0 : div_magic_any(e, pieces, g.pieces_magic); };
+    const auto bring = [&](uint32_t e, float (&v)[8]) {
+        const uint32_t n = row_of(e), k = (e - n * pieces) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        if (e < all && k < g.K) load8<XT>(static_cast<const typename XT::type*>(g.x) + n * g.ldx, (int64_t)k, g.K, v);
+    };
+    // A thread's first piece of x goes before those of W: loads come back in order.
+    float u[8], v[8];
+    if constexpr (FUSED) bring(threadIdx.x, u);
     // Two pieces are on their way while one is multiplied.  (Where there is no whole step nothing is loaded here.)
     Piece<R> a, b;
     if (way < whole) load(a, way);
@@ -71,30 +83,23 @@ __global__ __launch_bounds__(R * NT == 1 ? 1024 : 512) void mx4_rows_kernel(Args
     if constexpr (FUSED) {
         const int pitch = (chunks + 3) & ~3;
         uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + g.N * 64 * chunks);
-        // all rows' pieces of 8 elements, one after the other; the next of a thread is on its way while one is rounded
-        const uint32_t pieces = 16 * chunks, all = (uint32_t)g.N * pieces;
-        const auto bring = [&](uint32_t e, float (&v)[8]) {
-            const uint32_t n = div_magic_any(e, pieces, g.pieces_magic), k = (e - n * pieces) * 8;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-            if (e < all && k < g.K) load8<XT>(static_cast<const typename XT::type*>(g.x) + n * g.ldx, (int64_t)k, g.K, v);
-        };
-        float v[8], after[8];
-        bring(threadIdx.x, v);
-        for (uint32_t e = threadIdx.x; e - threadIdx.x < all; e += blockDim.x) {
-            bring(e + blockDim.x, after);
+        const auto round = [&](uint32_t e, const float (&v)[8]) {
             const uint32_t s = mx4_scale(max_of_4(mx4_most(v)));
             const uint32_t word = mx4_codes(v, mx4_factor(s));
             uint32_t bytes = s << (e / 4 % 4 * 8);
             bytes |= (uint32_t)dpp_move_i<0x141>((int)bytes);
             bytes |= (uint32_t)dpp_move_i<0x140>((int)bytes);
-            if (e < all) {
-                const uint32_t n = div_magic_any(e, pieces, g.pieces_magic);
-                reinterpret_cast<uint32_t*>(lds)[e] = word;
-                if (e % 16 == 0) scales[n * pitch + (e - n * pieces) / 16] = bytes;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = after[i];
+            if (e >= all) return;
+            const uint32_t n = row_of(e);
+            reinterpret_cast<uint32_t*>(lds)[e] = word;
+            if (e % 16 == 0) scales[n * pitch + (e - n * pieces) / 16] = bytes;
+        };
+        for (uint32_t e = 0; e < all; e += 2 * blockDim.x) {
+            const uint32_t next = e + blockDim.x;
+            if (next < all) bring(next + threadIdx.x, v);
+            round(e + threadIdx.x, u);
+            if (next + blockDim.x < all) bring(next + blockDim.x + threadIdx.x, u);
+            if (next < all) round(next + threadIdx.x, v);
         }
         const int row = min(r, (int)g.N - 1);
         x[0] = lds + row * 64 * chunks + 16 * kb;
