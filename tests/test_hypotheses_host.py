@@ -404,3 +404,10 @@ def test_tiles_wait_for_their_stages(texts):
         assert len(inside) == 1, (name, inside)
         found += 1
     assert found == 4 * 6      # three types and the sums of shares of K
+
+
+def test_the_package_offers_them():
+    import paper_1811_00206_amd as package
+    for name in ("bs_mx4_codes_bytes", "bs_mx4_scales_bytes", "bs_mx4_pack", "bs_mx4_unpack", "bs_mx4_gemm_workspace_bytes", "bs_mx4_gemm",
+                 "bs_mx4_gemm_packed_workspace_bytes", "bs_mx4_gemm_packed", "bs_mx4_gemm_plan", "bs_beam_step_workspace_bytes", "bs_beam_step", "bs_beam_reorder"):
+        assert name in package.__all__ and callable(getattr(package, name))
