@@ -3,6 +3,7 @@
 // Few rows: a wavefront has 16 rows of W, which go from memory to the matrix unit, and reads x beside them.  Many: tiles that pass
 // through LDS (bs_mx4_tiles.h), with K split between workgroups where there are few of them; a second kernel then adds their sums up,
 // in order.  Dense x is rounded by a kernel of its own first, or, where that is little work, by every workgroup for itself.
+// Bound: HBM for few rows (16384 x 8192 for one row 14.2 us, 71 MB at 5 TB/s; 10000 x 1500 5.0, latency), the matrix unit for many.
 #include <type_traits>
 
 #include "bs_mx4_tiles.h"

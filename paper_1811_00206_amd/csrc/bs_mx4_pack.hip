@@ -2,6 +2,7 @@
 //
 // A lane holds 8 consecutive elements of a row and four lanes a block, so that the largest magnitude is two lane exchanges away; 16
 // lanes gather the four scale bytes of a word.  Magnitudes are compared as whole numbers, infinities and NaN the largest.
+// 6000 x 3000 in fp32 13.5 us and back 16.3, 16384 x 8192 in bfloat16 66 to 76 and 57 to 61 (a copy of as many bytes 16.0 and 66).
 #include "bs_mx4.h"
 
 namespace bs {

@@ -7,6 +7,10 @@
 // long for a row's eight bytes as for a whole line, and those of every stage were half of all requests.  A wavefront's operands of the
 // next step are read while this one's are multiplied, over the end of a stage too: its last step first waits for the next stage, meets
 // the others, and sends for the one after it.
+//
+// 4096 rows by 16384 x 8192 take 255 us at 256 x 256, 4.3 PFLOP/s (300 where calls follow one another without a pause), bound by the power that
+// the matrix unit takes: with nothing but its instructions the loop takes 222 to 235 on the same data, 251 without loads, 172 without the
+// instructions.  256 rows by 32003 x 1500 take 15 to 17 us, beginning and end of a tile of six stages as much as the stages.
 #pragma once
 
 #include "bs_mx4.h"
