@@ -451,6 +451,7 @@ int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_
  * y[n][r] = sum_k W[r][k] * X[n][k] (+ bias[r]) for N rows of activations, where X is x as bs_mx4_pack would round it: the matrix
  * unit multiplies 4-bit numbers on both sides.
  * x     DEVICE in   N rows of K of type dtype, ldx >= K apart       y  DEVICE out  N rows of M, same type, ldy >= M apart
+ *                                                                               (rows that share bytes with x's: BS_ERR_UNSUPPORTED)
  * bias  DEVICE in   M fp32, may be NULL
  * bs_mx4_gemm_packed takes x packed already (an activation that several matrices multiply); dtype is y's type there.
  * Products are exact, sums fp32.  The order of the additions depends on M, K and N alone, and is the same in both calls.

@@ -963,7 +963,7 @@ def _product(out, shape, like, dtype):
 def bs_mx4_gemm(codes, scales, x, bias=None, out=None, workspace=None):
     """W . x (+ bias) for an MX matrix [M, K] and x [K] -> y [M], or one row per vector, x [N, K] -> y [N, M], of x's type
     (float32, float16, bfloat16); x is rounded to MX 4-bit on the way, as bs_mx4_pack does.  bias: float32 [M].  Rows of x and `out` may be
-    slices of wider ones.  `workspace`: at least bs_mx4_gemm_workspace_bytes(...) bytes, or one from torch's allocator."""
+    slices of wider ones, but not share memory.  `workspace`: at least bs_mx4_gemm_workspace_bytes(...) bytes, or one from torch's allocator."""
     y = (_native or _calls()).mx4_gemm(codes, scales, x, bias, out, workspace)
     if y is not None:
         return y

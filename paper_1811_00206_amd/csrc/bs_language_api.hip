@@ -205,6 +205,8 @@ int bs_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t 
     if (!type_ok(dtype) || N > kMost || M * N > kMostOutputs) return BS_ERR_UNSUPPORTED;
     const size_t size = bs::dtype_bytes(dtype);
     if (!aligned(x, size) || !aligned(y, size) || !aligned(bias, 4)) return BS_ERR_ALIGN;
+    if (rows_meet(reinterpret_cast<uintptr_t>(x), ldx * size, reinterpret_cast<uintptr_t>(y), ldy * size, N, K * size, N, M * size))
+        return BS_ERR_UNSUPPORTED;
     return bs::launch_mx4_gemm(codes, scales, M, K, x, ldx, nullptr, nullptr, dtype, N, bias, y, ldy, workspace, workspace_bytes,
                                static_cast<hipStream_t>(stream));
 }

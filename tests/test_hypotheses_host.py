@@ -81,7 +81,7 @@ def test_bad_arguments_are_refused_before_launch():
     lib = b.load_library()
     p, odd, null = (ctypes.c_void_p(a) for a in (4096, 4097, 0))      # never dereferenced: validation fails first
     two = ctypes.c_void_p(4098)                                       # aligned for 16 bits, not for 32
-    four = ctypes.c_void_p(4100)
+    four, far = ctypes.c_void_p(4100), ctypes.c_void_p(1 << 30)
 
     def refused(f, good, changes):
         for status, change in changes:
@@ -97,8 +97,8 @@ def test_bad_arguments_are_refused_before_launch():
     refused(lib.bs_mx4_unpack, (p, p, 4, 64, p, 0, null),
             ((1, {0: null}), (1, {1: null}), (1, {4: null}), (2, {2: -1}), (2, {3: 0}), (3, {5: 7}), (3, {2: big}), (4, {0: four}), (4, {1: two}),
              (4, {4: two}), (4, {4: odd, 5: 2})))
-    refused(lib.bs_mx4_gemm, (p, p, 40, 64, p, 0, 1, 64, null, p, 40, null, 0, null),
-            (*((1, {at: null}) for at in (0, 1, 4, 9)), (2, {2: 0}), (2, {3: 0}), (2, {6: 0}), (2, {7: 63}), (2, {10: 39}), (3, {5: 3}), (3, {6: big}),
+    refused(lib.bs_mx4_gemm, (p, p, 40, 64, p, 0, 1, 64, null, far, 40, null, 0, null),
+            ((3, {9: p}), (3, {9: ctypes.c_void_p(4096 + 63 * 4)}), (3, {9: ctypes.c_void_p(4096 - 39 * 4)}), *((1, {at: null}) for at in (0, 1, 4, 9)), (2, {2: 0}), (2, {3: 0}), (2, {6: 0}), (2, {7: 63}), (2, {10: 39}), (3, {5: 3}), (3, {6: big}),
              (3, {2: 1 << 20, 6: (1 << 16) + 1, 10: 1 << 20}), (4, {0: four}), (4, {1: two}), (4, {4: two}), (4, {8: two}), (4, {9: two}), (4, {9: odd, 5: 1}),
              (6, {6: 60}), (6, {6: 60, 11: p, 12: 60 * 68 - 1}), (6, {6: 60, 11: four, 12: 1 << 30})))
     refused(lib.bs_mx4_gemm_packed, (p, p, 40, 64, p, p, 9, null, p, 0, 40, null, 0, null),
