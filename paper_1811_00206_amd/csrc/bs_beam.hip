@@ -517,10 +517,20 @@ Plan plan_for(int dtype, int64_t rows, int W, int64_t V, int n) {
     const int E = 16 / dtype_bytes(dtype);
     const int64_t vectors = (V + E - 1) / E;
     if (rows >= (V <= 2048 ? 1024 : 2048)) return {true, 1, vectors};
-    // all lists of a sequence are joined by one workgroup, kCandidates at most
-    const int64_t most = kCandidates / ((int64_t)W * n) < kSlices ? kCandidates / ((int64_t)W * n) : kSlices;
-    int64_t slices = 1;
-    while (slices * 2 <= most && rows * slices < 512 && vectors / (slices * 2) >= 2 * kThreads) slices *= 2;
+    // Slices of a row: as many as an estimate of the time, in microseconds, is least for.  A compute unit's workgroups take .04 for each
+    // element of a thread and 1 more, one alone is bound by latency, and the join takes longer from one candidate a thread on.  (Seventeen
+    // sizes that were timed with 1 to 16 slices meet it within 2: 5 x 9 rows of 101681 22.3 us with 16, 16.1 with 5, 28.8 with 1; 123 x 4 of
+    // 72125 38.2 with 2, 34.7 with 1; 38 x 8 of 53421 27.9 with 1, 24.1 with 3, 32.7 with 8.)
+    int slices = 1;
+    double least = 0;
+    for (int s = 1; s <= kSlices && (s == 1 || (W * n * s <= kCandidates && vectors >= s * kThreads)); ++s) {
+        const double each = (double)V / s / kThreads, alone = .05 * each + 1.5, all = (double)((rows * s + 255) / 256) * (.04 * each + 1);
+        const int candidates = W * n * s;
+        const double cost = (all > alone ? all : alone) + .03 * s + (candidates <= kThreads ? 0 : 1 + candidates / 600. + (candidates <= 4 * kThreads ? 0 : 3));
+        if (s > 1 && cost >= least) continue;
+        least = cost;
+        slices = s;
+    }
     Plan p{false, 1, (vectors + slices - 1) / slices};
     p.slices = (int)((vectors + p.slice_vectors - 1) / p.slice_vectors);
     return p;

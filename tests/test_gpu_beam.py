@@ -91,6 +91,23 @@ def test_long_rows(dtype, W, V):
     check(*draw(2, W, V, dtype), n=64)
 
 
+@pytest.mark.parametrize("dtype,V,slices", [(0, 628, 1), (0, 2140, 2), (2, 6139, 3), (0, 4213, 4), (0, 5510, 5), (0, 6235, 6), (1, 14997, 7), (0, 9186, 8), (0, 11601, 9),
+                                            (0, 14096, 10), (0, 17116, 11), (0, 20518, 12), (0, 24576, 13), (0, 28087, 14), (2, 32375, 15), (1, 37031, 16)])
+def test_rows_in_slices(dtype, V, slices):
+    """Rows in every number of slices: chosen words in one of them, in all, and equal ones across their edges."""
+    assert bs.bs_beam_step_workspace_bytes(dtype, 1, 1, V, 1) == slices * 24
+    dtype = TYPES[dtype]
+    logits, scores = draw(1, 1, V, dtype)
+    check(logits, scores, n=33)
+    check(logits, scores, end=3)
+    check(torch.arange(V, device=DEV).float().div(-V).to(dtype).view(1, V), scores, n=40)
+    check((torch.arange(V, device=DEV) % 97 == 5).to(dtype).view(1, V), scores, n=17)
+    logits[:, : V // 2] = -math.inf
+    check(logits, scores, n=9)
+    logits[:, 5: V - 3] = -math.inf
+    check(logits, scores, n=9)
+
+
 def test_rows_anywhere():
     """Rows that are slices of wider ones and start on no boundary give the same bits."""
     for dtype in TYPES:
