@@ -9,7 +9,7 @@
 // logits have the same sums to the last bit, and tie.  A row's n largest are found as bs_logprobs finds them.
 // A second kernel joins the rows of a sequence: a candidate's total is scores + ((x - m) - log s); of the lists that are full each
 // answers for its share of the n, the least of those totals is a bound, and what reaches it is ordered by counting what comes before.
-// 256 x 16 rows of 32003 in bfloat16 take 92 to 96 us, of 9740 vector instructions each, and the join 6; 32 x 8 rows 14 and 4.3, latency.
+// 256 x 16 rows of 32003 in bfloat16 take 91 to 96 us, of 9740 vector instructions each, and the join 6; 32 x 8 rows 14 and 4.3, latency.
 //
 // The states.  Bound: HBM.  8 states of 2048 and 513 words for 256 x 16 beams, 234 MB, take 40 us.
 #include <type_traits>
