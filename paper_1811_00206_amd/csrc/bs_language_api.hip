@@ -37,18 +37,29 @@ bool aligned4(const void* a, const void* b, const void* c, const void* d) {
     return aligned(a, 4) && aligned(b, 4) && aligned(c, 4) && aligned(d, 4);
 }
 
-// Whether one of `ra` rows of `na` bytes, pa apart from a on, and one of `rb` rows of nb bytes, pb apart from b on, share any: rows of one
-// tensor do not, and na <= pa, nb <= pb.
-bool rows_meet(uintptr_t a, int64_t pa, uintptr_t b, int64_t pb, int64_t ra, int64_t na, int64_t rb, int64_t nb) {
-    const int64_t d = (int64_t)(b - a);
-    if (d >= (ra - 1) * pa + na || -d >= (rb - 1) * pb + nb) return false;
+// `count` rows of `bytes` bytes, `pitch` apart.  Nothing is asked of a single row's pitch.
+struct Rows {
+    uintptr_t at;
+    int64_t pitch, count, bytes;
+    Rows(const void* p, int64_t rows, int64_t n, int64_t ld, int64_t size) : at(reinterpret_cast<uintptr_t>(p)), count(rows), bytes(n * size) {
+        if (rows == 1) pitch = bytes;
+        else if (__builtin_mul_overflow(ld, size, &pitch)) pitch = -1;
+    }
+    bool fit() const { return pitch >= bytes && pitch <= (INT64_MAX - bytes) / count; }      // some memory holds them
+};
+
+// Whether a row of one and a row of the other share any byte: rows of one tensor do not.
+bool rows_meet(const Rows& a, const Rows& b) {
+    if (!a.fit() || !b.fit()) return true;
+    const int64_t d = (int64_t)(b.at - a.at);
+    if (d >= (a.count - 1) * a.pitch + a.bytes || -d >= (b.count - 1) * b.pitch + b.bytes) return false;
     // rows of a to look at: where both are equally far apart the same distances come again, so that one with all b beside it will do
     const auto meets = [&](int64_t i) {
-        const int64_t to = i * pa - d, j = to >= 0 ? to / pb : -1;      // the last row of b that starts at or before it
-        return (j >= 0 && j < rb && to - j * pb < nb) || (j + 1 < rb && (j + 1) * pb - to < na);
+        const int64_t to = i * a.pitch - d, j = to >= 0 ? to / b.pitch : -1;      // the last row of b that starts at or before it
+        return (j >= 0 && j < b.count && to - j * b.pitch < b.bytes) || (j + 1 < b.count && (j + 1) * b.pitch - to < a.bytes);
     };
-    if (pa == pb && ra == rb) return meets(d >= 0 ? ra - 1 : 0);
-    for (int64_t i = 0; i < ra; ++i)
+    if (a.pitch == b.pitch && a.count == b.count) return meets(d >= 0 ? a.count - 1 : 0);
+    for (int64_t i = 0; i < a.count; ++i)
         if (meets(i)) return true;
     return false;
 }
@@ -151,9 +162,7 @@ int bs_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, in
     if (ldg < V) return BS_ERR_SHAPE;
     const int64_t size = bs::dtype_bytes(dtype);
     if (!aligned(grad, size)) return BS_ERR_ALIGN;
-    if ((grad != logits || ldg != ld) &&
-        rows_meet(reinterpret_cast<uintptr_t>(logits), ld * size, reinterpret_cast<uintptr_t>(grad), ldg * size, T, V * size, T, V * size))
-        return BS_ERR_UNSUPPORTED;
+    if ((grad != logits || ldg != ld) && rows_meet(Rows(logits, T, V, ld, size), Rows(grad, T, V, ldg, size))) return BS_ERR_UNSUPPORTED;
     if (!aligned4(lse, entropy, g_logprob, g_entropy)) return BS_ERR_ALIGN;
     return bs::launch_logprobs_backward(logits, dtype, T, V, ld, targets, lse, entropy, g_logprob, g_entropy, grad, ldg,
                                         static_cast<hipStream_t>(stream));
@@ -205,8 +214,7 @@ int bs_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t 
     if (!type_ok(dtype) || N > kMost || M * N > kMostOutputs) return BS_ERR_UNSUPPORTED;
     const size_t size = bs::dtype_bytes(dtype);
     if (!aligned(x, size) || !aligned(y, size) || !aligned(bias, 4)) return BS_ERR_ALIGN;
-    if (rows_meet(reinterpret_cast<uintptr_t>(x), ldx * size, reinterpret_cast<uintptr_t>(y), ldy * size, N, K * size, N, M * size))
-        return BS_ERR_UNSUPPORTED;
+    if (rows_meet(Rows(x, N, K, ldx, size), Rows(y, N, M, ldy, size))) return BS_ERR_UNSUPPORTED;
     return bs::launch_mx4_gemm(codes, scales, M, K, x, ldx, nullptr, nullptr, dtype, N, bias, y, ldy, workspace, workspace_bytes,
                                static_cast<hipStream_t>(stream));
 }
@@ -267,15 +275,14 @@ int bs_beam_reorder(int count, const void* const* states, void* const* outs, con
         bytes += row_bytes[i];
     }
     if (!aligned(parents, 4)) return BS_ERR_ALIGN;
-    const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+    const Rows chosen(parents, 1, B * W, B * W, 4);
     for (int i = 0; i < count; ++i) {
-        if (rows_meet(at(parents), B * W * 4, at(outs[i]), out_pitch[i], 1, B * W * 4, B * W, row_bytes[i])) return BS_ERR_UNSUPPORTED;
+        const Rows out(outs[i], B * W, row_bytes[i], out_pitch[i], 1);
+        if (rows_meet(chosen, out)) return BS_ERR_UNSUPPORTED;
         for (int j = 0; j < count; ++j) {
             const bool itself = i == j && states[j] == outs[i] && pitch[j] == out_pitch[i];
-            if (!itself && rows_meet(at(states[j]), pitch[j], at(outs[i]), out_pitch[i], B * W, row_bytes[j], B * W, row_bytes[i]))
-                return BS_ERR_UNSUPPORTED;
-            if (j < i && rows_meet(at(outs[j]), out_pitch[j], at(outs[i]), out_pitch[i], B * W, row_bytes[j], B * W, row_bytes[i]))
-                return BS_ERR_UNSUPPORTED;
+            if (!itself && rows_meet(Rows(states[j], B * W, row_bytes[j], pitch[j], 1), out)) return BS_ERR_UNSUPPORTED;
+            if (j < i && rows_meet(Rows(outs[j], B * W, row_bytes[j], out_pitch[j], 1), out)) return BS_ERR_UNSUPPORTED;
         }
     }
     return bs::launch_beam_reorder(count, states, outs, row_bytes, pitch, out_pitch, B, W, parents, static_cast<hipStream_t>(stream));
