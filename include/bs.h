@@ -451,9 +451,9 @@ int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_
  * y[n][r] = sum_k W[r][k] * X[n][k] (+ bias[r]) for N rows of activations, where X is x as bs_mx4_pack would round it: the matrix
  * unit multiplies 4-bit numbers on both sides.
  * x     DEVICE in   N rows of K of type dtype, ldx >= K apart       y  DEVICE out  N rows of M, same type, ldy >= M apart
- *                                                                               (rows that share bytes with x's: BS_ERR_UNSUPPORTED)
  * bias  DEVICE in   M fp32, may be NULL
  * bs_mx4_gemm_packed takes x packed already (an activation that several matrices multiply); dtype is y's type there.
+ * y over any byte that is read: BS_ERR_UNSUPPORTED.
  * Products are exact, sums fp32.  The order of the additions depends on M, K and N alone, and is the same in both calls.
  * A NaN or an infinity in x makes its row of y NaN, a block of W that is NaN its column.  N <= 2^24, M N <= 2^36.
  * workspace as for bs_spmm.

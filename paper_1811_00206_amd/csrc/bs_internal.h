@@ -89,6 +89,18 @@ int launch_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t
 int launch_logprobs_backward(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const int64_t* targets, const float* lse,
                              const float* entropy, const float* g_logprob, const float* g_entropy, void* grad, int64_t ldg,
                              hipStream_t st);
+// `count` rows of `bytes` bytes, `pitch` apart.  Nothing is asked of a single row's pitch.
+struct Rows {
+    uintptr_t at;
+    int64_t pitch, count, bytes;
+    Rows(const void* p, int64_t rows, int64_t n, int64_t ld, int64_t size) : at(reinterpret_cast<uintptr_t>(p)), count(rows), bytes(n * size) {
+        if (rows == 1) pitch = bytes;
+        else if (__builtin_mul_overflow(ld, size, &pitch)) pitch = -1;
+    }
+    bool fit() const { return pitch >= bytes && pitch <= (INT64_MAX - bytes) / count; }      // some memory holds them
+};
+// Whether a row of one and a row of the other share any byte; rows of one tensor do not.  (bs_language_api.hip)
+bool rows_meet(const Rows& a, const Rows& b);
 // MX 4-bit matrices (bs_mx4_pack.hip, bs_mx4_gemm.hip) and beam search (bs_beam.hip)
 int launch_mx4_pack(const void* W, int dtype, int64_t M, int64_t K, int64_t ld, uint8_t* codes, uint8_t* scales, hipStream_t st);
 int launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, void* W, int dtype, hipStream_t st);

@@ -1,6 +1,25 @@
 // C-ABI entry points of the calls on 4-bit matrices and logits: argument validation on the host, then the launchers.
 #include "bs_mx4.h"
 
+namespace bs {
+
+bool rows_meet(const Rows& a, const Rows& b) {
+    if (!a.fit() || !b.fit()) return true;
+    const int64_t d = (int64_t)(b.at - a.at);
+    if (d >= (a.count - 1) * a.pitch + a.bytes || -d >= (b.count - 1) * b.pitch + b.bytes) return false;
+    // rows of a to look at: where both are equally far apart the same distances come again, so that one with all b beside it will do
+    const auto meets = [&](int64_t i) {
+        const int64_t to = i * a.pitch - d, j = to >= 0 ? to / b.pitch : -1;      // the last row of b that starts at or before it
+        return (j >= 0 && j < b.count && to - j * b.pitch < b.bytes) || (j + 1 < b.count && (j + 1) * b.pitch - to < a.bytes);
+    };
+    if (a.pitch == b.pitch && a.count == b.count) return meets(d >= 0 ? a.count - 1 : 0);
+    for (int64_t i = 0; i < a.count; ++i)
+        if (meets(i)) return true;
+    return false;
+}
+
+}  // namespace bs
+
 namespace {
 
 constexpr int64_t kMost = (int64_t)1 << 24;      // rows, columns
@@ -37,32 +56,8 @@ bool aligned4(const void* a, const void* b, const void* c, const void* d) {
     return aligned(a, 4) && aligned(b, 4) && aligned(c, 4) && aligned(d, 4);
 }
 
-// `count` rows of `bytes` bytes, `pitch` apart.  Nothing is asked of a single row's pitch.
-struct Rows {
-    uintptr_t at;
-    int64_t pitch, count, bytes;
-    Rows(const void* p, int64_t rows, int64_t n, int64_t ld, int64_t size) : at(reinterpret_cast<uintptr_t>(p)), count(rows), bytes(n * size) {
-        if (rows == 1) pitch = bytes;
-        else if (__builtin_mul_overflow(ld, size, &pitch)) pitch = -1;
-    }
-    bool fit() const { return pitch >= bytes && pitch <= (INT64_MAX - bytes) / count; }      // some memory holds them
-};
-
-// Whether a row of one and a row of the other share any byte: rows of one tensor do not.
-bool rows_meet(const Rows& a, const Rows& b) {
-    if (!a.fit() || !b.fit()) return true;
-    const int64_t d = (int64_t)(b.at - a.at);
-    if (d >= (a.count - 1) * a.pitch + a.bytes || -d >= (b.count - 1) * b.pitch + b.bytes) return false;
-    // rows of a to look at: where both are equally far apart the same distances come again, so that one with all b beside it will do
-    const auto meets = [&](int64_t i) {
-        const int64_t to = i * a.pitch - d, j = to >= 0 ? to / b.pitch : -1;      // the last row of b that starts at or before it
-        return (j >= 0 && j < b.count && to - j * b.pitch < b.bytes) || (j + 1 < b.count && (j + 1) * b.pitch - to < a.bytes);
-    };
-    if (a.pitch == b.pitch && a.count == b.count) return meets(d >= 0 ? a.count - 1 : 0);
-    for (int64_t i = 0; i < a.count; ++i)
-        if (meets(i)) return true;
-    return false;
-}
+using bs::Rows;
+using bs::rows_meet;
 
 }  // namespace
 

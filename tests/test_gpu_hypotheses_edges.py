@@ -1,0 +1,50 @@
+"""Calls for several hypotheses at the borders of what they take: results beside what is read, and in its place."""
+import pytest
+import torch
+
+from paper_1811_00206_amd import binding as bs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = (torch.float32, torch.float16, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K,N", [(48, 256, 4), (48, 256, 40), (256, 1024, 80)])
+def test_products_beside_what_they_read(M, K, N, dtype):
+    """All in one piece of memory, each next to the other: y in front of everything, in the middle and behind."""
+    g = torch.Generator().manual_seed(M + N)
+    W, x = bs.bs_mx4_pack(torch.randn(M, K, generator=g).to(DEV)), torch.randn(N, K, generator=g).to(dtype).to(DEV)
+    X, bias = bs.bs_mx4_pack(x), torch.randn(M, generator=g).to(DEV)
+    want = bs.bs_mx4_gemm(*W, x, bias=bias)
+    parts, size = {"codes": W[0], "scales": W[1], "x": x, "x_codes": X[0], "x_scales": X[1], "bias": bias}, N * M * x.element_size()
+    for order in (["y", *parts], ["codes", "x", "x_codes", "y", "scales", "x_scales", "bias"], [*parts, "y"]):
+        lengths = {k: v.numel() * v.element_size() for k, v in parts.items()} | {"y": size}
+        assert all(n % 16 == 0 for n in lengths.values())
+        room, at, placed = torch.zeros(sum(lengths.values()), dtype=torch.uint8, device=DEV), 0, {}
+        for k in order:
+            like = want if k == "y" else parts[k]
+            placed[k] = room[at:at + lengths[k]].view(like.dtype).view(like.shape)
+            if k != "y":
+                placed[k].copy_(like)
+            at += lengths[k]
+        y = placed["y"]
+        assert torch.equal(bs.bs_mx4_gemm(placed["codes"], placed["scales"], placed["x"], bias=placed["bias"], out=y), want)
+        y.zero_()
+        assert torch.equal(bs.bs_mx4_gemm_packed(placed["codes"], placed["scales"], placed["x_codes"], placed["x_scales"], K, dtype=dtype, bias=placed["bias"], out=y), want)
+        assert all(torch.equal(placed[k], v) for k, v in parts.items())
+
+
+def test_a_product_over_its_operands_is_refused():
+    M, K, N = 128, 512, 8
+    codes, scales = bs.bs_mx4_pack(torch.randn(M, K, device=DEV))
+    x_codes, x_scales = bs.bs_mx4_pack(torch.randn(N, K, device=DEV))
+    kept = [t.clone() for t in (codes, scales, x_codes, x_scales)]
+    for over in (codes, x_codes):
+        out = over.flatten()[:N * 64 * 4].view(torch.float32)[: N * 16].view(N, 16)
+        small = codes[:16], scales[:16]
+        with pytest.raises(bs.BsError) as e:
+            bs.bs_mx4_gemm_packed(*small, x_codes, x_scales, K, out=out)
+        assert e.value.status == 3
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((codes, scales, x_codes, x_scales), kept))

@@ -32,3 +32,31 @@ def test_the_pitch_of_a_single_row_does_not_count():
     """
     out = subprocess.run([sys.executable, "-c", textwrap.dedent(code)], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, (out.returncode, out.stdout + out.stderr)
+
+
+def test_products_refuse_a_result_over_what_they_read():
+    """Workgroups store their part of y while others still read the matrix, x or the bias."""
+    lib, null, far = b.load_library(), ctypes.c_void_p(0), 1 << 40
+    M, K, N = 40, 300, 9      # rows of the matrix are 192 bytes of codes and 12 of scales
+    at = {"codes": 1 << 20, "scales": 2 << 20, "x": 3 << 20, "x_scales": 4 << 20, "bias": 5 << 20}
+    sizes = {"codes": M * 192, "scales": M * 12, "x_scales": N * 12, "bias": M * 4}
+    for dtype, size in ((0, 4), (1, 2), (2, 2)):
+        for ldy in (M, M + 7):
+            span = ((N - 1) * ldy + M) * size
+            for packed in (False, True):
+                x_bytes = N * 192 if packed else ((N - 1) * (K + 3) + K) * size
+
+                def status(y):
+                    p = {k: ctypes.c_void_p(v) for k, v in at.items()}
+                    if packed:
+                        return lib.bs_mx4_gemm_packed(p["codes"], p["scales"], M, K, p["x"], p["x_scales"], N, p["bias"], ctypes.c_void_p(y), dtype, ldy, null,
+                                                      0, null)
+                    return lib.bs_mx4_gemm(p["codes"], p["scales"], M, K, p["x"], dtype, N, K + 3, p["bias"], ctypes.c_void_p(y), ldy, ctypes.c_void_p(far), 1 << 20,
+                                           null)
+
+                for what, first in at.items():
+                    if what == "x_scales" and not packed:
+                        continue
+                    last = first + (x_bytes if what == "x" else sizes[what]) - size
+                    for y in (first, last, first - span + size):
+                        assert status(y) == 3, (what, dtype, ldy, packed, y - first)
