@@ -442,6 +442,7 @@ size_t bs_mx4_scales_bytes(int64_t M, int64_t K);
  * With e the biased exponent of a block's largest magnitude as fp32 (0 for subnormal numbers): s = max(e - 2, 0), and the code is the
  * number nearest to w * 2^(127 - s), the even code of two that are equally near, 6 for all that is larger; its sign is w's.
  * A block that holds an infinity or a NaN: s = 255, codes 0.
+ * Both calls: an output over what is read, or over the other one, BS_ERR_UNSUPPORTED.
  */
 int bs_mx4_pack(const void* W, int dtype, int64_t M, int64_t K, int64_t ld, uint8_t* codes, uint8_t* scales, void* stream);
 /* W  DEVICE out  M x K, contiguous: the values the codes stand for, rounded to dtype */

@@ -56,6 +56,8 @@ bool aligned4(const void* a, const void* b, const void* c, const void* d) {
     return aligned(a, 4) && aligned(b, 4) && aligned(c, 4) && aligned(d, 4);
 }
 
+using bs::mx4_codes_place;
+using bs::mx4_scales_place;
 using bs::Rows;
 using bs::rows_meet;
 
@@ -178,6 +180,8 @@ int bs_mx4_pack(const void* W, int dtype, int64_t M, int64_t K, int64_t ld, uint
     if (ld < K) return BS_ERR_SHAPE;
     if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
     if (!aligned(W, bs::dtype_bytes(dtype))) return BS_ERR_ALIGN;
+    const Rows from(W, M, K, ld, bs::dtype_bytes(dtype)), c = mx4_codes_place(codes, M, K), sc = mx4_scales_place(scales, M, K);
+    if (rows_meet(c, from) || rows_meet(sc, from) || rows_meet(c, sc)) return BS_ERR_UNSUPPORTED;
     return bs::launch_mx4_pack(W, dtype, M, K, ld, codes, scales, static_cast<hipStream_t>(stream));
 }
 
@@ -187,6 +191,8 @@ int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_
     if (st) return st;
     if (!type_ok(dtype)) return BS_ERR_UNSUPPORTED;
     if (!aligned(W, bs::dtype_bytes(dtype))) return BS_ERR_ALIGN;
+    const Rows to(W, 1, M * K, 0, bs::dtype_bytes(dtype));
+    if (rows_meet(mx4_codes_place(codes, M, K), to) || rows_meet(mx4_scales_place(scales, M, K), to)) return BS_ERR_UNSUPPORTED;
     return bs::launch_mx4_unpack(codes, scales, M, K, W, dtype, static_cast<hipStream_t>(stream));
 }
 

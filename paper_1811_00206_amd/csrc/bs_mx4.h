@@ -12,6 +12,8 @@ namespace bs {
 constexpr int64_t mx4_chunks(int64_t K) { return (K + 127) / 128; }         // of four blocks
 constexpr int64_t mx4_row_bytes(int64_t K) { return 64 * mx4_chunks(K); }
 constexpr int64_t mx4_scale_pitch(int64_t K) { return 4 * mx4_chunks(K); }
+inline Rows mx4_codes_place(const uint8_t* codes, int64_t M, int64_t K) { return Rows(codes, 1, M * mx4_row_bytes(K), 0, 1); }
+inline Rows mx4_scales_place(const uint8_t* scales, int64_t M, int64_t K) { return Rows(scales, 1, M * mx4_scale_pitch(K), 0, 1); }
 
 #ifdef __HIPCC__
 

@@ -388,9 +388,8 @@ int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int6
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))) return BS_ERR_WORKSPACE;
     // y over what workgroups read while others store
     const Rows out(y, N, M, ldy, dtype_bytes(dtype));
-    if (rows_meet(Rows(codes, 1, M * mx4_row_bytes(K), 0, 1), out) || rows_meet(Rows(scales, 1, M * mx4_scale_pitch(K), 0, 1), out) ||
-        (bias && rows_meet(Rows(bias, 1, M, 0, 4), out)) ||
-        (!x && (rows_meet(Rows(x_codes, 1, N * mx4_row_bytes(K), 0, 1), out) || rows_meet(Rows(x_scales, 1, N * mx4_scale_pitch(K), 0, 1), out))))
+    if (rows_meet(mx4_codes_place(codes, M, K), out) || rows_meet(mx4_scales_place(scales, M, K), out) || (bias && rows_meet(Rows(bias, 1, M, 0, 4), out)) ||
+        (!x && (rows_meet(mx4_codes_place(x_codes, N, K), out) || rows_meet(mx4_scales_place(x_scales, N, K), out))))
         return BS_ERR_UNSUPPORTED;
     uint8_t* at = static_cast<uint8_t*>(workspace);
     const bool dense = x && fused(p, M, K, N);

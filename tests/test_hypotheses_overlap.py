@@ -60,3 +60,31 @@ def test_products_refuse_a_result_over_what_they_read():
                     last = first + (x_bytes if what == "x" else sizes[what]) - size
                     for y in (first, last, first - span + size):
                         assert status(y) == 3, (what, dtype, ldy, packed, y - first)
+
+
+def test_packing_refuses_codes_and_scales_over_the_matrix_or_each_other():
+    lib, null = b.load_library(), ctypes.c_void_p(0)
+    M, K = 7, 300
+    for dtype, size in ((0, 4), (1, 2), (2, 2)):
+        for ld in (K, K + 5):
+            W, far, span = 1 << 20, 1 << 30, ((M - 1) * ld + K) * size
+
+            def pack(codes, scales):
+                return lib.bs_mx4_pack(ctypes.c_void_p(W), dtype, M, K, ld, ctypes.c_void_p(codes), ctypes.c_void_p(scales), null)
+
+            end = (W + span - 1) // 16 * 16      # in the last row, whose end no boundary of 16 bytes has to be
+            for codes in (W, W + 16, W - M * 192 + 16, end):
+                assert pack(codes, far) == 3, (dtype, ld, codes - W)
+            for scales in (W, W - M * 12 + 4, (W + span - 1) // 4 * 4):
+                assert pack(far, scales) == 3, (dtype, ld, scales - W)
+            for scales in (far, far + M * 192 - 4, far - M * 12 + 4):
+                assert pack(far, scales) == 3, (dtype, ld, scales - far)
+
+
+def test_unpacking_refuses_a_matrix_over_its_codes_and_scales():
+    lib, null = b.load_library(), ctypes.c_void_p(0)
+    M, K, codes, scales = 7, 300, 1 << 20, 1 << 30
+    for dtype, size in ((0, 4), (1, 2), (2, 2)):
+        for at, there in ((codes, M * 192), (scales, M * 12)):
+            for W in (at, at + there - size, at - M * K * size + size):
+                assert lib.bs_mx4_unpack(ctypes.c_void_p(codes), ctypes.c_void_p(scales), M, K, ctypes.c_void_p(W), dtype, null) == 3, (dtype, W - at)
