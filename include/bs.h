@@ -484,6 +484,7 @@ int bs_mx4_gemm_plan(int64_t M, int64_t K, int64_t N, int64_t* out, int n_out);
  * Scores are compared in 64 bits before they are rounded to fp32; the lower beam, then the lower word comes first among equals.
  * What offers nothing: a word whose logit is -inf; a beam whose score is not finite; a beam that goes on with a logit that is NaN or
  * +inf.  Where fewer than n continuations are left the rest have score -inf, word max(end, 0), parent min(place, W - 1), and are finished.
+ * Where n is W, out_scores may be scores and out_finished finished; outputs over inputs or one another otherwise: BS_ERR_UNSUPPORTED.
  * 1 <= W <= BS_BEAM_WIDTH_MAX, 1 <= n <= BS_BEAM_WIDTH_MAX.  workspace as for bs_spmm.
  */
 #define BS_BEAM_WIDTH_MAX 64

@@ -636,6 +636,17 @@ int launch_beam_step(const void* logits, int dtype, int64_t B, int W, int64_t V,
                      void* workspace, size_t workspace_bytes, hipStream_t st) {
     const size_t need = beam_step_workspace_bytes(dtype, B, W, V, n);
     if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)) return BS_ERR_WORKSPACE;
+    // A sequence's workgroup of the join reads that sequence's scores and flags, and stores its outputs behind a barrier: those may take
+    // the others' place where they are as many.
+    const Rows outs[] = {{out_scores, 1, B * n, 0, 4}, {out_tokens, 1, B * n, 0, 4}, {out_parents, 1, B * n, 0, 4}, {out_finished, 1, B * n, 0, 1}};
+    const Rows x(logits, B * W, V, ld, dtype_bytes(dtype)), before(scores, 1, B * W, 0, 4), over(finished, 1, B * W, 0, 1);
+    for (int i = 0; i < 4; ++i) {
+        if (rows_meet(outs[i], x)) return BS_ERR_UNSUPPORTED;
+        if (!(i == 0 && out_scores == scores && n == W) && rows_meet(outs[i], before)) return BS_ERR_UNSUPPORTED;
+        if (finished && !(i == 3 && out_finished == finished && n == W) && rows_meet(outs[i], over)) return BS_ERR_UNSUPPORTED;
+        for (int j = 0; j < i; ++j)
+            if (rows_meet(outs[i], outs[j])) return BS_ERR_UNSUPPORTED;
+    }
     const Plan p = plan_for(dtype, B * W, W, V, n);
     Args g{};
     g.logits = logits; g.B = B; g.V = V; g.ld = ld; g.end = end; g.W = W; g.n = n;

@@ -48,3 +48,18 @@ def test_a_product_over_its_operands_is_refused():
         assert e.value.status == 3
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((codes, scales, x_codes, x_scales), kept))
+
+
+@pytest.mark.parametrize("B,W,V", [(1, 4, 5000), (40, 7, 900), (150, 8, 1500)])
+def test_a_step_in_place(B, W, V):
+    """Scores and flags over those before: the same results."""
+    import ctypes
+    lib, g = bs.load_library(), torch.Generator().manual_seed(B)
+    logits, scores = torch.randn(B * W, V, generator=g).to(DEV), torch.randn(B, W, generator=g).to(DEV)
+    finished = (torch.rand(B, W, generator=g) < 0.3).to(DEV)
+    want = bs.bs_beam_step(logits, scores, finished, end=3)
+    tokens, parents = (torch.empty((B, W), dtype=torch.int32, device=DEV) for _ in range(2))
+    workspace = torch.empty(bs.bs_beam_step_workspace_bytes(bs.BS_F32, B, W, V, W), dtype=torch.uint8, device=DEV)
+    p = [ctypes.c_void_p(t.data_ptr()) for t in (logits, scores, finished, tokens, parents, workspace)]
+    assert lib.bs_beam_step(p[0], 0, B, W, V, V, p[1], p[2], 3, W, p[1], p[3], p[4], p[2], p[5], workspace.numel(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    assert all(torch.equal(a, b) for a, b in zip((scores, tokens, parents, finished), want))

@@ -88,3 +88,33 @@ def test_unpacking_refuses_a_matrix_over_its_codes_and_scales():
         for at, there in ((codes, M * 192), (scales, M * 12)):
             for W in (at, at + there - size, at - M * K * size + size):
                 assert lib.bs_mx4_unpack(ctypes.c_void_p(codes), ctypes.c_void_p(scales), M, K, ctypes.c_void_p(W), dtype, null) == 3, (dtype, W - at)
+
+
+def test_a_step_refuses_outputs_over_inputs_or_one_another():
+    """A sequence's workgroup stores while others still read.  Scores and finished flags alone may take their inputs' place, whole."""
+    lib, null = b.load_library(), ctypes.c_void_p(0)
+    B, W, V = 3, 5, 300
+    for n in (W, 4, 9):
+        for dtype, size in ((0, 4), (1, 2), (2, 2)):
+            for ld in (V, V + 11):
+                inputs = {"logits": (1 << 20, ((B * W - 1) * ld + V) * size), "scores": (2 << 20, B * W * 4), "finished": (3 << 20, B * W)}
+                outputs = {"scores": 4 * B * n, "tokens": 4 * B * n, "parents": 4 * B * n, "finished": B * n}
+
+                def status(**places):
+                    out = {k: ctypes.c_void_p(places.get(k, (5 + i) << 20)) for i, k in enumerate(outputs)}
+                    p = {k: ctypes.c_void_p(v[0]) for k, v in inputs.items()}
+                    return lib.bs_beam_step(p["logits"], dtype, B, W, V, ld, p["scores"], p["finished"], 2, n, out["scores"], out["tokens"], out["parents"], out["finished"],
+                                            ctypes.c_void_p(1 << 30), 1 << 30, null)
+
+                for k, mine in outputs.items():
+                    unit = 1 if k == "finished" else 4
+                    for what, (first, there) in inputs.items():
+                        places = {first, (first + there - 1) // unit * unit, -(-(first - mine + 1) // unit) * unit}
+                        if what == k and n == W:
+                            places.remove(first)      # in place
+                        for at in places:
+                            assert status(**{k: at}) == 3, (k, what, n, dtype, ld, at - first)
+                    for other, there in outputs.items():
+                        if other != k:
+                            for at in (20 << 20, (20 << 20) + (there - 1) // unit * unit, (20 << 20) - mine + 4):
+                                assert status(**{other: 20 << 20, k: at}) == 3, (k, other, n, at)
