@@ -516,7 +516,11 @@ struct Plan {
 Plan plan_for(int dtype, int64_t rows, int W, int64_t V, int n) {
     const int E = 16 / dtype_bytes(dtype);
     const int64_t vectors = (V + E - 1) / E;
-    if (rows >= (V <= 2048 ? 1024 : 2048)) return {true, 1, vectors};
+    // A wavefront for a row takes the n-th largest of its 64 lanes' largest for the bound: near n = 64 that is the least of all of them,
+    // and so many words reach it that the list floods, unless it has room for the whole row.  256 x 16 rows of 2000 in bfloat16 take 64 us
+    // for n = 58, 183 for 60 and 329 for 64, a workgroup for a row 65, 67 and 69; 32 x 64 of 8003 for n = 64 850, and 207; 128 x 64 of
+    // 32003 2824, and 379; 256 x 16 of 700 in binary16 for n = 56 62, and 67, for 58 140, and 70; 1024 x 4 of 256 for n = 64 47, and 54.
+    if ((n < 58 || V <= kList) && rows >= (V <= 2048 ? 1024 : 2048)) return {true, 1, vectors};
     // Slices of a row: as many as an estimate of the time, in microseconds, is least for.  A compute unit's workgroups take .04 for each
     // element of a thread and 1 more, one alone is bound by latency, and the join takes longer from one candidate a thread on.  (Seventeen
     // sizes that were timed with 1 to 16 slices meet it within 2: 5 x 9 rows of 101681 22.3 us with 16, 16.1 with 5, 28.8 with 1; 123 x 4 of

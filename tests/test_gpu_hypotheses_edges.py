@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_1811_00206_amd import binding as bs
+from test_gpu_beam import check, draw
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -63,3 +64,56 @@ def test_a_step_in_place(B, W, V):
     p = [ctypes.c_void_p(t.data_ptr()) for t in (logits, scores, finished, tokens, parents, workspace)]
     assert lib.bs_beam_step(p[0], 0, B, W, V, V, p[1], p[2], 3, W, p[1], p[3], p[4], p[2], p[5], workspace.numel(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
     assert all(torch.equal(a, b) for a, b in zip((scores, tokens, parents, finished), want))
+
+
+def _best(f):
+    """Microseconds of a call in a graph of ten, the best of five replays."""
+    f()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(10):
+            f()
+    times = []
+    for _ in range(6):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        graph.replay()
+        end.record()
+        end.synchronize()
+        times.append(begin.elapsed_time(end) * 100)
+    return min(times[1:])
+
+
+@pytest.mark.parametrize("B,W,V,dtype", [(256, 16, 2000, torch.bfloat16), (64, 32, 8003, torch.float32)])
+def test_a_few_more_hypotheses_take_little_longer(B, W, V, dtype):
+    """Many rows of ordinary logits, as many hypotheses as there are lanes: no walk of the row for each of them."""
+    g = torch.Generator(DEV).manual_seed(1)
+    logits, scores = (torch.randn(B * W, V, generator=g, device=DEV) * 3).to(dtype), torch.randn(B, W, generator=g, device=DEV)
+    workspace = torch.empty(max(bs.bs_beam_step_workspace_bytes(0, B, W, V, n) for n in (48, 64)), dtype=torch.uint8, device=DEV)
+    few, many = (_best(lambda: bs.bs_beam_step(logits, scores, n=n, workspace=workspace)) for n in (48, 64))
+    assert many < 3 * few, (few, many)      # a third more of a step's lists, and the join grows by their square: 1.8 times at most
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,W,V", [(16, 64, 200), (16, 64, 256), (16, 64, 257), (16, 64, 1000), (16, 64, 2000), (32, 64, 2500)])
+def test_as_many_hypotheses_as_lanes(B, W, V, dtype):
+    logits, scores = draw(B, W, V, dtype)
+    for n in (57, 58, 64):
+        check(logits, scores, n=n)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,W,V", [(512, 2, 2000), (1024, 2, 2500)])
+def test_floods_of_many_rows(B, W, V, dtype):
+    """A wavefront for a row: more words above the bound than its list takes, because all large ones come to few lanes; more or fewer of them
+    than it has room for in a second pass."""
+    rows, scores = draw(B, W, V, dtype)
+    lane = torch.arange(V, device=DEV) // (16 // rows.element_size()) % 64
+    for lanes, n in ((39, 40), (20, 21), (3, 5), (55, 57)):
+        logits = torch.where(lane < lanes, rows.abs() + 4, -rows.abs())
+        check(logits, scores, n=n)
+    # a hundred words above many equal ones
+    logits = torch.where(torch.arange(V, device=DEV) % 20 == 3, rows.abs() + 1, torch.ones_like(rows))
+    check(logits, scores, n=33)
+    check(logits, scores, n=57)
