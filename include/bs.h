@@ -393,7 +393,7 @@ int bs_q4_moe(const void* x, int dtype, int64_t T, int64_t ldx, int64_t D, const
               size_t workspace_bytes, void* stream);
 
 /*
- * T rows of V logits, ld >= V elements apart (V < 2^31; only as aligned as the type), one target each (< 0: none)
+ * T rows of V logits, ld >= V elements apart (V < 2^31 - 64; only as aligned as the type), one target each (< 0: none)
  *   lse[t]      log of the sum of exp(logits)        entropy[t]  of the row's distribution
  *   logprob[t]  of the target; 0 without one, NaN for one that is not below V
  *   top_values, top_ids  [T][top_n] the top_n largest log probabilities, the lower index first among equals;
@@ -475,13 +475,14 @@ int bs_mx4_gemm_plan(int64_t M, int64_t K, int64_t N, int64_t* out, int n_out);
  * One step of beam search for B sequences of W beams each: of all continuations, the n with the best score.
  *   a beam w that goes on offers every word v:  scores[b][w] + logits[b][w][v] - lse(logits[b][w])
  *   a beam that is finished offers itself:      scores[b][w], with the word `end`
- * logits    DEVICE in   B * W rows of V, ld >= V apart (V < 2^31; only as aligned as the type)
+ * logits    DEVICE in   B * W rows of V, ld >= V apart (V < 2^31 - 64; only as aligned as the type)
  * scores    DEVICE in   B x W fp32, the beams' log probabilities
  * finished  DEVICE in   B x W bytes, not 0 where a beam is finished; may be NULL.  Rows of finished beams are not read.
  * end       the word that finishes a beam; negative: none does (finished ones then offer word 0)
  * out_scores, out_tokens, out_parents, out_finished  DEVICE out  B x n, best first: score, word, the beam it continues, and whether it
  *           is finished (one byte, 0 or 1)
- * Scores are compared in 64 bits before they are rounded to fp32; the lower beam, then the lower word comes first among equals.
+ * Scores are compared in 64 bits before they are rounded to fp32.  Among equals the lower beam comes first; of one beam the larger logit,
+ * also where both make the same score (0 and 1e-20 beside a largest of 5), then the lower word.
  * What offers nothing: a word whose logit is -inf; a beam whose score is not finite; a beam that goes on with a logit that is NaN or
  * +inf.  Where fewer than n continuations are left the rest have score -inf, word max(end, 0), parent min(place, W - 1), and are finished.
  * Where n is W, out_scores may be scores and out_finished finished; outputs over inputs or one another otherwise: BS_ERR_UNSUPPORTED.

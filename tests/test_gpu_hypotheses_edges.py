@@ -117,3 +117,25 @@ def test_floods_of_many_rows(B, W, V, dtype):
     logits = torch.where(torch.arange(V, device=DEV) % 20 == 3, rows.abs() + 1, torch.ones_like(rows))
     check(logits, scores, n=33)
     check(logits, scores, n=57)
+
+
+@pytest.mark.parametrize("V", [50, 3001, 40000])
+def test_words_whose_scores_alone_are_equal(V):
+    """Different logits that make the same total in 64 bits: in the order of the logits, not of the words, and cut to n by it; in one slice of a
+    row, in several, and for all words where the beams' scores leave nothing of them."""
+    logits = torch.full((4, V), -1.0, device=DEV)
+    logits[:, V // 2] = 5.0
+    small = [7, V // 2 + 1, V - 2, 21, V // 2 - 9]
+    for i, at in enumerate(small):
+        logits[:, at] = i * 1e-20
+    scores = torch.tensor([[-1.0, -1.0], [-2.0, -1.0]], device=DEV)
+    for n in (2, 3, 5, 6, 9):
+        tokens = check(logits, scores, n=n)[1]
+        assert tokens[1].tolist()[2:7] == small[::-1][:max(n - 2, 0)]      # behind both beams' best words, -1 and -2 here and -6 there
+    g = torch.Generator().manual_seed(V)
+    logits = torch.randn(6, V, generator=g).to(DEV)
+    scores = torch.tensor([[-1e30, -1e30, -1e30], [-2e30, -1e30, 1e30]], device=DEV)
+    for n in (1, 4, 11):
+        tokens, parents = check(logits, scores, n=n)[1:3]
+        assert parents.tolist() == [[0] * n, [2] * n]
+        assert torch.equal(tokens.long(), torch.topk(logits[[0, 5]], n, -1).indices)
