@@ -530,7 +530,8 @@ Plan plan_for(int dtype, int64_t rows, int W, int64_t V, int n) {
     for (int s = 1; s <= kSlices && (s == 1 || (W * n * s <= kCandidates && vectors >= s * kThreads)); ++s) {
         const double each = (double)V / s / kThreads, alone = .05 * each + 1.5, all = (double)((rows * s + 255) / 256) * (.04 * each + 1);
         const int candidates = W * n * s;
-        const double cost = (all > alone ? all : alone) + .03 * s + (candidates <= kThreads ? 0 : 1 + candidates / 600. + (candidates <= 4 * kThreads ? 0 : 3));
+        const double join = candidates <= kThreads ? 0 : 1 + candidates / 600. + (candidates <= 4 * kThreads ? 0 : 3);
+        const double cost = (all > alone ? all : alone) + .03 * s + join;
         if (s > 1 && cost >= least) continue;
         least = cost;
         slices = s;

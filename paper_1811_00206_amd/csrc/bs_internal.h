@@ -105,7 +105,7 @@ bool rows_meet(const Rows& a, const Rows& b);
 int launch_mx4_pack(const void* W, int dtype, int64_t M, int64_t K, int64_t ld, uint8_t* codes, uint8_t* scales, hipStream_t st);
 int launch_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, void* W, int dtype, hipStream_t st);
 // x: a dense one of type dtype, or nullptr where it is packed already
-size_t mx4_gemm_workspace_bytes(bool packed, int dtype, int64_t M, int64_t K, int64_t N);
+size_t mx4_gemm_workspace_bytes(bool packed, int64_t M, int64_t K, int64_t N);
 int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int64_t ldx, const uint8_t* x_codes,
                     const uint8_t* x_scales, int dtype, int64_t N, const float* bias, void* y, int64_t ldy, void* workspace,
                     size_t workspace_bytes, hipStream_t st);

@@ -198,12 +198,12 @@ int bs_mx4_unpack(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_
 
 size_t bs_mx4_gemm_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N) {
     if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost || M * N > kMostOutputs) return 0;
-    return bs::mx4_gemm_workspace_bytes(false, dtype, M, K, N);
+    return bs::mx4_gemm_workspace_bytes(false, M, K, N);
 }
 
 size_t bs_mx4_gemm_packed_workspace_bytes(int dtype, int64_t M, int64_t K, int64_t N) {
     if (!matrix_ok(M, K) || M > kMost || K > kMost || !type_ok(dtype) || N < 1 || N > kMost || M * N > kMostOutputs) return 0;
-    return bs::mx4_gemm_workspace_bytes(true, dtype, M, K, N);
+    return bs::mx4_gemm_workspace_bytes(true, M, K, N);
 }
 
 int bs_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int64_t K, const void* x, int dtype, int64_t N, int64_t ldx,

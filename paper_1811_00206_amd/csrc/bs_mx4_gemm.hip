@@ -235,20 +235,24 @@ int launch_tiles(Mx4Tiles g, hipStream_t st) {
     if (rc != BS_OK) return rc;
     const int64_t most = 65535;      // rows of a launch
     for (int64_t n = 0; n < g.N; n += most) {
-        hipLaunchKernelGGL(mx4_join_kernel<XT>, dim3((unsigned)((g.M + 1023) / 1024), (unsigned)(g.N - n < most ? g.N - n : most)), dim3(256), 0, st, g, n);
+        const dim3 grid((unsigned)((g.M + 1023) / 1024), (unsigned)(g.N - n < most ? g.N - n : most));
+        hipLaunchKernelGGL(mx4_join_kernel<XT>, grid, dim3(256), 0, st, g, n);
         const int code = hip_status(hipGetLastError());
         if (code != BS_OK) return code;
     }
     return BS_OK;
 }
 
+// Kinds of tiles go by their rows of y, but for the second one of 128 x 128, which has four stages in LDS.
+constexpr int kFourStages = 127;
+
 template <typename XT>
-int launch_tiles(const Mx4Tiles& t, int tn, hipStream_t st) {
-    switch (tn) {
+int launch_tiles(const Mx4Tiles& t, int kind, hipStream_t st) {
+    switch (kind) {
         case 32: return launch_tiles<XT, 32, 128, 1, 4, 4>(t, st);
         case 64: return launch_tiles<XT, 64, 128, 1, 4, 4>(t, st);
         case 96: return launch_tiles<XT, 96, 128, 1, 4, 4>(t, st);
-        case 127: return launch_tiles<XT, 128, 128, 2, 2, 4>(t, st);
+        case kFourStages: return launch_tiles<XT, 128, 128, 2, 2, 4>(t, st);
         case 128: return launch_tiles<XT, 128, 128, 2, 2, 2>(t, st);
         default: return launch_tiles<XT, 256, 256, 2, 2, 2>(t, st);
     }
@@ -272,7 +276,7 @@ struct Tile {
     double alone, full, begin;
 };
 constexpr Tile kTiles[] = {{32, 32, 128, 1, 0.45, 0.45, 2.2}, {64, 64, 128, 1, 0.5, 0.5, 2.8}, {96, 96, 128, 1, 0.56, 0.56, 3.2},
-                           {127, 128, 128, 1, 0.64, 0.64, 3.5}, {128, 128, 128, 2, 0.77, 1.1, 3.0}, {256, 256, 256, 1, 1.75, 1.75, 7.0}};
+                           {kFourStages, 128, 128, 1, 0.64, 0.64, 3.5}, {128, 128, 128, 2, 0.77, 1.1, 3.0}, {256, 256, 256, 1, 1.75, 1.75, 7.0}};
 
 double matrix_us(int64_t M, int chunks) { return (double)M * chunks * 68 / 4.6e6; }
 
@@ -334,6 +338,7 @@ Plan plan_for(int64_t M, int64_t K, int64_t N) {
 }
 
 size_t packed_bytes(int64_t K, int64_t N) { return (size_t)(N * (mx4_row_bytes(K) + mx4_scale_pitch(K)) + 15) / 16 * 16; }
+
 template <typename XT>
 int launch(Args g, const Plan& p, float* sums, hipStream_t st) {
     if (p.tile) {
@@ -376,7 +381,7 @@ void mx4_gemm_plan_describe(int64_t M, int64_t K, int64_t N, int64_t* out, int n
 static size_t workspace_of(const Plan& p, bool packed, int64_t M, int64_t K, int64_t N) {
     return (packed || fused(p, M, K, N) ? 0 : packed_bytes(K, N)) + (p.split > 1 ? (size_t)p.split * M * N * 4 : 0);
 }
-size_t mx4_gemm_workspace_bytes(bool packed, int, int64_t M, int64_t K, int64_t N) {
+size_t mx4_gemm_workspace_bytes(bool packed, int64_t M, int64_t K, int64_t N) {
     return workspace_of(plan_for(M, K, N), packed, M, K, N);
 }
 
@@ -388,7 +393,8 @@ int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int6
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))) return BS_ERR_WORKSPACE;
     // y over what workgroups read while others store
     const Rows out(y, N, M, ldy, dtype_bytes(dtype));
-    if (rows_meet(mx4_codes_place(codes, M, K), out) || rows_meet(mx4_scales_place(scales, M, K), out) || (bias && rows_meet(Rows(bias, 1, M, 0, 4), out)) ||
+    if (rows_meet(mx4_codes_place(codes, M, K), out) || rows_meet(mx4_scales_place(scales, M, K), out) ||
+        (bias && rows_meet(Rows(bias, 1, M, 0, 4), out)) ||
         (!x && (rows_meet(mx4_codes_place(x_codes, N, K), out) || rows_meet(mx4_scales_place(x_scales, N, K), out))))
         return BS_ERR_UNSUPPORTED;
     uint8_t* at = static_cast<uint8_t*>(workspace);
@@ -402,7 +408,8 @@ int launch_mx4_gemm(const uint8_t* codes, const uint8_t* scales, int64_t M, int6
         at += packed_bytes(K, N);
     }
     float* const sums = reinterpret_cast<float*>(at);
-    const Args g{codes, scales, x_codes, x_scales, dense ? x : nullptr, ldx, M, K, N, magic_u32((uint32_t)(16 * mx4_chunks(K))), (int)mx4_chunks(K), 1, 1, bias, y, ldy};
+    const Args g{codes, scales, x_codes, x_scales, dense ? x : nullptr, ldx, M, K, N, magic_u32((uint32_t)(16 * mx4_chunks(K))),
+                 (int)mx4_chunks(K), 1, 1, bias, y, ldy};
     switch (dtype) {
         case BS_F32: return launch<F32>(g, p, sums, st);
         case BS_F16: return launch<F16>(g, p, sums, st);

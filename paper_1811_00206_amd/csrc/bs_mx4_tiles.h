@@ -39,18 +39,22 @@ constexpr int kMx4ScaleBytes = (TN + TM) * 8 * kMx4Group;
 template <int TN, int TM, int NB>
 constexpr int kMx4LdsBytes = NB * kMx4StageBytes<TN, TM> + 2 * kMx4ScaleBytes<TN, TM>;
 
-// 16 (4) bytes for each lane of `lanes` (of the first 32 and of the last), from `base` + a lane's offset to LDS at `to`, lane after lane.  In assembly: the compiler takes
-// every read of LDS for one of what such a load brings, and would wait for all that are on their way.  Nothing in registers is written
-// but M0, which nothing else here uses and which has to be there a wait state before; all lanes are active before and after.
+// 16 (4) bytes for each lane of `lanes` (of the first 32 and of the last), from `base` + a lane's offset to LDS at `to`, lane after lane.
+// In assembly: the compiler takes every read of LDS for one of what such a load brings, and would wait for all that are on their way.
+// Nothing in registers is written but M0, which nothing else here uses and which has to be there a wait state before; all lanes are active
+// before and after.  A load of no lanes is counted and comes back in order like the others: products of one stage, whose first wait lets
+// twice as many loads go on as that stage has, would be wrong otherwise.
 template <int BYTES>
 __device__ __forceinline__ void send_to_lds(const uint8_t* base, uint32_t offset, uint32_t to, uint32_t lanes) {
     static_assert(BYTES == 16 || BYTES == 4);
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(offset),
+        asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(offset),
                      "s"(base), "s"(to), "s"(lanes)
                      : "memory");
     else
-        asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n\ts_mov_b64 exec, -1" ::"v"(offset),
+        asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                     "global_load_lds_dword %0, %1\n\ts_mov_b64 exec, -1" ::"v"(offset),
                      "s"(base), "s"(to), "s"(lanes)
                      : "memory");
 }
@@ -96,8 +100,9 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
     const auto row_of = [&](int r) { return r < TN ? min((uint32_t)r, x_last) : min((uint32_t)(r - TN), w_last); };
 #pragma unroll
     for (int i = 0; i < kCodeLoads; ++i) from[i] = row_of((i * 4 + wave) * 8 + (lane >> 3)) * pitch + 16 * block;
-    // Scales: two lanes bring a row's 32 bytes, the second half in front in every other eight rows, for the sake of LDS banks.  A group that is not whole comes by words, eight lanes a row, those behind the last again
-    // the last.  (Where rows are no multiple of 128 some wavefronts bring what another brings too.)
+    // Scales: two lanes bring a row's 32 bytes, the second half in front in every other eight rows, for the sake of LDS banks.  A group that
+    // is not whole comes by words, eight lanes a row, those behind the last again the last.  (Where rows are no multiple of 128 some
+    // wavefronts bring what another brings too.)
     const auto scale_row = [&](int i) { return min((i * 4 + wave) * 32, kRows - 32); };
     uint32_t scale_from[kScaleLoads];
     uint32_t word_from[kScaleLoads][4];
@@ -123,7 +128,8 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
         const int chunk = 2 * (first + kMx4Group * group), r = scale_row(i);
         const uint32_t to = lds_at + kScalesAt + (group & 1) * kMx4ScaleBytes<TN, TM> + r * 32;
         const bool any = first + kMx4Group * group < last, whole = chunk + 2 * kMx4Group <= g.chunks;
-        const uint32_t lanes = __builtin_amdgcn_readfirstlane(any && whole ? ~0u : 0u), by_words = __builtin_amdgcn_readfirstlane(any && !whole ? ~0u : 0u);
+        const uint32_t lanes = __builtin_amdgcn_readfirstlane(any && whole ? ~0u : 0u),
+                       by_words = __builtin_amdgcn_readfirstlane(any && !whole ? ~0u : 0u);
         const uint8_t* const base = r < TN ? xsc : wsc;
         send_to_lds<16>(base + (int64_t)chunk * 4, scale_from[i], to, lanes);
 #pragma unroll
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(256) void mx4_tiles_kernel(Mx4Tiles g) {
 #pragma unroll
         for (int n = 0; n < kSlots; ++n) part(n);
     };
-        constexpr int kEarly = kCodeLoads / 2, kLeft = (NB - 2) * kCodeLoads;
+    constexpr int kEarly = kCodeLoads / 2, kLeft = (NB - 2) * kCodeLoads;
     static_assert(kLeft < 64);
     const std::integral_constant<int, kLeft> ALL_BUT_LATER;
     const int whole = min(last, g.chunks / 2);      // stages of two chunks
